@@ -25,6 +25,9 @@
  *                                               token staleness, adaptive anchors and refresh
  *   host schedule        gc_schedule_anchors, gc_schedule_full_steps, gc_sampler_step_times,
  *                        gc_schedule_forced_views, gc_schedule_advance_gaps
+ *   inside the denoiser  gc_rope_table, gc_rope   rotary positions of a slice of the views' tokens
+ *                        gc_qk_norm_rope        per-head norms of queries and keys with the rotation
+ *                        gc_attention_plan, gc_attention   attention over packed sequences
  *
  * Conventions shared by every call
  *   - Every call returns GC_OK (0) or a negative GC_ERR_* code and never
@@ -613,6 +616,145 @@ int gc_schedule_anchors(int N, int a, int64_t c, int32_t* anchors_out);
 int gc_schedule_full_steps(int rule, int S, int E, uint8_t* is_full_out);
 int gc_sampler_step_times(const gc_sampler* smp, int S, int k, double* t, double* t_next);
 int gc_sampler_alpha_bar(const gc_sampler* smp, int t, double* abar);
+
+/*
+ * Operators of the denoiser's own blocks.  A cached step runs the denoiser on
+ * the anchor views' tokens only, with every token's structural index and
+ * rotary slot preserved (Sec. 3.2, batch-sliced anchor forward), and assets
+ * have different numbers of foreground tokens: the operators below take
+ * explicit positions and sequences of different lengths laid end to end.
+ *
+ * Heads are tensors [tokens][heads][dim] described by gc_heads: channels are
+ * contiguous, tokens and heads have strides of their own (in elements), so a
+ * part of a fused projection's output is read or written where it lies.  The
+ * data pointer must be 16-byte aligned and both strides a multiple of 16
+ * bytes (GC_ERR_ALIGN).  Storage is GC_F32 or GC_BF16; arithmetic is float32
+ * with one rounding at the end.  dim is a multiple of 8, at most
+ * GC_MAX_HEAD_DIM; a tensor has at most GC_MAX_HEADS heads.
+ */
+#define GC_MAX_HEAD_DIM 256
+#define GC_MAX_HEADS 1024
+#define GC_MAX_AXES 4
+
+typedef struct gc_heads {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} gc_heads;
+
+/* pairs of the rotation: column j turns channels (j, j + R/2) or (2j, 2j + 1) */
+#define GC_ROPE_HALF 0
+#define GC_ROPE_INTERLEAVED 1
+
+/*
+ * Scaling of the rotary frequencies for contexts longer than the one the
+ * model was trained on (40 bytes).  A frequency f turns r = original_len * f
+ * / (2 pi) times over the original context; with g = clamp((r - low) /
+ * (high - low), 0, 1) it becomes g * f + (1 - g) * f / factor: fast columns
+ * stay, slow ones are stretched.  low = high = +inf (or any bounds no r
+ * reaches) stretches all alike.  cos and sin are multiplied by amplitude.
+ */
+typedef struct gc_rope_scaling {
+  double factor;        /* > 0 */
+  double original_len;  /* > 0 */
+  double low, high;     /* low <= high; low == high is a step: r >= low stays */
+  double amplitude;     /* finite */
+} gc_rope_scaling;
+
+/*
+ * Table of cos and sin for gc_rope: table[p][j] = amplitude * (cos(p f_j),
+ * sin(p f_j)), computed in double and rounded once.  The R/2 columns are
+ * dealt to n_axes axes in order, sections[i] columns to axis i; within an
+ * axis of n columns, column i has f = base^(-i/n), then scaled.
+ *   table     device float [n_pos][sum of sections][2] output
+ *   sections  host int32 [n_axes], each >= 1, their sum even and at most
+ *             GC_MAX_HEAD_DIM / 2; n_axes 1..GC_MAX_AXES
+ *   scaling   host, NULL: none
+ */
+int gc_rope_table(float* table, int64_t n_pos, const int32_t* sections, int n_axes, double base,
+                  const gc_rope_scaling* scaling, hipStream_t stream);
+
+/*
+ * Rotary positions.  With R = 2 * (sum of sections), each token's first R
+ * channels of every head are turned in pairs: column j of axis ax(j) turns
+ * (a, b) to (a c - b s, b c + a s), (c, s) = table[positions[t][ax(j)]][j];
+ * channels R.. are copied.  R is a multiple of 4 and at most dim.  A position
+ * outside [0, n_pos) gives NaN in its columns' channels.
+ *   x, out     [n_tokens][heads][dim]; out may be x itself (same pointer and
+ *              strides), and may otherwise share no byte with an input
+ *   positions  device int32 [n_tokens][n_axes]
+ *   table      device float [n_pos][R/2][2] (gc_rope_table)
+ *   layout     GC_ROPE_HALF or GC_ROPE_INTERLEAVED
+ * n_tokens = 0 is legal and does nothing.
+ */
+int gc_rope(const gc_heads* x, int64_t n_tokens, int heads, int dim, int dtype, const int32_t* positions,
+            const float* table, int64_t n_pos, const int32_t* sections, int n_axes, int layout, const gc_heads* out,
+            hipStream_t stream);
+
+/*
+ * RMS norms of queries and keys for each head, and the rotation of gc_rope,
+ * in one pass: y = x / sqrt(mean over dim of x^2 + eps) * gain, turned.
+ *   q, q_out  [n_tokens][heads][dim];  k, k_out  [n_tokens][kv_heads][dim]
+ *   q_gain, k_gain  device float [dim], 16-byte aligned
+ *   eps       finite, >= 0
+ * An output may be its own input; it may otherwise share no byte with an
+ * input or the other output (columns of one fused buffer are apart).
+ */
+int gc_qk_norm_rope(const gc_heads* q, int heads, const gc_heads* k, int kv_heads, int64_t n_tokens, int dim, int dtype,
+                    const float* q_gain, const float* k_gain, double eps, const int32_t* positions, const float* table,
+                    int64_t n_pos, const int32_t* sections, int n_axes, int layout, const gc_heads* q_out,
+                    const gc_heads* k_out, hipStream_t stream);
+
+/*
+ * Attention over packed sequences.  Sequence s has q_lens[s] query tokens and
+ * k_lens[s] key tokens, which lie end to end in q and in k, v.  Query head h
+ * reads kv head h / (heads / kv_heads).  For query token i of its sequence
+ *   s_j = scale * q_i . k_j,  l = sum exp(s_j - max s),  out = sum exp(s_j - max s) v_j / l,
+ *   lse = max s + log l,
+ * over the keys it sees: all of its sequence, or with causal != 0 those with
+ * j <= i + k_len - q_len (the last query sees the last key).  A row that sees
+ * no key, or only scores of -inf, gets out = 0 and lse = -inf.  What a masked key or
+ * value holds, NaN and infinities included, has no effect.
+ *
+ * gc_attention_plan lays out the work of such a batch (host; no device work):
+ * once per set of lengths, whatever the number of layers and steps.  It fills
+ * *info and, unless items is NULL, info->n_items * GC_ATTENTION_ITEM_WORDS
+ * words of items (capacity_words: room there, GC_ERR_CAPACITY if too little).
+ *   q_lens, k_lens  host int32 [n_seq], >= 0, each sum below 2^31; n_seq >= 0
+ *   heads a multiple of kv_heads; dim a multiple of 8
+ *
+ * gc_attention runs it.
+ *   q, out   [sum of q_lens][heads][dim];  k, v  [sum of k_lens][kv_heads][dim]
+ *   lse      device float [heads][sum of q_lens], or NULL
+ *   info     host, as gc_attention_plan filled it
+ *   items    device int32, a copy of the plan's items, 16-byte aligned
+ *   scale    finite, > 0
+ *   workspace  device, info->workspace_bytes, 16-byte aligned, zero before its
+ *            first use; a call leaves it ready for the next.  Calls in flight
+ *            at the same time need workspaces of their own.  May be NULL if
+ *            info->workspace_bytes is 0.
+ * The result does not depend on the order in which blocks run.
+ */
+#define GC_ATTENTION_ITEM_WORDS 12
+
+typedef struct gc_attention_info {
+  int32_t heads, kv_heads, dim, dtype, causal;
+  int32_t n_seq;
+  int32_t total_q, total_k;
+  int32_t kind;       /* kernel variant */
+  int32_t tile_rows;  /* rows of an item: query tokens times heads of a group */
+  int32_t n_items;
+  int32_t n_slots;    /* partial results of split rows */
+  int32_t n_groups;   /* tiles whose keys are split */
+  int32_t reserved[3];
+  int64_t workspace_bytes;
+} gc_attention_info;
+
+int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, int n_seq, int heads, int kv_heads, int dim,
+                      int dtype, int causal, gc_attention_info* info, int32_t* items, int64_t capacity_words);
+int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads* v, const gc_heads* out, float* lse,
+                 const gc_attention_info* info, const int32_t* items, double scale, void* workspace, size_t ws_bytes,
+                 hipStream_t stream);
 
 #ifdef __cplusplus
 }

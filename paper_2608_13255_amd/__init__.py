@@ -12,6 +12,7 @@ library has not been built.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Dict, List, Optional, Sequence, Tuple
@@ -31,6 +32,9 @@ GC_PRED_NONE, GC_PRED_EPS, GC_PRED_V, GC_PRED_VEL = 0, 1, 2, 3
 GC_FULL_PERIODIC, GC_FULL_HEAD_MID_TAIL, GC_FULL_HEAD_TAIL_E = 0, 1, 2
 GC_MAX_VIEWS, GC_MAX_ANCHORS, GC_MAX_GRID = 64, 8, 4094
 GC_NOALLOC_SCRATCH_BYTES = 1 << 20
+GC_MAX_HEAD_DIM, GC_MAX_HEADS, GC_MAX_AXES = 256, 1024, 4
+GC_ROPE_HALF, GC_ROPE_INTERLEAVED = 0, 1
+GC_ATTENTION_ITEM_WORDS = 12
 ERRORS = {-1: "GC_ERR_ARG", -2: "GC_ERR_SHAPE", -3: "GC_ERR_DTYPE", -4: "GC_ERR_ALIGN",
           -5: "GC_ERR_ALIAS", -6: "GC_ERR_CAPACITY", -7: "GC_ERR_HIP"}
 
@@ -60,6 +64,27 @@ class UniPCStep(ctypes.Structure):
                 ("p_mk", ctypes.c_double)]
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class RopeScaling(ctypes.Structure):
+    """gc_rope_scaling: rotary frequencies for contexts longer than the trained one."""
+    _fields_ = [("factor", ctypes.c_double), ("original_len", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("amplitude", ctypes.c_double)]
+
+    def __init__(self, factor: float, original_len: float, low: float = 1.0, high: float = 32.0,
+                 amplitude: float = 1.0):
+        super().__init__(factor, original_len, low, high, amplitude)
+
+
+class AttentionInfo(ctypes.Structure):
+    """gc_attention_info: sizes of a plan (gc_attention_plan)."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "dim", "dtype", "causal", "n_seq", "total_q",
+                                              "total_k", "kind", "tile_rows", "n_items", "n_slots", "n_groups")]
+    _fields_ += [("reserved", ctypes.c_int32 * 3), ("workspace_bytes", ctypes.c_int64)]
+
+
 @dataclass(frozen=True)
 class Sampler:
     """gc_sampler: kind GC_DDIM (linear betas over T steps) or GC_FLOW_EULER."""
@@ -80,6 +105,7 @@ _vp = ctypes.c_void_p
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _i = ctypes.c_int
 _i64 = ctypes.c_int64
+_headsp = ctypes.POINTER(_Heads)
 
 
 def lib() -> ctypes.CDLL:
@@ -137,6 +163,14 @@ def lib() -> ctypes.CDLL:
             "gc_sampler_step_times": ([ctypes.POINTER(_Sampler), _i, _i, ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(ctypes.c_double)], _i),
             "gc_sampler_alpha_bar": ([ctypes.POINTER(_Sampler), _i, ctypes.POINTER(ctypes.c_double)], _i),
+            "gc_rope_table": ([_vp, _i64, _i32p, _i, ctypes.c_double, ctypes.POINTER(RopeScaling), _vp], _i),
+            "gc_rope": ([_headsp, _i64, _i, _i, _i, _vp, _vp, _i64, _i32p, _i, _i, _headsp, _vp], _i),
+            "gc_qk_norm_rope": ([_headsp, _i, _headsp, _i, _i64, _i, _i, _vp, _vp, ctypes.c_double, _vp, _vp, _i64,
+                                 _i32p, _i, _i, _headsp, _headsp, _vp], _i),
+            "gc_attention_plan": ([_i32p, _i32p, _i, _i, _i, _i, _i, _i, ctypes.POINTER(AttentionInfo), _i32p, _i64],
+                                  _i),
+            "gc_attention": ([_headsp, _headsp, _headsp, _headsp, _vp, ctypes.POINTER(AttentionInfo), _vp,
+                              ctypes.c_double, _vp, ctypes.c_size_t, _vp], _i),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -950,3 +984,202 @@ def gc_sampler_alpha_bar(sampler: Sampler, t: int) -> float:
 
 
 lib()
+
+
+# ---------------------------------------------------------------------------
+# operators of the denoiser's own blocks
+# ---------------------------------------------------------------------------
+
+def _heads(t: torch.Tensor, name: str) -> _Heads:
+    """gc_heads of a device tensor [tokens, heads, dim] whose channels are
+    contiguous.  The stride of an axis of one element or none is of no
+    consequence, and torch may hold any there."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, dim] (got {tuple(t.shape)})")
+    n, h, d = t.shape
+    st, sh, sc = t.stride()
+    if sc != 1 and d > 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    if h <= 1:
+        sh = d
+    if n <= 1:
+        st = h * d
+    return _Heads(t.data_ptr(), st, sh)
+
+
+def _like_heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> torch.Tensor:
+    if tuple(t.shape) != tuple(shape) or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must be {like.dtype} {list(shape)} on {like.device} (got {t.dtype} {list(t.shape)} "
+                         f"on {t.device})")
+    return t
+
+
+def _rope_args(positions: torch.Tensor, table: torch.Tensor, sections: Optional[Sequence[int]], x: torch.Tensor):
+    """(positions, table, n_pos, sections, n_axes) as the C calls take them."""
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError("table must be float32 [n_pos, columns, 2]")
+    sec = [int(table.shape[1])] if sections is None else [int(n) for n in sections]
+    if sum(sec) != table.shape[1]:
+        raise ValueError(f"sections {sec} do not sum to the table's {table.shape[1]} columns")
+    if not 1 <= len(sec) <= GC_MAX_AXES:
+        raise ValueError(f"sections must name 1 to {GC_MAX_AXES} axes")
+    T = x.shape[0]
+    if positions.dtype != torch.int32 or tuple(positions.shape) not in ((T, len(sec)),) + (((T,),) if len(sec) == 1 else ()):
+        raise ValueError(f"positions must be int32 [{T}, {len(sec)}]")
+    for t, name in ((positions, "positions"), (table, "table")):
+        if t.device != x.device:
+            raise ValueError(f"{name} must be on {x.device} (got {t.device})")
+    return _dev(positions, "positions"), _dev(table, "table"), int(table.shape[0]), _I32[len(sec)](*sec), len(sec)
+
+
+def gc_rope_table(n_pos: int, sections: Sequence[int], base: float = 10000.0, scaling: Optional[RopeScaling] = None,
+                  table: torch.Tensor = None, device="cuda", stream=None) -> torch.Tensor:
+    """float32 [n_pos, sum(sections), 2]: cos and sin of each position times
+    each column's frequency.  sections: columns of each position axis."""
+    sec = [int(n) for n in sections]
+    if not 1 <= len(sec) <= GC_MAX_AXES:
+        raise ValueError(f"sections must name 1 to {GC_MAX_AXES} axes")
+    if n_pos < 1:
+        raise ValueError("n_pos must be at least 1")
+    fresh = []
+    if table is None:
+        table = torch.empty((n_pos, max(0, sum(sec)), 2), dtype=torch.float32, device=device)
+        fresh.append(table)
+    if table.dtype != torch.float32 or tuple(table.shape) != (n_pos, sum(sec), 2):
+        raise ValueError(f"table must be float32 [{n_pos}, {sum(sec)}, 2]")
+    _check(lib().gc_rope_table(_dev(table, "table"), n_pos, _I32[len(sec)](*sec), len(sec), float(base),
+                               ctypes.byref(scaling) if scaling is not None else None, _stream(stream)),
+           "gc_rope_table")
+    _keep(stream, fresh)
+    return table
+
+
+def gc_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, sections: Optional[Sequence[int]] = None,
+            layout: int = GC_ROPE_HALF, out: torch.Tensor = None, stream=None) -> torch.Tensor:
+    """Rotary positions on heads x [tokens, heads, dim] (float32 or bfloat16,
+    any token and head strides of whole 16 bytes).  positions int32 [tokens]
+    or [tokens, axes]; table from gc_rope_table; sections: its columns of each
+    axis (default: one axis).  out may be x."""
+    hx = _heads(x, "x")
+    dt = dtype_code(x)
+    args = _rope_args(positions, table, sections, x)
+    fresh = []
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        fresh.append(out)
+    ho = _heads(_like_heads(out, "out", x.shape, x), "out")
+    T, H, D = x.shape
+    _check(lib().gc_rope(ctypes.byref(hx), T, H, D, dt, *args, layout, ctypes.byref(ho), _stream(stream)), "gc_rope")
+    _keep(stream, fresh)
+    return out
+
+
+def gc_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain: torch.Tensor, k_gain: torch.Tensor,
+                    positions: torch.Tensor, table: torch.Tensor, eps: float = 1e-6,
+                    sections: Optional[Sequence[int]] = None, layout: int = GC_ROPE_HALF, q_out: torch.Tensor = None,
+                    k_out: torch.Tensor = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """RMS norm of each head of q [tokens, heads, dim] and k [tokens,
+    kv_heads, dim] with gains float32 [dim], and gc_rope, in one pass.  q_out
+    and k_out may be q and k."""
+    hq, hk = _heads(q, "q"), _heads(k, "k")
+    dt = dtype_code(q)
+    T, H, D = q.shape
+    _like_heads(k, "k", (T, k.shape[1], D), q)
+    for g, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        if g.dtype != torch.float32 or tuple(g.shape) != (D,) or g.device != q.device:
+            raise ValueError(f"{name} must be float32 [{D}] on {q.device}")
+    args = _rope_args(positions, table, sections, q)
+    fresh = []
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        fresh.append(q_out)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        fresh.append(k_out)
+    ho, hp = _heads(_like_heads(q_out, "q_out", q.shape, q), "q_out"), _heads(_like_heads(k_out, "k_out", k.shape, q), "k_out")
+    _check(lib().gc_qk_norm_rope(ctypes.byref(hq), H, ctypes.byref(hk), k.shape[1], T, D, dt, _dev(q_gain, "q_gain"),
+                                 _dev(k_gain, "k_gain"), float(eps), *args, layout, ctypes.byref(ho), ctypes.byref(hp),
+                                 _stream(stream)), "gc_qk_norm_rope")
+    _keep(stream, fresh)
+    return q_out, k_out
+
+
+@dataclass
+class AttentionPlan:
+    """Output of gc_attention_plan: the sizes, the items on the device and the
+    workspace (None where no keys are split).  Calls in flight at the same
+    time (on different streams) need a plan of their own each where there is a
+    workspace."""
+    info: AttentionInfo
+    items: torch.Tensor
+    workspace: Optional[torch.Tensor]
+
+
+def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, kv_heads: int, dim: int,
+                      dtype: torch.dtype, causal: bool = False, device="cuda", stream=None) -> AttentionPlan:
+    """Work of attention over packed sequences of these lengths (host lists),
+    for gc_attention: made once and kept while the lengths stay.  The items
+    are copied and the workspace cleared on `stream` (default: torch's current
+    stream)."""
+    if len(q_lens) != len(k_lens):
+        raise ValueError("q_lens and k_lens must have the same length")
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"heads must be float32 or bfloat16 (got {dtype})")
+    code = GC_F32 if dtype == torch.float32 else GC_BF16
+    n = len(q_lens)
+    ql = np.ascontiguousarray(q_lens, dtype=np.int64).reshape(n)
+    kl = np.ascontiguousarray(k_lens, dtype=np.int64).reshape(n)
+    if n and (ql.min() < 0 or kl.min() < 0 or ql.max() >= 1 << 31 or kl.max() >= 1 << 31):
+        raise ValueError("lengths must lie in [0, 2^31)")
+    ql, kl = ql.astype(np.int32), kl.astype(np.int32)
+    info = AttentionInfo()
+    args = (ql.ctypes.data_as(_i32p), kl.ctypes.data_as(_i32p), n, int(heads), int(kv_heads), int(dim), code,
+            int(bool(causal)), ctypes.byref(info))
+    _check(lib().gc_attention_plan(*args, None, 0), "gc_attention_plan")
+    words = info.n_items * GC_ATTENTION_ITEM_WORDS
+    host = np.empty(max(1, words), np.int32)
+    _check(lib().gc_attention_plan(*args, host.ctypes.data_as(_i32p), words), "gc_attention_plan")
+    s = _side_stream(stream)
+    with torch.cuda.stream(s if s is not None else torch.cuda.current_stream()):
+        items = torch.from_numpy(host).to(device)
+        ws = (torch.zeros(info.workspace_bytes, dtype=torch.uint8, device=device) if info.workspace_bytes else None)
+    return AttentionPlan(info, items, ws)
+
+
+def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: AttentionPlan,
+                 scale: Optional[float] = None, out: torch.Tensor = None, lse: torch.Tensor = None,
+                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Attention of q [sum of q_lens, heads, dim] over k, v [sum of k_lens,
+    kv_heads, dim] with the plan of their lengths; scale defaults to
+    1 / sqrt(dim).  Returns (out like q, lse float32 [heads, sum of q_lens])."""
+    info = plan.info
+    H, Hk, D, T, S = info.heads, info.kv_heads, info.dim, info.total_q, info.total_k
+    if dtype_code(q) != info.dtype or tuple(q.shape) != (T, H, D):
+        raise ValueError(f"q must be [{T}, {H}, {D}] of the plan's type (got {q.dtype} {list(q.shape)})")
+    _like_heads(k, "k", (S, Hk, D), q)
+    _like_heads(v, "v", (S, Hk, D), q)
+    if plan.items.device != q.device:
+        raise ValueError(f"the plan is on {plan.items.device}, q on {q.device}")
+    hq, hk, hv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    fresh = []
+    if out is None:
+        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        fresh.append(out)
+    if lse is None:
+        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        fresh.append(lse)
+    ho = _heads(_like_heads(out, "out", (T, H, D), q), "out")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (H, T) or lse.device != q.device:
+        raise ValueError(f"lse must be float32 [{H}, {T}] on {q.device}")
+    ws = plan.workspace
+    _check(lib().gc_attention(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), ctypes.byref(ho), _dev(lse, "lse"),
+                              ctypes.byref(info), _dev(plan.items, "items"),
+                              1.0 / math.sqrt(D) if scale is None else float(scale),
+                              None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(stream)),
+           "gc_attention")
+    _keep(stream, fresh + [plan.items] + ([] if ws is None else [ws]))
+    return out, lse
