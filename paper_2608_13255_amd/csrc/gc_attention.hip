@@ -7,100 +7,60 @@
 #include <cmath>
 #include <vector>
 
-#include "gc_attention_plan.h"
+#include "gc_attention_core.h"
 
 namespace gc {
 namespace {
 
-struct AttentionArgs {
-  const void *q, *k, *v;
-  void* out;
-  float* lse;
-  int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
-  const AttentionItem* items;
-  int heads, kv_heads, group, dim;
-  int total_q, total_k;
-  int causal;
-  float scale;
+// Keys per part: a multiple of every variant's tile.
+constexpr int kPartKeys = 64;
+// Blocks to fill the card with: one for each of 256 compute units, two of the smaller ones.
+constexpr int kCus = 256;
+
+struct Batch {
+  const int32_t *q_lens, *k_lens;
+  int n_seq, group, kv_heads, causal;
 };
 
-constexpr int kSimpleBlock = 256;
-constexpr int kSimpleRows = 32;
+// Keys that the rows [row0, row0 + tile) of a sequence see, at most.
+int keys_seen(const Batch& b, int s, int row0, int tile) {
+  if (!b.causal) return b.k_lens[s];
+  const int64_t rows = (int64_t)b.q_lens[s] * b.group;
+  const int64_t last = (std::min<int64_t>(rows, (int64_t)row0 + tile) - 1) / b.group;
+  const int64_t n = last + b.k_lens[s] - b.q_lens[s] + 1;
+  return (int)std::max<int64_t>(0, std::min<int64_t>(n, b.k_lens[s]));
+}
 
-// One wave takes a row at a time: its 64 lanes score 64 keys, then hold up to
-// four channels each of the weighted sum of the values.
-template <class T>
-__global__ __launch_bounds__(kSimpleBlock) void k_attention_rows(const AttentionArgs p) {
-  __shared__ float qs[kSimpleBlock / 64][GC_MAX_HEAD_DIM];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int kvh = blockIdx.x % p.kv_heads;
-  const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
-  const int last = it.row0 + kSimpleRows < it.rows ? it.row0 + kSimpleRows : it.rows;
-  for (int r = it.row0 + wave; r < last; r += kSimpleBlock / 64) {
-    const int tok = r / p.group, head = kvh * p.group + r % p.group;
-    const int64_t qt = (int64_t)it.q_token0 + tok;
-    const T* q = (const T*)p.q + qt * p.q_token + head * p.q_head;
-    for (int d = lane * 2; d < p.dim; d += 128) {
-      float x[2];
-      load_heads<2>(q + d, x);
-      qs[wave][d] = x[0], qs[wave][d + 1] = x[1];
-    }
-    __builtin_amdgcn_wave_barrier();
-    int n = it.k_len;
-    if (p.causal) n = tok + it.reach < n ? tok + it.reach : n;
-    float m = -__builtin_inff(), l = 0.f, acc[4] = {};
-    for (int j0 = 0; j0 < n; j0 += 64) {
-      const int j = j0 + lane;
-      float s = -__builtin_inff();
-      if (j < n) {
-        const T* k = (const T*)p.k + ((int64_t)it.k_token0 + j) * p.k_token + kvh * p.k_head;
-        float dot = 0.f;
-        for (int d = 0; d < p.dim; d += 4) {
-          float x[4];
-          load_heads<4>(k + d, x);
-          for (int i = 0; i < 4; ++i) dot = __builtin_fmaf(x[i], qs[wave][d + i], dot);
-        }
-        s = dot * p.scale;
-      }
-      float mx = s;
-      for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-      const float mn = fmaxf(m, mx);
-      const float ms = mn == -__builtin_inff() ? 0.f : mn;
-      const float w = expf(s - ms), f = expf(m - ms);
-      m = mn;
-      float sum = w;
-      for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-      l = l * f + sum;
-      for (int i = 0; i < 4; ++i) acc[i] *= f;
-      const int c = n - j0 < 64 ? n - j0 : 64;
-      for (int jj = 0; jj < c; ++jj) {
-        const float wj = __shfl(w, jj);
-        const T* v = (const T*)p.v + ((int64_t)it.k_token0 + j0 + jj) * p.v_token + kvh * p.v_head;
-        for (int i = 0; i < 4; i += 2) {
-          const int d = 2 * lane + 64 * i;
-          if (d < p.dim) {
-            float x[2];
-            load_heads<2>(v + d, x);
-            acc[i] = __builtin_fmaf(wj, x[0], acc[i]);
-            acc[i + 1] = __builtin_fmaf(wj, x[1], acc[i + 1]);
-          }
-        }
-      }
-    }
-    // l > 0, or NaN scores: a row without a key or with scores of -inf alone is 0
-    const bool none = l == 0.f;
-    const float inv = none ? 0.f : 1.f / l;
-    T* o = (T*)p.out + qt * p.o_token + head * p.o_head;
-    for (int i = 0; i < 4; i += 2) {
-      const int d = 2 * lane + 64 * i;
-      if (d < p.dim) {
-        const float x[2] = {none ? 0.f : acc[i] * inv, none ? 0.f : acc[i + 1] * inv};
-        store_heads<2>(o + d, x);
-      }
-    }
-    if (p.lse && lane == 0) p.lse[(int64_t)head * p.total_q + qt] = none ? -__builtin_inff() : m + logf(l);
+int parts_of(int keys, int part) { return keys <= part ? 1 : (int)(((int64_t)keys + part - 1) / part); }
+
+template <class F>
+void each_tile(const Batch& b, int tile, F f) {
+  int64_t q0 = 0, k0 = 0;
+  for (int s = 0; s < b.n_seq; ++s) {
+    const int64_t rows = (int64_t)b.q_lens[s] * b.group;
+    for (int64_t r = 0; r < rows; r += tile) f(s, (int)r, (int)rows, (int)q0, (int)k0);
+    q0 += b.q_lens[s], k0 += b.k_lens[s];
   }
 }
+
+// The variant and the keys a part holds at most (what is longer is split).
+void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
+  int64_t most_rows = 0, work[kAttnKinds] = {}, tiles[kAttnKinds] = {};
+  for (int s = 0; s < b.n_seq; ++s) most_rows = std::max(most_rows, (int64_t)b.q_lens[s] * b.group);
+  for (int k = 0; k < kAttnKinds; ++k) {
+    const int tile = attention_tile_rows(k);
+    each_tile(b, tile, [&](int s, int r, int, int, int) { work[k] += keys_seen(b, s, r, tile), ++tiles[k]; });
+  }
+  if (most_rows <= 32) *kind = kAttnKeys;
+  else *kind = attention_has_rows8(dim, dtype) && tiles[kAttnRows8] * b.kv_heads >= kCus ? kAttnRows8 : kAttnRows4;
+  const int64_t blocks = *kind == kAttnRows8 ? kCus : 2 * kCus;
+  int64_t keys = work[*kind] * b.kv_heads / blocks + 1;
+  keys = std::max<int64_t>(keys, *kind == kAttnKeys ? 256 : 512);
+  keys = (keys + kPartKeys - 1) / kPartKeys * kPartKeys;
+  *part = (int)std::min<int64_t>(keys, 0x7fffffc0);
+}
+
+int64_t counter_bytes(int64_t n_groups, int kv_heads) { return (n_groups * kv_heads * 4 + 255) / 256 * 256; }
 
 }  // namespace
 }  // namespace gc
@@ -118,32 +78,51 @@ extern "C" int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, i
   if (n_seq < 0 || n_seq > (1 << 24)) return fail(GC_ERR_CAPACITY, "%s: n_seq=%d outside [0, 2^24]", who, n_seq);
   if (n_seq > 0 && (!q_lens || !k_lens)) return fail(GC_ERR_ARG, "%s: q_lens or k_lens is null", who);
   const int group = heads / kv_heads;
-  int64_t total_q = 0, total_k = 0, n_items = 0;
-  const int tile = kSimpleRows;
+  int64_t total_q = 0, total_k = 0;
   for (int s = 0; s < n_seq; ++s) {
     if (q_lens[s] < 0 || k_lens[s] < 0) return fail(GC_ERR_SHAPE, "%s: sequence %d has lengths %d and %d", who, s, q_lens[s], k_lens[s]);
     total_q += q_lens[s];
     total_k += k_lens[s];
     if ((int64_t)q_lens[s] * group > 0x7fffffffLL - GC_MAX_HEADS) return fail(GC_ERR_CAPACITY, "%s: sequence %d has over 2^31 query rows", who, s);
-    n_items += ((int64_t)q_lens[s] * group + tile - 1) / tile;
   }
-  if (total_q > 0x7fffffffLL || total_k > 0x7fffffffLL) return fail(GC_ERR_CAPACITY, "%s: over 2^31-1 tokens", who);
+  if (total_q > 0x7fffffffLL || total_k > 0x7fffffffLL - 1024) return fail(GC_ERR_CAPACITY, "%s: over 2^31-1 tokens", who);
+  const Batch b = {q_lens, k_lens, n_seq, group, kv_heads, causal};
+  int kind, part;
+  choose(b, dim, dtype, &kind, &part);
+  const int tile = attention_tile_rows(kind);
+  int64_t n_items = 0, n_slots = 0, n_groups = 0;
+  each_tile(b, tile, [&](int s, int r, int, int, int) {
+    const int n = parts_of(keys_seen(b, s, r, tile), part);
+    n_items += n;
+    if (n > 1) n_slots += n, ++n_groups;
+  });
   if (n_items * kv_heads > 0x7fffffffLL) return fail(GC_ERR_CAPACITY, "%s: over 2^31-1 blocks", who);
   std::memset(info, 0, sizeof(*info));
   info->heads = heads, info->kv_heads = kv_heads, info->dim = dim, info->dtype = dtype, info->causal = causal != 0;
   info->n_seq = n_seq, info->total_q = (int32_t)total_q, info->total_k = (int32_t)total_k;
-  info->kind = kAttnRows, info->tile_rows = tile, info->n_items = (int32_t)n_items;
+  info->kind = kind, info->tile_rows = tile, info->n_items = (int32_t)n_items;
+  info->n_slots = (int32_t)n_slots, info->n_groups = (int32_t)n_groups;
+  info->workspace_bytes = n_slots == 0 ? 0 : counter_bytes(n_groups, kv_heads) +
+                          n_slots * kv_heads * tile * (int64_t)(attention_padded_dim(dim) + 2) * 4;
   if (!items) return GC_OK;
   if (capacity_words < n_items * GC_ATTENTION_ITEM_WORDS)
     return fail(GC_ERR_CAPACITY, "%s: %lld words for %lld items of %d", who, (long long)capacity_words, (long long)n_items, GC_ATTENTION_ITEM_WORDS);
   AttentionItem* it = reinterpret_cast<AttentionItem*>(items);
-  int64_t q0 = 0, k0 = 0;
-  for (int s = 0; s < n_seq; ++s) {
-    const int rows = q_lens[s] * group;
-    for (int r = 0; r < rows; r += tile)
-      *it++ = AttentionItem{(int32_t)q0, rows, r, (int32_t)k0, 0, k_lens[s], k_lens[s] - q_lens[s] + 1, k_lens[s], -1, -1, 1, -1};
-    q0 += q_lens[s], k0 += k_lens[s];
-  }
+  int32_t slot = 0, group_id = 0;
+  each_tile(b, tile, [&](int s, int r, int rows, int q0, int k0) {
+    const int keys = keys_seen(b, s, r, tile), n = parts_of(keys, part);
+    // the parts as equal as whole tiles of keys allow
+    const int64_t step = (((int64_t)keys + n - 1) / n + kPartKeys - 1) / kPartKeys * kPartKeys;
+    for (int i = 0; i < n; ++i) {
+      const int begin = (int)std::min<int64_t>(i * step, keys), end = (int)std::min<int64_t>((i + 1) * step, keys);
+      *it++ = AttentionItem{q0, rows, r, k0, begin, i + 1 == n ? keys : end, k_lens[s] - q_lens[s] + 1, k_lens[s],
+                            n > 1 ? slot + i : -1, n > 1 ? slot : -1, n, n > 1 ? group_id : -1};
+    }
+    if (n > 1) slot += n, ++group_id;
+  });
+  // the longest first: what is left at the end is short
+  AttentionItem* first = reinterpret_cast<AttentionItem*>(items);
+  std::stable_sort(first, it, [](const AttentionItem& x, const AttentionItem& y) { return x.k_end - x.k_begin > y.k_end - y.k_begin; });
   return GC_OK;
 }
 
@@ -155,8 +134,11 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
   if (!info) return fail(GC_ERR_ARG, "%s: info is null", who);
   int rc = check_head_sizes(info->heads, info->dim, info->dtype, who);
   if (rc) return rc;
-  if (info->kv_heads < 1 || info->heads % info->kv_heads || info->kind != kAttnRows || info->tile_rows != kSimpleRows ||
-      info->n_items < 0 || info->total_q < 0 || info->total_k < 0 || info->workspace_bytes < 0)
+  if (info->kv_heads < 1 || info->heads % info->kv_heads || info->kind < 0 || info->kind >= kAttnKinds ||
+      (info->kind == kAttnRows8 && !attention_has_rows8(info->dim, info->dtype)) || info->tile_rows != attention_tile_rows(info->kind) ||
+      info->n_items < 0 || info->total_q < 0 || info->total_k < 0 || info->n_slots < 0 || info->n_groups < 0 ||
+      info->workspace_bytes < (info->n_slots == 0 ? 0 : counter_bytes(info->n_groups, info->kv_heads) + (int64_t)info->n_slots *
+                               info->kv_heads * info->tile_rows * (attention_padded_dim(info->dim) + 2) * 4))
     return fail(GC_ERR_ARG, "%s: info is not gc_attention_plan's", who);
   if (!(scale > 0.0) || !std::isfinite(scale)) return fail(GC_ERR_ARG, "%s: scale must be finite and above 0", who);
   if (info->n_items == 0) return GC_OK;
@@ -171,6 +153,9 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
       (rc = check_heads_out(*out, info->total_q, info->heads, dim, "out", who)))
     return rc;
   if (info->total_k > 0 && ((rc = check_heads(k, dtype, "k", who)) || (rc = check_heads(v, dtype, "v", who)))) return rc;
+  // the range of a tile's buffer ends at its sequence's last key: tokens may not share memory
+  if (info->total_k > 1 && (k->token_stride < dim || v->token_stride < dim))
+    return fail(GC_ERR_SHAPE, "%s: the token strides of k and v must be at least dim=%d", who, dim);
   const int64_t es = dtype_bytes(dtype);
   const size_t out_bytes = (size_t)((info->total_q - 1) * out->token_stride + (info->heads - 1) * out->head_stride + dim) * es;
   const size_t lse_bytes = lse ? (size_t)info->heads * info->total_q * 4 : 0;
@@ -202,8 +187,13 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
   p.total_q = info->total_q, p.total_k = info->total_k;
   p.causal = info->causal;
   p.scale = (float)scale;
-  const dim3 grid((unsigned)(info->n_items * info->kv_heads));
-  if (dtype == GC_F32) hipLaunchKernelGGL(k_attention_rows<float>, grid, dim3(kSimpleBlock), 0, stream, p);
-  else hipLaunchKernelGGL(k_attention_rows<uint16_t>, grid, dim3(kSimpleBlock), 0, stream, p);
+  if (info->n_slots > 0) {
+    p.counters = reinterpret_cast<uint32_t*>(workspace);
+    p.partial = reinterpret_cast<float*>((char*)workspace + counter_bytes(info->n_groups, info->kv_heads));
+  }
+  const unsigned blocks = (unsigned)(info->n_items * info->kv_heads);
+  const bool known = dtype == GC_F32 ? launch_attention_f32(p, info->kind, blocks, stream)
+                                     : launch_attention_bf16(p, info->kind, blocks, stream);
+  if (!known) return fail(GC_ERR_SHAPE, "%s: no kernel for dim=%d", who, dim);
   return after_launch(stream, who);
 }

@@ -1,0 +1,35 @@
+// Attention kernels for bfloat16 heads.
+#include "gc_attention_kernels.h"
+
+namespace gc {
+namespace {
+
+template <int kDim>
+void launch(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream) {
+  constexpr int kBlocks = kDim <= 192 ? 2 : 1;
+  constexpr int kWaves = kDim <= 128 ? 4 : 2;
+  if constexpr (kDim <= 128) {
+    if (kind == kAttnRows8) {
+      hipLaunchKernelGGL((k_attention_rows<uint16_t, kDim, 1, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);
+      return;
+    }
+  }
+  if (kind == kAttnKeys) hipLaunchKernelGGL((k_attention_keys<uint16_t, kDim, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, stream, p);
+  else hipLaunchKernelGGL((k_attention_rows<uint16_t, kDim, 1, kBlocks, 4, kDim <= 128 ? 2 : 1>), dim3(blocks), dim3(256), 0, stream, p);
+}
+
+}  // namespace
+
+bool launch_attention_bf16(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream) {
+  switch (attention_padded_dim(p.dim)) {
+    case 32: launch<32>(p, kind, blocks, stream); return true;
+    case 64: launch<64>(p, kind, blocks, stream); return true;
+    case 96: launch<96>(p, kind, blocks, stream); return true;
+    case 128: launch<128>(p, kind, blocks, stream); return true;
+    case 192: launch<192>(p, kind, blocks, stream); return true;
+    case 256: launch<256>(p, kind, blocks, stream); return true;
+  }
+  return false;
+}
+
+}  // namespace gc

@@ -24,7 +24,22 @@ struct AttentionItem {
 };
 static_assert(sizeof(AttentionItem) == GC_ATTENTION_ITEM_WORDS * 4, "item words");
 
-// kernel variants (gc_attention_info.kind)
-constexpr int kAttnRows = 0;
+// Kernel variants (gc_attention_info.kind) and their rows an item.
+enum AttentionKind { kAttnRows8 = 0, kAttnRows4 = 1, kAttnKeys = 2, kAttnKinds = 3 };
+inline int attention_tile_rows(int kind) { return kind == kAttnRows8 ? 256 : kind == kAttnRows4 ? 128 : 32; }
+
+// Head dims are padded to the next of these in LDS and registers.
+inline int attention_padded_dim(int dim) {
+  return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;
+}
+
+// Whether eight waves' rows fit the registers at two waves a SIMD; wider
+// heads take four waves with a SIMD's registers each.
+inline bool attention_has_rows8(int dim, int dtype) { return attention_padded_dim(dim) <= (dtype == GC_F32 ? 96 : 128); }
+
+struct AttentionArgs;
+// Launches of one storage type (false: no such variant).
+bool launch_attention_bf16(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream);
+bool launch_attention_f32(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream);
 
 }  // namespace gc
