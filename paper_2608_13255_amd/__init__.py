@@ -990,68 +990,90 @@ lib()
 # operators of the denoiser's own blocks
 # ---------------------------------------------------------------------------
 
+_Tensor = torch.Tensor
+_CONTIGUOUS = torch.contiguous_format
+# GC_F32 / GC_BF16 by torch type
+_HEAD_CODES = {torch.float32: GC_F32, torch.bfloat16: GC_BF16}
+# (host array, columns, axes) of the position axes' columns, by their values
+_SECTIONS: Dict[Tuple[int, ...], tuple] = {}
+
+
 def _heads(t: torch.Tensor, name: str) -> _Heads:
     """gc_heads of a device tensor [tokens, heads, dim] whose channels are
     contiguous.  The stride of an axis of one element or none is of no
     consequence, and torch may hold any there."""
-    if not isinstance(t, torch.Tensor):
+    if type(t) is not _Tensor and not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor (got {t.device})")
-    if t.dim() != 3:
+    strides = t.stride()
+    if len(strides) != 3:
         raise ValueError(f"{name} must be [tokens, heads, dim] (got {tuple(t.shape)})")
+    st, sh, sc = strides
     n, h, d = t.shape
-    st, sh, sc = t.stride()
     if sc != 1 and d > 1:
         raise ValueError(f"{name} must have contiguous channels")
-    if h <= 1:
-        sh = d
-    if n <= 1:
-        st = h * d
-    return _Heads(t.data_ptr(), st, sh)
+    return _Heads(t.data_ptr(), st if n > 1 else h * d, sh if h > 1 else d)
+
+
+def _head_code(t: torch.Tensor) -> int:
+    code = _HEAD_CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"heads must be float32 or bfloat16 (got {t.dtype})")
+    return code
 
 
 def _like_heads(t: torch.Tensor, name: str, shape, like: torch.Tensor) -> torch.Tensor:
-    if tuple(t.shape) != tuple(shape) or t.dtype != like.dtype or t.device != like.device:
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device:
         raise ValueError(f"{name} must be {like.dtype} {list(shape)} on {like.device} (got {t.dtype} {list(t.shape)} "
                          f"on {t.device})")
     return t
 
 
+def _sections(sections: Sequence[int]) -> tuple:
+    key = tuple(map(int, sections))
+    got = _SECTIONS.get(key)
+    if got is None:
+        if not 1 <= len(key) <= GC_MAX_AXES:
+            raise ValueError(f"sections must name 1 to {GC_MAX_AXES} axes")
+        if len(_SECTIONS) >= 256:
+            _SECTIONS.clear()
+        got = _SECTIONS[key] = (_I32[len(key)](*key), sum(key), len(key))
+    return got
+
+
 def _rope_args(positions: torch.Tensor, table: torch.Tensor, sections: Optional[Sequence[int]], x: torch.Tensor):
     """(positions, table, n_pos, sections, n_axes) as the C calls take them."""
-    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2:
+    rows, cols, two = table.shape if table.dim() == 3 else (0, 0, 0)
+    if two != 2 or table.dtype != torch.float32:
         raise ValueError("table must be float32 [n_pos, columns, 2]")
-    sec = [int(table.shape[1])] if sections is None else [int(n) for n in sections]
-    if sum(sec) != table.shape[1]:
-        raise ValueError(f"sections {sec} do not sum to the table's {table.shape[1]} columns")
-    if not 1 <= len(sec) <= GC_MAX_AXES:
-        raise ValueError(f"sections must name 1 to {GC_MAX_AXES} axes")
-    T = x.shape[0]
-    if positions.dtype != torch.int32 or tuple(positions.shape) not in ((T, len(sec)),) + (((T,),) if len(sec) == 1 else ()):
-        raise ValueError(f"positions must be int32 [{T}, {len(sec)}]")
+    sec, columns, axes = _sections((cols,) if sections is None else sections)
+    if columns != cols:
+        raise ValueError(f"sections {list(sec)} do not sum to the table's {cols} columns")
+    T, shape = x.shape[0], positions.shape
+    if positions.dtype != torch.int32 or not (shape == (T, axes) or (axes == 1 and shape == (T,))):
+        raise ValueError(f"positions must be int32 [{T}, {axes}]")
+    device = x.get_device()
     for t, name in ((positions, "positions"), (table, "table")):
-        if t.device != x.device:
+        if t.get_device() != device:
             raise ValueError(f"{name} must be on {x.device} (got {t.device})")
-    return _dev(positions, "positions"), _dev(table, "table"), int(table.shape[0]), _I32[len(sec)](*sec), len(sec)
+    return _dev(positions, "positions"), _dev(table, "table"), rows, sec, axes
 
 
 def gc_rope_table(n_pos: int, sections: Sequence[int], base: float = 10000.0, scaling: Optional[RopeScaling] = None,
                   table: torch.Tensor = None, device="cuda", stream=None) -> torch.Tensor:
     """float32 [n_pos, sum(sections), 2]: cos and sin of each position times
     each column's frequency.  sections: columns of each position axis."""
-    sec = [int(n) for n in sections]
-    if not 1 <= len(sec) <= GC_MAX_AXES:
-        raise ValueError(f"sections must name 1 to {GC_MAX_AXES} axes")
+    sec, columns, axes = _sections(sections)
     if n_pos < 1:
         raise ValueError("n_pos must be at least 1")
     fresh = []
     if table is None:
-        table = torch.empty((n_pos, max(0, sum(sec)), 2), dtype=torch.float32, device=device)
+        table = torch.empty((n_pos, max(0, columns), 2), dtype=torch.float32, device=device)
         fresh.append(table)
-    if table.dtype != torch.float32 or tuple(table.shape) != (n_pos, sum(sec), 2):
-        raise ValueError(f"table must be float32 [{n_pos}, {sum(sec)}, 2]")
-    _check(lib().gc_rope_table(_dev(table, "table"), n_pos, _I32[len(sec)](*sec), len(sec), float(base),
+    if table.dtype != torch.float32 or table.shape != (n_pos, columns, 2):
+        raise ValueError(f"table must be float32 [{n_pos}, {columns}, 2]")
+    _check(lib().gc_rope_table(_dev(table, "table"), n_pos, sec, axes, float(base),
                                ctypes.byref(scaling) if scaling is not None else None, _stream(stream)),
            "gc_rope_table")
     _keep(stream, fresh)
@@ -1065,15 +1087,17 @@ def gc_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, secti
     or [tokens, axes]; table from gc_rope_table; sections: its columns of each
     axis (default: one axis).  out may be x."""
     hx = _heads(x, "x")
-    dt = dtype_code(x)
+    dt = _head_code(x)
     args = _rope_args(positions, table, sections, x)
-    fresh = []
-    if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        fresh.append(out)
-    ho = _heads(_like_heads(out, "out", x.shape, x), "out")
     T, H, D = x.shape
-    _check(lib().gc_rope(ctypes.byref(hx), T, H, D, dt, *args, layout, ctypes.byref(ho), _stream(stream)), "gc_rope")
+    if out is None:
+        out = torch.empty_like(x, memory_format=_CONTIGUOUS)
+        ho = _Heads(out.data_ptr(), H * D, D)
+        fresh = (out,)
+    else:
+        ho = _heads(_like_heads(out, "out", x.shape, x), "out")
+        fresh = ()
+    _check(lib().gc_rope(hx, T, H, D, dt, *args, layout, ho, _stream(stream)), "gc_rope")
     _keep(stream, fresh)
     return out
 
@@ -1086,24 +1110,30 @@ def gc_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain: torch.Tensor, k_ga
     kv_heads, dim] with gains float32 [dim], and gc_rope, in one pass.  q_out
     and k_out may be q and k."""
     hq, hk = _heads(q, "q"), _heads(k, "k")
-    dt = dtype_code(q)
+    dt = _head_code(q)
     T, H, D = q.shape
-    _like_heads(k, "k", (T, k.shape[1], D), q)
+    Hk = k.shape[1]
+    _like_heads(k, "k", (T, Hk, D), q)
+    device = q.get_device()
     for g, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
-        if g.dtype != torch.float32 or tuple(g.shape) != (D,) or g.device != q.device:
+        if g.dtype != torch.float32 or g.shape != (D,) or g.get_device() != device:
             raise ValueError(f"{name} must be float32 [{D}] on {q.device}")
     args = _rope_args(positions, table, sections, q)
     fresh = []
     if q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        q_out = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        ho = _Heads(q_out.data_ptr(), H * D, D)
         fresh.append(q_out)
+    else:
+        ho = _heads(_like_heads(q_out, "q_out", q.shape, q), "q_out")
     if k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        k_out = torch.empty_like(k, memory_format=_CONTIGUOUS)
+        hp = _Heads(k_out.data_ptr(), Hk * D, D)
         fresh.append(k_out)
-    ho, hp = _heads(_like_heads(q_out, "q_out", q.shape, q), "q_out"), _heads(_like_heads(k_out, "k_out", k.shape, q), "k_out")
-    _check(lib().gc_qk_norm_rope(ctypes.byref(hq), H, ctypes.byref(hk), k.shape[1], T, D, dt, _dev(q_gain, "q_gain"),
-                                 _dev(k_gain, "k_gain"), float(eps), *args, layout, ctypes.byref(ho), ctypes.byref(hp),
-                                 _stream(stream)), "gc_qk_norm_rope")
+    else:
+        hp = _heads(_like_heads(k_out, "k_out", k.shape, q), "k_out")
+    _check(lib().gc_qk_norm_rope(hq, H, hk, Hk, T, D, dt, _dev(q_gain, "q_gain"), _dev(k_gain, "k_gain"), eps, *args,
+                                 layout, ho, hp, _stream(stream)), "gc_qk_norm_rope")
     _keep(stream, fresh)
     return q_out, k_out
 
@@ -1118,6 +1148,10 @@ class AttentionPlan:
     items: torch.Tensor
     workspace: Optional[torch.Tensor]
 
+    def __post_init__(self):
+        i = self.info
+        self.sizes = (i.heads, i.kv_heads, i.dim, i.total_q, i.total_k)
+
 
 def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, kv_heads: int, dim: int,
                       dtype: torch.dtype, causal: bool = False, device="cuda", stream=None) -> AttentionPlan:
@@ -1127,9 +1161,9 @@ def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, 
     stream)."""
     if len(q_lens) != len(k_lens):
         raise ValueError("q_lens and k_lens must have the same length")
-    if dtype not in (torch.float32, torch.bfloat16):
+    code = _HEAD_CODES.get(dtype)
+    if code is None:
         raise ValueError(f"heads must be float32 or bfloat16 (got {dtype})")
-    code = GC_F32 if dtype == torch.float32 else GC_BF16
     n = len(q_lens)
     ql = np.ascontiguousarray(q_lens, dtype=np.int64).reshape(n)
     kl = np.ascontiguousarray(k_lens, dtype=np.int64).reshape(n)
@@ -1156,30 +1190,31 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
     """Attention of q [sum of q_lens, heads, dim] over k, v [sum of k_lens,
     kv_heads, dim] with the plan of their lengths; scale defaults to
     1 / sqrt(dim).  Returns (out like q, lse float32 [heads, sum of q_lens])."""
-    info = plan.info
-    H, Hk, D, T, S = info.heads, info.kv_heads, info.dim, info.total_q, info.total_k
-    if dtype_code(q) != info.dtype or tuple(q.shape) != (T, H, D):
+    info, ws = plan.info, plan.workspace
+    H, Hk, D, T, S = plan.sizes
+    if q.shape != (T, H, D) or _head_code(q) != info.dtype:
         raise ValueError(f"q must be [{T}, {H}, {D}] of the plan's type (got {q.dtype} {list(q.shape)})")
     _like_heads(k, "k", (S, Hk, D), q)
     _like_heads(v, "v", (S, Hk, D), q)
-    if plan.items.device != q.device:
+    device = q.get_device()
+    if plan.items.get_device() != device:
         raise ValueError(f"the plan is on {plan.items.device}, q on {q.device}")
     hq, hk, hv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     fresh = []
     if out is None:
-        out = torch.empty((T, H, D), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        ho = _Heads(out.data_ptr(), H * D, D)
         fresh.append(out)
+    else:
+        ho = _heads(_like_heads(out, "out", q.shape, q), "out")
     if lse is None:
         lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
         fresh.append(lse)
-    ho = _heads(_like_heads(out, "out", (T, H, D), q), "out")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (H, T) or lse.device != q.device:
+    elif lse.dtype != torch.float32 or lse.shape != (H, T) or lse.get_device() != device:
         raise ValueError(f"lse must be float32 [{H}, {T}] on {q.device}")
-    ws = plan.workspace
-    _check(lib().gc_attention(ctypes.byref(hq), ctypes.byref(hk), ctypes.byref(hv), ctypes.byref(ho), _dev(lse, "lse"),
-                              ctypes.byref(info), _dev(plan.items, "items"),
-                              1.0 / math.sqrt(D) if scale is None else float(scale),
-                              None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), _stream(stream)),
-           "gc_attention")
-    _keep(stream, fresh + [plan.items] + ([] if ws is None else [ws]))
+    _check(lib().gc_attention(hq, hk, hv, ho, _dev(lse, "lse"), info, plan.items.data_ptr(),
+                              1.0 / math.sqrt(D) if scale is None else scale, None if ws is None else ws.data_ptr(),
+                              0 if ws is None else ws.numel(), _stream(stream)), "gc_attention")
+    if stream is not None:
+        _keep(stream, fresh + [plan.items] + ([] if ws is None else [ws]))
     return out, lse

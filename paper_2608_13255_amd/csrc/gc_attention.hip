@@ -43,21 +43,40 @@ void each_tile(const Batch& b, int tile, F f) {
   }
 }
 
+// Items of a variant with parts of at most `part` keys.
+int64_t items_of(const Batch& b, int tile, int part) {
+  int64_t n = 0;
+  each_tile(b, tile, [&](int s, int r, int, int, int) { n += parts_of(keys_seen(b, s, r, tile), part); });
+  return n;
+}
+
 // The variant and the keys a part holds at most (what is longer is split).
 void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
-  int64_t most_rows = 0, work[kAttnKinds] = {}, tiles[kAttnKinds] = {};
-  for (int s = 0; s < b.n_seq; ++s) most_rows = std::max(most_rows, (int64_t)b.q_lens[s] * b.group);
-  for (int k = 0; k < kAttnKinds; ++k) {
-    const int tile = attention_tile_rows(k);
-    each_tile(b, tile, [&](int s, int r, int, int, int) { work[k] += keys_seen(b, s, r, tile), ++tiles[k]; });
+  int64_t most_rows = 0, tiles8 = 0;
+  for (int s = 0; s < b.n_seq; ++s) {
+    const int64_t rows = (int64_t)b.q_lens[s] * b.group;
+    most_rows = std::max(most_rows, rows);
+    tiles8 += (rows + 255) / 256;
   }
   if (most_rows <= 32) *kind = kAttnKeys;
-  else *kind = attention_has_rows8(dim, dtype) && tiles[kAttnRows8] * b.kv_heads >= kCus ? kAttnRows8 : kAttnRows4;
-  const int64_t blocks = *kind == kAttnRows8 ? kCus : 2 * kCus;
-  int64_t keys = work[*kind] * b.kv_heads / blocks + 1;
-  keys = std::max<int64_t>(keys, *kind == kAttnKeys ? 256 : 512);
-  keys = (keys + kPartKeys - 1) / kPartKeys * kPartKeys;
-  *part = (int)std::min<int64_t>(keys, 0x7fffffc0);
+  else *kind = attention_has_rows8(dim, dtype) && tiles8 * b.kv_heads >= kCus ? kAttnRows8 : kAttnRows4;
+  // the blocks that the card holds at once
+  const int64_t blocks = *kind == kAttnKeys ? kCus * attention_keys_blocks(dim, dtype) : *kind == kAttnRows8 ? kCus : 2 * kCus;
+  const int tile = attention_tile_rows(*kind);
+  int64_t work = 0, most = 0;
+  each_tile(b, tile, [&](int s, int r, int, int, int) {
+    const int64_t n = keys_seen(b, s, r, tile);
+    work += n, most = std::max(most, n);
+  });
+  // the shortest parts with which all blocks are there at once, so that they end together
+  int64_t low = std::max<int64_t>(work * b.kv_heads / blocks + 1, *kind == kAttnKeys ? 256 : 512), high = std::max(low, most);
+  while (low < high) {
+    const int64_t mid = (low + high) / 2;
+    if (items_of(b, tile, (int)mid) * b.kv_heads <= blocks) high = mid;
+    else low = mid + 1;
+  }
+  low = (low + kPartKeys - 1) / kPartKeys * kPartKeys;
+  *part = (int)std::min<int64_t>(low, 0x7fffffc0);
 }
 
 int64_t counter_bytes(int64_t n_groups, int kv_heads) { return (n_groups * kv_heads * 4 + 255) / 256 * 256; }

@@ -7,7 +7,7 @@ namespace {
 template <int kDim>
 void launch(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream) {
   constexpr int kBlocks = kDim <= 192 ? 2 : 1;
-  constexpr int kWaves = kDim <= 128 ? 4 : 2;
+  constexpr int kWaves = attention_keys_waves(kDim, 2);
   if constexpr (kDim <= 128) {
     if (kind == kAttnRows8) {
       hipLaunchKernelGGL((k_attention_rows<uint16_t, kDim, 1, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);

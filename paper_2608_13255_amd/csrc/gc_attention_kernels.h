@@ -2,6 +2,8 @@
 // their own, and waves that share the rows and have keys of their own.
 #pragma once
 
+#include <type_traits>
+
 #include "gc_attention_core.h"
 
 namespace gc {
@@ -12,6 +14,13 @@ __device__ __forceinline__ void wait_loads() {
   static_assert(kLeft < 64, "the counter has 6 bits");
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt((kLeft & 15) | (7 << 4) | (15 << 8) | ((kLeft >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+
+// Until the wave's reads of LDS have arrived.
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));
   asm volatile("" ::: "memory");
 }
 
@@ -149,10 +158,6 @@ __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const 
   TileLoader<T, kDim, kKeys, kWaves> kl, vl;
   kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, wave, lane);
   vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, wave, lane);
-  if (it.k_begin < it.k_end) {
-    kl.load(lds, it.k_begin, it.k_len, wave);
-    vl.load(lds + kTile, it.k_begin, it.k_len, wave);
-  }
 
   Core<T, kDim, kNq, kKeyBlocks> core;
   core.init();
@@ -163,6 +168,10 @@ __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const 
     const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + n * 32 + (lane & 31));
     limit[n] = r.limit < it.k_end ? r.limit : it.k_end;
     core.load_q(n, (const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
+  }
+  if (it.k_begin < it.k_end) {
+    kl.load(lds, it.k_begin, it.k_len, wave);
+    vl.load(lds + kTile, it.k_begin, it.k_len, wave);
   }
   // the wave's rows see at most high keys, the block's rows at least low (limits grow with the row)
   const int high = __builtin_amdgcn_readlane(limit[kNq - 1], 31);
@@ -216,7 +225,9 @@ __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const 
 template <class T, int kDim, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionArgs p) {
   constexpr int kKeys = 32, kTile = kKeys * kDim * (int)sizeof(T);
-  constexpr int kNext = 2 * TileLoader<T, kDim, kKeys, 1>::kMine;   // loads of a tile
+  // the loads that may be outstanding where a tile is needed: the three asked for after it (the counter's
+  // range is 63: where they are more, a few of them are waited for too)
+  constexpr int kLoads = TileLoader<T, kDim, kKeys, 1>::kMine, kLeft = 3 * kLoads < 63 ? 3 * kLoads : 63;
   static_assert(32 * kDim * 4 <= 4 * kTile, "a wave's result fits its tiles");
   __shared__ __attribute__((aligned(1024))) char lds[kWaves * 4 * kTile];
   __shared__ float ml[kWaves][32][2];
@@ -225,53 +236,61 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
   char* mine = lds + wave * 4 * kTile;
 
+  // Tile i of the wave: K at mine + i % 2 * 2 kTile, V behind it.  Two tiles
+  // are on their way at any time: a K tile's successor but one is asked for as soon
+  // as its scores are in registers, a V tile's as soon as its products are issued.
   TileLoader<T, kDim, kKeys, 1> kl, vl;
   kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, 0, lane);
   vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, 0, lane);
   const int first = it.k_begin + wave * kKeys;
-  if (first < it.k_end) {
-    kl.load(mine, first, it.k_len, 0);
-    vl.load(mine + kTile, first, it.k_len, 0);
-  }
+  constexpr int kStep = kWaves * kKeys;
+  const int last_key = it.k_len - 1;
+  // past the wave's last tile the loads go on, from a tile that is there, so that the counts below hold
+  const auto load_k = [&](int key0, int stage) { kl.load(mine + stage * 2 * kTile, key0 < it.k_end ? key0 : last_key, it.k_len, 0); };
+  const auto load_v = [&](int key0, int stage) { vl.load(mine + stage * 2 * kTile + kTile, key0 < it.k_end ? key0 : last_key, it.k_len, 0); };
   Core<T, kDim, 1, 1> core;
   core.init();
   const RowOf r = row_of(p, it, kv_head, it.row0 + (lane & 31));
   const int limit[1] = {r.limit < it.k_end ? r.limit : it.k_end};
   core.load_q(0, (const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
+  if (first < it.k_end) {
+    load_k(first, 0);
+    load_v(first, 0);
+    load_k(first + kStep, 1);
+    load_v(first + kStep, 1);
+  }
   const int low = __builtin_amdgcn_readfirstlane(limit[0]);
   const int high = __builtin_amdgcn_readlane(limit[0], 31);
   const float c = p.scale * kLog2e;
 
   int stage = 0;
-  const auto next = [&](int key0) {
+  const auto tile = [&](int key0, auto masked) {
+    constexpr bool kMasked = decltype(masked)::value;
     char* kt = mine + stage * 2 * kTile;
+    f32x16 s[1][1];
+    wait_loads<kLeft>();
+    core.scores(kt, lane, s);
+    wait_lds();
+    load_k(key0 + 2 * kStep, stage);
+    softmax_tile<kMasked>(core, s, c, key0, limit, lane);
+    wait_loads<kLeft>();
+    const uint32_t left_out = core.template add_values<kMasked>(kt + kTile, lane, s);
+    wait_lds();
+    load_v(key0 + 2 * kStep, stage);
     stage ^= 1;
-    if (key0 + kWaves * kKeys < it.k_end) {
-      kl.load(mine + stage * 2 * kTile, key0 + kWaves * kKeys, it.k_len, 0);
-      vl.load(mine + stage * 2 * kTile + kTile, key0 + kWaves * kKeys, it.k_len, 0);
-      wait_loads<(kNext < 63 ? kNext : 63)>();   // the counter's range is 63: one load more is waited for
-    } else {
-      wait_loads<0>();
-    }
-    return kt;
+    return left_out;
   };
   int key0 = first;
-  for (; key0 + kKeys <= low; key0 += kWaves * kKeys) {
-    const char* kt = next(key0);
-    tile_step<false, 1>(core, kt, kt + kTile, c, key0, limit, lane);
-  }
+  for (; key0 + kKeys <= low; key0 += kStep) tile(key0, std::false_type{});
   const int first_masked = key0;
   uint32_t bad = 0;
-  for (; key0 < it.k_end; key0 += kWaves * kKeys) {
-    const char* kt = next(key0);
-    if (key0 < high) bad |= tile_step<true, 1>(core, kt, kt + kTile, c, key0, limit, lane);
-  }
+  for (; key0 < high; key0 += kStep) bad |= tile(key0, std::true_type{});
   if (__any(bad != 0))
     add_nonfinite<T>(core, vl.base, vl.stride, p.dim, first_masked, high, kKeys, kWaves * kKeys, limit, lane);
   // the waves' results, added by the first wave in their order
   float l[1] = {sum_halves(core.l[0])};
+  wait_loads<0>();   // (also before the block's LDS is given up)
   if constexpr (kWaves > 1) {
-    wait_loads<0>();
     float* o = reinterpret_cast<float*>(mine);
 #pragma unroll
     for (int d = 0; d < kDim / 32; ++d)

@@ -37,6 +37,17 @@ inline int attention_padded_dim(int dim) {
 // heads take four waves with a SIMD's registers each.
 inline bool attention_has_rows8(int dim, int dtype) { return attention_padded_dim(dim) <= (dtype == GC_F32 ? 96 : 128); }
 
+// The waves of a block of kAttnKeys: two tiles of 32 keys and values each, in
+// at most 128 KiB; and the blocks of a compute unit (160 KiB of LDS).
+constexpr int attention_keys_waves(int padded, int bytes) {
+  return padded * bytes <= 256 ? 4 : padded * bytes <= 512 ? 2 : 1;
+}
+inline int attention_keys_blocks(int dim, int dtype) {
+  const int row = attention_padded_dim(dim) * dtype_bytes(dtype);
+  const int lds = attention_keys_waves(row, 1) * (4 * 32 * row + 256) + 64;
+  return 163840 / lds < 4 ? 163840 / lds : 4;
+}
+
 struct AttentionArgs;
 // Launches of one storage type (false: no such variant).
 bool launch_attention_bf16(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream);
