@@ -27,7 +27,7 @@ __device__ __forceinline__ void wait_lds() {
 // Four channels of a finished row.
 __device__ __forceinline__ void store4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 __device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
-  *reinterpret_cast<u32x2*>(p) = u32x2{f2_to_bf16x2_bits(x[0], x[1]), f2_to_bf16x2_bits(x[2], x[3])};
+  *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
 }
 
 // One row's result from its weighted sum (by four channels), maximum and sum.

@@ -59,36 +59,62 @@ inline int check_heads_out(const gc_heads& o, int64_t t, int h, int dim, const c
 // device
 // ---------------------------------------------------------------------------
 
-// V channels as floats, one memory access of V * sizeof(T) bytes (at most 16).
-template <int V>
-__device__ __forceinline__ void load_heads(const float* p, float (&x)[V]) {
-  typedef float fv __attribute__((ext_vector_type(V)));
-  const fv v = *reinterpret_cast<const fv*>(p);
-#pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = v[i];
+// V channels as floats, one memory access of V * sizeof(T) bytes (at most
+// 16); kOnce: data that is not used again soon, past the caches.
+template <bool kOnce, class X>
+__device__ __forceinline__ X load_vec(const void* p) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(reinterpret_cast<const X*>(p));
+  else return *reinterpret_cast<const X*>(p);
 }
-template <int V>
-__device__ __forceinline__ void load_heads(const uint16_t* p, float (&x)[V]) {
-  typedef uint32_t uv __attribute__((ext_vector_type(V / 2)));
-  const uv v = *reinterpret_cast<const uv*>(p);
-#pragma unroll
-  for (int i = 0; i < V; ++i) x[i] = (i & 1) ? __uint_as_float(v[i / 2] & 0xffff0000u) : __uint_as_float(v[i / 2] << 16);
+template <bool kOnce, class X>
+__device__ __forceinline__ void store_vec(void* p, X x) {
+  if constexpr (kOnce) __builtin_nontemporal_store(x, reinterpret_cast<X*>(p));
+  else *reinterpret_cast<X*>(p) = x;
 }
+// V channels as they lie in memory, and as floats.
+template <class T, int V>
+struct HeadVec;
 template <int V>
+struct HeadVec<float, V> {
+  typedef float type __attribute__((ext_vector_type(V)));
+  __device__ __forceinline__ static float at(const type& v, int i) { return v[i]; }
+};
+template <int V>
+struct HeadVec<uint16_t, V> {
+  typedef uint32_t type __attribute__((ext_vector_type(V / 2)));
+  __device__ __forceinline__ static float at(const type& v, int i) {
+    return __uint_as_float((i & 1) ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
+  }
+};
+template <int V, class T>
+__device__ __forceinline__ void load_heads(const T* p, float (&x)[V]) {
+  const auto v = *reinterpret_cast<const typename HeadVec<T, V>::type*>(p);
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = HeadVec<T, V>::at(v, i);
+}
+template <int V, bool kOnce = false>
 __device__ __forceinline__ void store_heads(float* p, const float (&x)[V]) {
   typedef float fv __attribute__((ext_vector_type(V)));
   fv v;
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = x[i];
-  *reinterpret_cast<fv*>(p) = v;
+  store_vec<kOnce, fv>(p, v);
 }
-template <int V>
+// Two floats to a pair of bfloat16, round to nearest even (a NaN stays one).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 v;
+  v.x = (__bf16)lo;
+  v.y = (__bf16)hi;
+  return __builtin_bit_cast(uint32_t, v);
+}
+template <int V, bool kOnce = false>
 __device__ __forceinline__ void store_heads(uint16_t* p, const float (&x)[V]) {
   typedef uint32_t uv __attribute__((ext_vector_type(V / 2)));
   uv v;
 #pragma unroll
-  for (int i = 0; i < V; i += 2) v[i / 2] = f2_to_bf16x2_bits(x[i], x[i + 1]);
-  *reinterpret_cast<uv*>(p) = v;
+  for (int i = 0; i < V; i += 2) v[i / 2] = pack_bf16(x[i], x[i + 1]);
+  store_vec<kOnce, uv>(p, v);
 }
 
 }  // namespace gc

@@ -3,19 +3,26 @@
 //
 // A column j of the rotation turns two channels (a, b) of a head to
 // (a c - b s, b c + a s) with (c, s) = table[position][j].  One lane holds
-// both channels of its columns (V columns: two accesses of V channels), so
-// nothing is exchanged for the turn; the norm's sum of squares is one
-// butterfly over the lanes of a head.
+// both channels of its columns (two runs of V channels), so nothing is
+// exchanged for the turn; the norm's sum of squares is one butterfly over the
+// lanes of a head.
 //
 // Memory-bound: each value is read and written once, about 3 operations a
-// value (7 with the norm) against 4 or 8 bytes.
+// value (7 with the norm) against 4 or 8 bytes.  What counted: all of a
+// wave's loads issued before anything waits, the sixteen bytes of
+// neighbouring lanes side by side, and arguments chosen between queries
+// and keys in scalar registers.  196608 tokens x 32 heads x 128 bfloat16 with the
+// norms: 535 us (6.0 TB/s of a copy's 6.5); 196608 x 16 x 128, 64 channels turned: 289 us
+// (5.8 TB/s); 13823 x 16 x 64 float: 20.7 us (5.5 TB/s).
+#include <type_traits>
+
 #include "gc_heads.h"
 
 namespace gc {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kUnroll = 4;   // heads a lane has in flight
+constexpr int64_t kOnceBytes = 64 << 20;   // read and written
 
 struct Sections {
   int n;                     // axes
@@ -35,26 +42,89 @@ struct RopeArgs {
   int dim, half;             // half = R / 2 columns
   int lanes_log2;            // lanes of a head
   int slots_log2;            // heads of a token in a wave at a time
+  uint32_t head_groups;      // waves of a token
   float eps, inv_dim;
 };
 
-// One wave: 2^(6 - lanes_log2) heads at a time, of one token or, where a
+template <int kControl>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kControl, 0xf, 0xf, true));
+}
+
+// The sum over the 2^lanes_log2 lanes of a head, in every one of them.
+// (Mirroring half a row, or a row, pairs lanes whose sums so far are of different parts.)
+__device__ __forceinline__ float sum_lanes(float x, int lanes_log2) {
+  if (lanes_log2 > 0) x += dpp<0xb1>(x);    // lane ^ 1
+  if (lanes_log2 > 1) x += dpp<0x4e>(x);    // lane ^ 2
+  if (lanes_log2 > 2) x += dpp<0x141>(x);   // half row mirrored
+  if (lanes_log2 > 3) x += dpp<0x140>(x);   // row mirrored
+  if (lanes_log2 > 4) x += __shfl_xor(x, 16);
+  if (lanes_log2 > 5) x += __shfl_xor(x, 32);
+  return x;
+}
+
+// 1 / sqrt(m): the hardware's estimate and one Newton step, and the divide
+// and root where the estimate's range ends (0, tiny, infinite, NaN).
+__device__ __forceinline__ float reciprocal_root(float m) {
+  if (m > 0x1p-100f && m < 0x1p100f) {
+    const float y = __builtin_amdgcn_rsqf(m);
+    return __builtin_fmaf(0.5f * y, __builtin_fmaf(-m * y, y, 1.f), y);
+  }
+  return 1.f / __builtin_sqrtf(m);
+}
+
+// Keeps an argument in a scalar register: chosen between per lane, it would
+// otherwise be loaded from the argument segment by each lane again.
+template <class X>
+__device__ __forceinline__ void in_register(X& x) {
+  asm("" : "+s"(x));
+}
+// A device address as a pointer to device memory (not to any memory).
+template <class X>
+__device__ __forceinline__ X* at_address(uint64_t x) {
+  return (X*)(__attribute__((address_space(1))) X*)x;
+}
+
+// One wave: 2^(6 - lanes_log2) heads kHeads times over, of one token or, where a
 // token has fewer heads than that, of several.
-template <class T, int V, bool kHalf, bool kNorm, bool kWhole>
+template <class T, int V, int kHeads, bool kHalf, bool kNorm, bool kWhole, bool kOnce>
 __global__ __launch_bounds__(kBlock) void k_rope(const RopeArgs p) {
   const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6);
+  const uint32_t wave = blockIdx.x * (kBlock / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & ((1 << p.lanes_log2) - 1);
   const int slot = lane >> p.lanes_log2;
   const int tokens_log2 = 6 - p.lanes_log2 - p.slots_log2;
-  const int64_t t = (wave << tokens_log2) + (slot >> p.slots_log2);
-  const int h_first = slot & ((1 << p.slots_log2) - 1);
-  if ((wave << tokens_log2) >= p.n_tokens) return;
+  const uint32_t set = wave / p.head_groups;   // of 2^tokens_log2 tokens
+  const int64_t t = ((int64_t)set << tokens_log2) + (slot >> p.slots_log2);
+  if (((int64_t)set << tokens_log2) >= p.n_tokens) return;
+  const int h_first = (int)((wave - set * p.head_groups) << p.slots_log2) * kHeads + (slot & ((1 << p.slots_log2) - 1));
   const bool live = t < p.n_tokens && i * 2 * V < p.dim;
-  // the lane's two runs of V channels
-  const bool turns = i * V < p.half;
-  const int e0 = (turns && kHalf) ? i * V : 2 * i * V;
-  const int e1 = (turns && kHalf) ? p.half + i * V : e0 + V;
+  // the lane's two runs of V channels, neighbouring lanes' side by side
+  const int pair_lanes = p.half / V;
+  const bool turns = i < pair_lanes;
+  const int e0 = turns ? i * V : 2 * p.half + (i - pair_lanes) * V;
+  const int e1 = e0 + (turns ? p.half : p.dim / 2 - p.half);
+
+  // queries first, then keys
+  const int total = p.heads[0] + p.heads[1];
+  const auto head_of = [&](int u, const void* q, const void* k, int64_t q_token, int64_t k_token, int64_t q_head, int64_t k_head) {
+    const int h = h_first + (u << p.slots_log2);
+    uint64_t q_at = (uint64_t)q, k_at = (uint64_t)k;
+    in_register(q_at), in_register(k_at), in_register(q_token), in_register(k_token), in_register(q_head), in_register(k_head);
+    const bool key = h >= p.heads[0];
+    return at_address<T>(key ? k_at : q_at) + t * (key ? k_token : q_token) + (key ? h - p.heads[0] : h) * (key ? k_head : q_head);
+  };
+  using Vec = HeadVec<T, V>;
+  typename Vec::type raw[kHeads][2];
+#pragma unroll
+  for (int u = 0; u < kHeads; ++u) {
+    raw[u][0] = raw[u][1] = 0;
+    if (live && h_first + (u << p.slots_log2) < total) {   // on its way while the table's row is looked up
+      const T* x = head_of(u, p.in[0], p.in[1], p.in_token[0], p.in_token[1], p.in_head[0], p.in_head[1]);
+      raw[u][0] = load_vec<kOnce, typename Vec::type>(x + e0);
+      raw[u][1] = load_vec<kOnce, typename Vec::type>(x + e1);
+    }
+  }
 
   float c[V], s[V];
 #pragma unroll
@@ -64,98 +134,88 @@ __global__ __launch_bounds__(kBlock) void k_rope(const RopeArgs p) {
   }
   if (live && turns) {
     const int32_t* pos = p.positions + t * p.sec.n;
-    if constexpr (kWhole) {   // the lane's columns belong to one axis
-      int ax = 0;
-      for (int a = 0; a + 1 < p.sec.n; ++a) ax += i * V >= p.sec.end[a];
-      const int64_t at = pos[ax];
-      if (at >= 0 && at < p.n_pos) {
-        const float* row = p.table + (at * p.half + i * V) * 2;
+    // half pairs: columns i V ..; interleaved ones: those of both runs, V / 2 each
+    constexpr int kRun = kHalf ? V : V / 2;
 #pragma unroll
-        for (int j = 0; j < V; j += 2) {
-          float w[4];
-          load_heads<4>(row + 2 * j, w);
-          c[j] = w[0], s[j] = w[1], c[j + 1] = w[2], s[j + 1] = w[3];
+    for (int run = 0; run < V / kRun; ++run) {
+      const int col = i * kRun + run * (p.half / 2);
+      if constexpr (kWhole) {   // a run's columns belong to one axis
+        int ax = 0;
+        for (int k = 0; k + 1 < p.sec.n; ++k) ax += col >= p.sec.end[k];
+        const int64_t at = pos[ax];
+        if (at >= 0 && at < p.n_pos) {
+          float w[2 * kRun];
+          load_heads<2 * kRun>(p.table + (at * p.half + col) * 2, w);
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) c[run * kRun + j] = w[2 * j], s[run * kRun + j] = w[2 * j + 1];
+        } else {
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) c[run * kRun + j] = s[run * kRun + j] = __builtin_nanf("");
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) c[j] = s[j] = __builtin_nanf("");
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        int ax = 0;
-        for (int a = 0; a + 1 < p.sec.n; ++a) ax += i * V + j >= p.sec.end[a];
-        const int64_t at = pos[ax];
-        if (at >= 0 && at < p.n_pos) {
-          float w[2];
-          load_heads<2>(p.table + (at * p.half + i * V + j) * 2, w);
-          c[j] = w[0], s[j] = w[1];
-        } else {
-          c[j] = s[j] = __builtin_nanf("");
+        for (int j = 0; j < kRun; ++j) {
+          int ax = 0;
+          for (int k = 0; k + 1 < p.sec.n; ++k) ax += col + j >= p.sec.end[k];
+          const int64_t at = pos[ax];
+          if (at >= 0 && at < p.n_pos) {
+            float w[2];
+            load_heads<2>(p.table + (at * p.half + col + j) * 2, w);
+            c[run * kRun + j] = w[0], s[run * kRun + j] = w[1];
+          } else {
+            c[run * kRun + j] = s[run * kRun + j] = __builtin_nanf("");
+          }
         }
       }
     }
   }
 
-  const int total = p.heads[0] + p.heads[1];
-  for (int h0 = h_first; h0 < total; h0 += kUnroll << p.slots_log2) {
-    float a[kUnroll][V], b[kUnroll][V];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = h0 + (u << p.slots_log2);
+  for (int u = 0; u < kHeads; ++u) {
+    float a[V], b[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) a[u][j] = b[u][j] = 0.f;
-      if (live && h < total) {
-        const int w = h >= p.heads[0];
-        const T* x = (const T*)p.in[w] + t * p.in_token[w] + (int64_t)(h - (w ? p.heads[0] : 0)) * p.in_head[w];
-        load_heads<V>(x + e0, a[u]);
-        load_heads<V>(x + e1, b[u]);
+    for (int j = 0; j < V; ++j) a[j] = Vec::at(raw[u][0], j), b[j] = Vec::at(raw[u][1], j);
+    if constexpr (kNorm) {
+      float q = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) q = __builtin_fmaf(a[j], a[j], __builtin_fmaf(b[j], b[j], q));
+      const float r = reciprocal_root(__builtin_fmaf(sum_lanes(q, p.lanes_log2), p.inv_dim, p.eps));
+      if (live) {
+        uint64_t q_gain = (uint64_t)p.gain[0], k_gain = (uint64_t)p.gain[1];
+        in_register(q_gain), in_register(k_gain);
+        const float* gain = at_address<float>(h_first + (u << p.slots_log2) >= p.heads[0] ? k_gain : q_gain);
+        float g[V];
+        load_heads<V>(gain + e0, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) a[j] = a[j] * r * g[j];
+        load_heads<V>(gain + e1, g);
+#pragma unroll
+        for (int j = 0; j < V; ++j) b[j] = b[j] * r * g[j];
       }
     }
+    if (turns) {
+      if constexpr (kHalf) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = h0 + (u << p.slots_log2);
-      const int w = h >= p.heads[0];
-      if constexpr (kNorm) {
-        float q = 0.f;
+        for (int j = 0; j < V; ++j) {
+          const float x = a[j], y = b[j];
+          a[j] = __builtin_fmaf(x, c[j], -(y * s[j]));
+          b[j] = __builtin_fmaf(y, c[j], x * s[j]);
+        }
+      } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) q = __builtin_fmaf(a[u][j], a[u][j], __builtin_fmaf(b[u][j], b[u][j], q));
-        for (int d = 1; d < (1 << p.lanes_log2); d <<= 1) q += __shfl_xor(q, d);
-        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(q, p.inv_dim, p.eps));
-        if (live) {
-          float g[V];
-          load_heads<V>(p.gain[w] + e0, g);
-#pragma unroll
-          for (int j = 0; j < V; ++j) a[u][j] = a[u][j] * r * g[j];
-          load_heads<V>(p.gain[w] + e1, g);
-#pragma unroll
-          for (int j = 0; j < V; ++j) b[u][j] = b[u][j] * r * g[j];
+        for (int j = 0; j < V; ++j) {
+          float& x = 2 * j < V ? a[2 * j] : b[2 * j - V];
+          float& y = 2 * j < V ? a[2 * j + 1] : b[2 * j + 1 - V];
+          const float x0 = x, y0 = y;
+          x = __builtin_fmaf(x0, c[j], -(y0 * s[j]));
+          y = __builtin_fmaf(y0, c[j], x0 * s[j]);
         }
       }
-      if (live && h < total) {
-        if (turns) {
-          if constexpr (kHalf) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              const float x = a[u][j], y = b[u][j];
-              a[u][j] = x * c[j] - y * s[j];
-              b[u][j] = y * c[j] + x * s[j];
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              float& x = 2 * j < V ? a[u][2 * j] : b[u][2 * j - V];
-              float& y = 2 * j < V ? a[u][2 * j + 1] : b[u][2 * j + 1 - V];
-              const float u0 = x, u1 = y;
-              x = u0 * c[j] - u1 * s[j];
-              y = u1 * c[j] + u0 * s[j];
-            }
-          }
-        }
-        T* y = (T*)p.out[w] + t * p.out_token[w] + (int64_t)(h - (w ? p.heads[0] : 0)) * p.out_head[w];
-        store_heads<V>(y + e0, a[u]);
-        store_heads<V>(y + e1, b[u]);
-      }
+    }
+    if (live && h_first + (u << p.slots_log2) < total) {
+      T* y = head_of(u, p.out[0], p.out[1], p.out_token[0], p.out_token[1], p.out_head[0], p.out_head[1]);
+      store_heads<V, kOnce>(y + e0, a);
+      store_heads<V, kOnce>(y + e1, b);
     }
   }
 }
@@ -239,17 +299,34 @@ void launch_v(RopeArgs& p, int layout, hipStream_t stream) {
   const int total = p.heads[0] + p.heads[1];
   p.slots_log2 = 0;
   while ((1 << p.slots_log2) < total && (lanes << p.slots_log2) < 64) ++p.slots_log2;
-  const int64_t per_block = (int64_t)(kBlock / 64) << (6 - p.lanes_log2 - p.slots_log2);
-  const dim3 grid((unsigned)((p.n_tokens + per_block - 1) / per_block));
+  const int token_sets_log2 = 6 - p.lanes_log2 - p.slots_log2;
+  const int64_t sets = (p.n_tokens + (1 << token_sets_log2) - 1) >> token_sets_log2;
+  // Four times the heads a wave where that leaves each compute unit 32 waves (196608 x 32 x 128 bfloat16: 536 us against
+  // 575, 5741 x 32 x 80 float: 25 against 27); else the shorter waves (1024 x 32 x 64: 5.9 us against 7.2).
+  const auto groups = [&](int heads) { return (int64_t)((total + (heads << p.slots_log2) - 1) / (heads << p.slots_log2)); };
+  const bool many = sets * groups(4) >= 32 * 256;
+  p.head_groups = (uint32_t)groups(many ? 4 : 1);
+  const dim3 grid((unsigned)((sets * p.head_groups + kBlock / 64 - 1) / (kBlock / 64)));
   bool whole = true;
-  for (int a = 0; a < p.sec.n; ++a) whole = whole && p.sec.end[a] % V == 0;
-  if (layout == GC_ROPE_HALF) {
-    if (whole) hipLaunchKernelGGL((k_rope<T, V, true, kNorm, true>), grid, dim3(kBlock), 0, stream, p);
-    else hipLaunchKernelGGL((k_rope<T, V, true, kNorm, false>), grid, dim3(kBlock), 0, stream, p);
-  } else {
-    if (whole) hipLaunchKernelGGL((k_rope<T, V, false, kNorm, true>), grid, dim3(kBlock), 0, stream, p);
-    else hipLaunchKernelGGL((k_rope<T, V, false, kNorm, false>), grid, dim3(kBlock), 0, stream, p);
-  }
+  const int run = layout == GC_ROPE_HALF ? V : V / 2;   // columns that a lane takes from one row
+  for (int a = 0; a < p.sec.n; ++a) whole = whole && p.sec.end[a] % run == 0;
+  if (layout != GC_ROPE_HALF) whole = whole && p.half / 2 % run == 0;
+  // Past the caches what is over twice the L2 caches' 32 MiB (13823 x 16 x 64 float: 20.8 us against 23.0), if the lanes'
+  // runs are whole lines of 128 bytes (runs of 64 bytes: 307 us past the caches, 287 through them).
+  const int rest = p.dim / 2 - p.half;
+  const bool once = 2 * p.n_tokens * total * p.dim * (int64_t)sizeof(T) >= kOnceBytes &&
+                    p.half * (int)sizeof(T) % 128 == 0 && rest * (int)sizeof(T) % 128 == 0;
+  const auto go = [&](auto half, auto all, auto past) {
+    if (many)
+      hipLaunchKernelGGL((k_rope<T, V, 4, decltype(half)::value, kNorm, decltype(all)::value, decltype(past)::value>), grid,
+                         dim3(kBlock), 0, stream, p);
+    else
+      hipLaunchKernelGGL((k_rope<T, V, 1, decltype(half)::value, kNorm, decltype(all)::value, false>), grid, dim3(kBlock), 0,
+                         stream, p);
+  };
+  const auto with = [&](auto half, auto all) { once ? go(half, all, std::true_type{}) : go(half, all, std::false_type{}); };
+  const auto axes = [&](auto half) { whole ? with(half, std::true_type{}) : with(half, std::false_type{}); };
+  layout == GC_ROPE_HALF ? axes(std::true_type{}) : axes(std::false_type{});
 }
 
 // The widest access (16 bytes at most) of which both the turned pairs and the
