@@ -2,20 +2,21 @@
 #include "gc_attention_kernels.h"
 
 namespace gc {
+
 namespace {
 
 template <int kDim>
 void launch(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream) {
-  constexpr int kBlocks = kDim <= 192 ? 2 : 1;
   constexpr int kWaves = attention_keys_waves(kDim, 2);
+  constexpr int kBlocks = kDim <= 96 ? 2 : 1, kPerSimd = kDim <= 128 ? 2 : 1;
   if constexpr (kDim <= 128) {
-    if (kind == kAttnRows8) {
-      hipLaunchKernelGGL((k_attention_rows<uint16_t, kDim, 1, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);
+    if (kind == kAttnRows256) {
+      hipLaunchKernelGGL((k_attention_rows<kDim, 1, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);
       return;
     }
   }
   if (kind == kAttnKeys) hipLaunchKernelGGL((k_attention_keys<uint16_t, kDim, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, stream, p);
-  else hipLaunchKernelGGL((k_attention_rows<uint16_t, kDim, 1, kBlocks, 4, kDim <= 128 ? 2 : 1>), dim3(blocks), dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((k_attention_rows<kDim, 1, kBlocks, 4, kPerSimd>), dim3(blocks), dim3(256), 0, stream, p);
 }
 
 }  // namespace

@@ -65,50 +65,58 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Copies kKeys rows of a K or V tensor to LDS with the swizzle, straight from
-// memory (buffer loads to LDS: 16 bytes a lane, places in lane order).
-// Rows past the sequence's last key, and channels past dim, arrive as
-// zeros: the buffer's range ends there.
-template <class T, int kDim, int kKeys, int kWaves>
+// Copies tiles of kKeys rows of a K or V tensor, one after the other, to LDS
+// with the permutation, straight from memory (buffer loads to LDS: 16 bytes a
+// lane, places in lane order).  Rows past the last key, and channels past
+// dim, arrive as zeros: the buffer's range ends there.  kStep tiles are
+// `kStep - 1` others' apart.
+template <class T, int kDim, int kKeys, int kWaves, int kStep = 1>
 struct TileLoader {
   static constexpr int kChunks = kDim * (int)sizeof(T) / 16;
   static constexpr int kLoads = kKeys * kChunks / 64;     // of a wave's 64 lanes
   static constexpr int kMine = (kLoads + kWaves - 1) / kWaves;
   static_assert(kKeys * kChunks % 64 == 0, "whole loads");
-  const char* base;       // the head's first key
-  int64_t stride;         // bytes
-  int row_bytes;
+  const char* at;         // the next tile's first row
+  int64_t advance;        // bytes to the one after
+  int left;               // keys from there to the end
+  int stride, row_bytes;
   uint32_t offset[kMine];
 
+  // keys [first, end) of a sequence that starts at first_token
   __device__ __forceinline__ void init(const void* p, int64_t first_token, int64_t token_stride, int64_t head_off, int dim,
-                                       int wave, int lane) {
-    stride = token_stride * (int64_t)sizeof(T);
-    base = (const char*)p + first_token * stride + head_off * (int64_t)sizeof(T);
+                                       int first, int end, int wave, int lane) {
+    const int64_t bytes = token_stride * (int64_t)sizeof(T);
+    at = (const char*)p + (first_token + first) * bytes + head_off * (int64_t)sizeof(T);
+    advance = bytes * (kKeys * kStep);
+    left = end - first;
+    stride = (int)bytes;
     row_bytes = dim * (int)sizeof(T);
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
-      const int at = (wave + n * kWaves) * 64 + lane;
+      const int place16 = (wave + n * kWaves) % kLoads * 64 + lane;
       // the chunk that lies at this place: the exclusive or is its own inverse
-      const int row = at / kChunks, chunk = place<kChunks>(row, at % kChunks) / 16 - row * kChunks;
+      const int row = place16 / kChunks, chunk = place<kChunks>(row, place16 % kChunks) / 16 - row * kChunks;
       offset[n] = chunk * 16 < row_bytes ? (uint32_t)row * (uint32_t)stride + (uint32_t)chunk * 16u : 0x7ffffff0u;
     }
   }
 
-  // keys [first, first + kKeys) of a sequence of k_len, first < k_len
-  __device__ __forceinline__ void load(char* lds, int first, int k_len, int wave) const {
-    const int rows = k_len - first < kKeys ? k_len - first : kKeys;
-    const int bytes = (rows - 1) * (int)stride + row_bytes;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(base + first * stride), 0, bytes, 0x00027000);
+  // The next tile.  Past the end nothing is read (and the places get zeros): the number of loads outstanding is the same.
+  __device__ __forceinline__ void load(char* lds, int wave) {
+    const int rows = left < kKeys ? left : kKeys, some = (rows - 1) * stride + row_bytes;
+    const int bytes = rows > 0 ? some : 0;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, bytes, 0x00027000);
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
-      const int i = wave + n * kWaves;
-      if (kLoads % kWaves == 0 || i < kLoads)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(lds + i * 1024), 16, offset[n], 0, 0, 0);
+      // (where the loads are no multiple of the waves, some are made twice: every wave has the same number outstanding)
+      const int i = (wave + n * kWaves) % kLoads;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)(lds + i * 1024), 16, offset[n], 0, 0, 0);
     }
+    at += advance;
+    left -= kKeys * kStep;
   }
 };
 
-// The query rows of a wave: row n * 32 + lane % 32 of its tile for n < kBlocks.
+// A query row: its token, head and the keys that it sees.
 struct RowOf {
   int64_t token;
   int head;
@@ -130,16 +138,22 @@ __device__ __forceinline__ RowOf row_of(const AttentionArgs& p, const AttentionI
 // ---------------------------------------------------------------------------
 // bfloat16
 // ---------------------------------------------------------------------------
+// What one wave holds: the queries of kNq blocks of 32 rows (an operand of
+// S^T), O^T, and the rows' maximum in use and sum.  A tile is kKeyBlocks * 32
+// keys.
 template <class T, int kDim, int kNq, int kKeyBlocks>
 struct Core;
 
-template <int kDim, int kNq, int kKeyBlocks>
-struct Core<uint16_t, kDim, kNq, kKeyBlocks> {
-  static constexpr int kChunks = kDim / 8, kSteps = kDim / 16, kOut = kDim / 32;
-  bf16x8 q[kNq][kSteps];
+// S^T: key 32 b + 8 (i / 4) + 4 half + i % 4 of row block n
+template <int kNq, int kKeyBlocks>
+struct Scores {
+  f32x16 s[kNq][kKeyBlocks];
+};
+
+template <int kNq, int kOut>
+struct Accumulators {
   f32x16 o[kNq][kOut];
   float m[kNq], l[kNq];   // maximum in use (score times scale times log2 e) and this lane's part of the sum
-
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int n = 0; n < kNq; ++n) {
@@ -151,6 +165,24 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> {
       l[n] = 0.f;
     }
   }
+};
+
+template <int kDim, int kNq, int kKeyBlocks>
+struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
+  static constexpr int kChunks = kDim / 8, kSteps = kDim / 16, kOut = kDim / 32;
+  // operands of the scores and of the output, kNq products each
+  static constexpr int kOperands = kKeyBlocks * kSteps, kAhead = kOperands < 4 ? kOperands : 4;
+  static_assert(kOperands == 2 * kKeyBlocks * kOut, "as many of either kind");
+  using Accumulators<kNq, kOut>::o;
+  using Accumulators<kNq, kOut>::l;
+  using S = Scores<kNq, kKeyBlocks>;
+  bf16x8 q[kNq][kSteps];
+
+  // Weights as an operand of O^T = V^T P^T: element j of group g is key 16 g + 8 (j / 4) + 4 half + j % 4.  Rounded to
+  // bfloat16, the type that the matrix units take; the sum l is of the unrounded ones.
+  struct Weights {
+    bf16x8 w[kNq][2 * kKeyBlocks];
+  };
 
   __device__ __forceinline__ void load_q(int n, const uint16_t* row, int dim, int half) {
 #pragma unroll
@@ -161,34 +193,39 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> {
     }
   }
 
-  // scores of the tile, S^T: key 32 b + 8 (i / 4) + 4 half + i % 4
-  __device__ __forceinline__ void scores(const char* kt, int lane, f32x16 (&s)[kNq][kKeyBlocks]) const {
-    const int r = lane & 31, half = lane >> 5;
+  // Operand i of the scores: key block i % kKeyBlocks, channels 16 (i / kKeyBlocks) + 8 half ..
+  __device__ __forceinline__ static bf16x8 keys(const char* kt, int lane, int i) {
+    const int row = i % kKeyBlocks * 32 + (lane & 31);
+    return *reinterpret_cast<const bf16x8*>(kt + place<kChunks>(row, 2 * (i / kKeyBlocks) + (lane >> 5)));
+  }
+  __device__ __forceinline__ void score(S& s, bf16x8 k, int i) const {
+#pragma unroll
+    for (int n = 0; n < kNq; ++n)
+      s.s[n][i % kKeyBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][i / kKeyBlocks], s.s[n][i % kKeyBlocks], 0, 0, 0);
+  }
+  __device__ __forceinline__ static void clear(S& s) {
 #pragma unroll
     for (int n = 0; n < kNq; ++n)
 #pragma unroll
       for (int b = 0; b < kKeyBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) s.s[n][b][i] = 0.f;
+  }
+  __device__ __forceinline__ void scores(const char* kt, int lane, S& s) const {
+    clear(s);
 #pragma unroll
-    for (int t = 0; t < kSteps; ++t)
-#pragma unroll
-      for (int b = 0; b < kKeyBlocks; ++b) {
-        const int row = b * 32 + r;
-        const bf16x8 k = *reinterpret_cast<const bf16x8*>(kt + place<kChunks>(row, 2 * t + half));
-#pragma unroll
-        for (int n = 0; n < kNq; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][t], s[n][b], 0, 0, 0);
-      }
+    for (int i = 0; i < kOperands; ++i) score(s, keys(kt, lane, i), i);
   }
 
-  // Values [4 rows][16 channels] a group of 16 lanes, transposed: this lane's
-  // channel 32 d + lane % 32 of rows first .. first + 3 and first + 8 .. first + 11 (first 4 half further).
-  __device__ __forceinline__ u32x4 values(const char* vt, int first, int d, int lane) const {
+  // Operand i of the output: group i / kOut of the weights' keys, channels 32 (i % kOut) + lane % 32.  Two reads that
+  // transpose: four rows of 16 channels a group of 16 lanes, from rows first .. first + 3 and first + 8 .. first + 11
+  // (first 4 half further).
+  __device__ __forceinline__ static u32x4 values(const char* vt, int lane, int i) {
     u32x4 w;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int row = first + 8 * j + 4 * (lane >> 5) + ((lane >> 2) & 3);
-      const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+      const int row = 16 * (i / kOut) + 8 * j + 4 * (lane >> 5) + ((lane >> 2) & 3);
+      const int chunk = 4 * (i % kOut) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
       const char* at = vt + place<kChunks>(row, chunk) + (lane & 1) * 8;
       const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
       const u32x2 y = __builtin_bit_cast(u32x2, x);
@@ -196,14 +233,10 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> {
     }
     return w;
   }
-
-  // weights of keys 16 step + ... of block b, as the operand of O^T = V^T P^T; rounded to
-  // bfloat16, the type the matrix units take (the sum l is of the unrounded ones)
-  __device__ __forceinline__ static bf16x8 weights(const f32x16& s, int step) {
-    bf16x8 w;
+  __device__ __forceinline__ void add(const Weights& w, u32x4 v, int i) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = (__bf16)s[8 * step + j];
-    return w;
+    for (int n = 0; n < kNq; ++n)
+      o[n][i % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w.w[n][i / kOut], o[n][i % kOut], 0, 0, 0);
   }
 
   // Two values with those that are not finite replaced by zeros.
@@ -213,35 +246,128 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> {
     return lo | hi;
   }
 
-  // With kMasked, values that are not finite enter as zeros (a masked row's
-  // weight 0 times NaN or infinity would be NaN); returns whether there were any.
-  template <bool kMasked>
-  __device__ __forceinline__ uint32_t add_values(const char* vt, int lane, const f32x16 (&s)[kNq][kKeyBlocks]) {
+  // A tile's values, where rows may be masked: those that are not finite enter as zeros (a masked row's weight 0 times NaN
+  // or infinity would be NaN).  Returns whether there were any (add_nonfinite).
+  __device__ __forceinline__ uint32_t add_masked(const char* vt, int lane, const Weights& w) {
     uint32_t bad = 0;
 #pragma unroll
-    for (int b = 0; b < kKeyBlocks; ++b)
+    for (int i = 0; i < kOperands; ++i) {
+      u32x4 v = values(vt, lane, i);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        bf16x8 w[kNq];
-#pragma unroll
-        for (int n = 0; n < kNq; ++n) w[n] = weights(s[n][b], t);
-#pragma unroll
-        for (int d = 0; d < kOut; ++d) {
-          u32x4 raw = values(vt, 32 * b + 16 * t, d, lane);
-          if constexpr (kMasked) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t x = finite_pair(raw[j]);
-              bad |= raw[j] ^ x;
-              raw[j] = x;
-            }
-          }
-          const bf16x8 v = __builtin_bit_cast(bf16x8, raw);
-#pragma unroll
-          for (int n = 0; n < kNq; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[n], o[n][d], 0, 0, 0);
-        }
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t x = finite_pair(v[j]);
+        bad |= v[j] ^ x;
+        v[j] = x;
       }
+      add(w, v, i);
+    }
     return bad;
+  }
+  __device__ __forceinline__ void add_values(const char* vt, int lane, const Weights& w) {
+#pragma unroll
+    for (int i = 0; i < kOperands; ++i) add(w, values(vt, lane, i), i);
+  }
+
+  // Weight e of row block n.
+  __device__ __forceinline__ void weight(const S& s, float c, float ms, Weights& w, int n, int e, float& sum) const {
+    const float x = exp2_hw(__builtin_fmaf(s.s[n][e / 16][e % 16], c, -ms));
+    sum += x;
+    w.w[n][e / 8][e % 8] = (__bf16)x;
+  }
+  __device__ __forceinline__ void weights(const S& s, float c, const float (&ms)[kNq], Weights& w) {
+#pragma unroll
+    for (int n = 0; n < kNq; ++n) {
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16 * kKeyBlocks; ++e) weight(s, c, ms[n], w, n, e, sum);
+      l[n] += sum;
+    }
+  }
+
+  // The two parts of a tile's work when nothing is masked.  Each runs matrix
+  // products beside vector work that does not need them: a wave issues a few
+  // vector instructions while a product runs.  A part asks for its operands
+  // kAhead products ahead, and for the first ones of the part after it.
+  struct Operands {
+    bf16x8 k[kAhead];
+    u32x4 v[kAhead];
+  };
+  __device__ __forceinline__ static void first_values(const char* vt, int lane, Operands& x) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) x.v[i] = values(vt, lane, i);
+  }
+
+  // the values of the tile before, and this tile's largest scores (of this lane's)
+  __device__ __forceinline__ void values_and_maximum(Operands& x, const char* vt, const Weights& w, const S& s, const char* kt,
+                                                     int lane, float (&mx)[kNq]) {
+    u32x4 v[kOperands];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) v[i] = x.v[i];
+    constexpr int kSteps2 = 8 * kKeyBlocks * kNq;   // two scores a step
+#pragma unroll
+    for (int n = 0; n < kNq; ++n) mx[n] = s.s[n][0][0];
+#pragma unroll
+    for (int i = 0; i < kOperands; ++i) {
+      if (i + kAhead < kOperands) v[i + kAhead] = values(vt, lane, i + kAhead);
+      else x.k[i + kAhead - kOperands] = keys(kt, lane, i + kAhead - kOperands);
+      add(w, v[i], i);
+#pragma unroll
+      for (int e = i * kSteps2 / kOperands; e < (i + 1) * kSteps2 / kOperands; ++e) {
+        const int n = e % kNq, y = 2 * (e / kNq);
+        mx[n] = fmaxf(fmaxf(mx[n], s.s[n][y / 16][y % 16]), s.s[n][y / 16][y % 16 + 1]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kOperands; ++i) {
+      if (i + kAhead < kOperands) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      else __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+      for (int n = 0; n < kNq; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, (8 * kKeyBlocks + kOperands - 1) / kOperands, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // this tile's weights, and the next tile's scores
+  __device__ __forceinline__ void weights_and_scores(Operands& x, const S& s, float c, const float (&ms)[kNq], Weights& w,
+                                                     const char* kt, S& next, const char* vt, int lane) {
+    bf16x8 k[kOperands];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) k[i] = x.k[i];
+    constexpr int kWeights = 16 * kKeyBlocks * kNq;
+    float sum[kNq];
+#pragma unroll
+    for (int n = 0; n < kNq; ++n) sum[n] = 0.f;
+    clear(next);
+#pragma unroll
+    for (int i = 0; i < kOperands; ++i) {
+      if (i + kAhead < kOperands) k[i + kAhead] = keys(kt, lane, i + kAhead);
+      else x.v[i + kAhead - kOperands] = values(vt, lane, i + kAhead - kOperands);
+      score(next, k[i], i);
+#pragma unroll
+      for (int e = i * kWeights / kOperands; e < (i + 1) * kWeights / kOperands; ++e)
+        weight(s, c, ms[e / (16 * kKeyBlocks)], w, e / (16 * kKeyBlocks), e % (16 * kKeyBlocks), sum[e / (16 * kKeyBlocks)]);
+    }
+#pragma unroll
+    for (int n = 0; n < kNq; ++n) {
+      l[n] += sum[n];
+      // here and not where they are used, in the next part
+#pragma unroll
+      for (int g = 0; g < 2 * kKeyBlocks; ++g) asm volatile("" : "+v"(w.w[n][g]));
+    }
+#pragma unroll
+    for (int i = 0; i < kOperands; ++i) {
+      if (i + kAhead < kOperands) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int n = 0; n < kNq; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 7 * 8 * kKeyBlocks / kOperands, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
 };
 
@@ -249,23 +375,16 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> {
 // float32
 // ---------------------------------------------------------------------------
 template <int kDim, int kNq, int kKeyBlocks>
-struct Core<float, kDim, kNq, kKeyBlocks> {
+struct Core<float, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
   static constexpr int kChunks = kDim / 4, kSteps = kDim / 8, kOut = kDim / 32;
+  using Accumulators<kNq, kOut>::o;
+  using Accumulators<kNq, kOut>::l;
+  using S = Scores<kNq, kKeyBlocks>;
   f32x4 q[kNq][kSteps];
-  f32x16 o[kNq][kOut];
-  float m[kNq], l[kNq];
 
-  __device__ __forceinline__ void init() {
-#pragma unroll
-    for (int n = 0; n < kNq; ++n) {
-#pragma unroll
-      for (int d = 0; d < kOut; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[n][d][i] = 0.f;
-      m[n] = -__builtin_inff();
-      l[n] = 0.f;
-    }
-  }
+  struct Weights {
+    f32x16 w[kNq][kKeyBlocks];   // in the scores' order, a key a product
+  };
 
   __device__ __forceinline__ void load_q(int n, const float* row, int dim, int half) {
 #pragma unroll
@@ -276,36 +395,49 @@ struct Core<float, kDim, kNq, kKeyBlocks> {
   }
 
   // A lane's chunk holds channels 8 t + 4 half + j: product j of step t takes channels 8 t + j and 8 t + 4 + j.
-  __device__ __forceinline__ void scores(const char* kt, int lane, f32x16 (&s)[kNq][kKeyBlocks]) const {
-    const int r = lane & 31, half = lane >> 5;
+  __device__ __forceinline__ void scores(const char* kt, int lane, S& s) const {
 #pragma unroll
     for (int n = 0; n < kNq; ++n)
 #pragma unroll
       for (int b = 0; b < kKeyBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) s.s[n][b][i] = 0.f;
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
       for (int b = 0; b < kKeyBlocks; ++b) {
-        const int row = b * 32 + r;
-        const f32x4 k = *reinterpret_cast<const f32x4*>(kt + place<kChunks>(row, 2 * t + half));
+        const f32x4 k = *reinterpret_cast<const f32x4*>(kt + place<kChunks>(b * 32 + (lane & 31), 2 * t + (lane >> 5)));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int n = 0; n < kNq; ++n) s[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j], q[n][t][j], s[n][b], 0, 0, 0);
+          for (int n = 0; n < kNq; ++n) s.s[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j], q[n][t][j], s.s[n][b], 0, 0, 0);
       }
   }
 
+  __device__ __forceinline__ void weights(const S& s, float c, const float (&ms)[kNq], Weights& w) {
+#pragma unroll
+    for (int n = 0; n < kNq; ++n) {
+      float sum = 0.f;
+#pragma unroll
+      for (int b = 0; b < kKeyBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          w.w[n][b][i] = exp2_hw(__builtin_fmaf(s.s[n][b][i], c, -ms[n]));
+          sum += w.w[n][b][i];
+        }
+      l[n] += sum;
+    }
+  }
+
   // channel 32 d + lane % 32 of key 32 b + 8 (i / 4) + 4 half + i % 4
-  __device__ __forceinline__ float value(const char* vt, int b, int i, int d, int lane) const {
+  __device__ __forceinline__ static float value(const char* vt, int b, int i, int d, int lane) {
     const int row = 32 * b + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
     const int chunk = 8 * d + ((lane & 31) >> 2);
     return *reinterpret_cast<const float*>(vt + place<kChunks>(row, chunk) + (lane & 3) * 4);
   }
 
   template <bool kMasked>
-  __device__ __forceinline__ uint32_t add_values(const char* vt, int lane, const f32x16 (&s)[kNq][kKeyBlocks]) {
+  __device__ __forceinline__ uint32_t add_all(const char* vt, int lane, const Weights& w) {
     uint32_t bad = 0;
 #pragma unroll
     for (int b = 0; b < kKeyBlocks; ++b)
@@ -320,28 +452,30 @@ struct Core<float, kDim, kNq, kKeyBlocks> {
             v = fin ? v : 0.f;
           }
 #pragma unroll
-          for (int n = 0; n < kNq; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[n][b][i], o[n][d], 0, 0, 0);
+          for (int n = 0; n < kNq; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.w[n][b][i], o[n][d], 0, 0, 0);
         }
     return bad;
   }
+  __device__ __forceinline__ uint32_t add_masked(const char* vt, int lane, const Weights& w) { return add_all<true>(vt, lane, w); }
+  __device__ __forceinline__ void add_values(const char* vt, int lane, const Weights& w) { add_all<false>(vt, lane, w); }
 };
 
-// The values that add_values<true> left out, for the rows that see them: a
+// The values that add_masked left out, for the rows that see them: a
 // positive weight times NaN or infinity is that value.  Keys [first, end),
-// of which kKeys of every kStride are this wave's.
+// of which `keys` of every `step` are this wave's.
 template <class T, class C, int kNq>
-__device__ __forceinline__ void add_nonfinite(C& core, const char* base, int64_t stride, int dim, int first, int end, int keys,
-                                              int step, const int (&limit)[kNq], int lane) {
+__device__ __forceinline__ void add_nonfinite(const AttentionArgs& p, const AttentionItem& it, int kv_head, C& core, int first,
+                                              int end, int keys, int step, const int (&limit)[kNq], int lane) {
   for (int key0 = first; key0 < end; key0 += step)
     for (int key = key0; key < key0 + keys && key < end; ++key) {
-      const T* row = (const T*)(base + key * stride);
+      const T* row = (const T*)p.v + ((int64_t)it.k_token0 + key) * p.v_token + kv_head * p.v_head;
 #pragma unroll
       for (int d = 0; d < C::kOut; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int c = 32 * d + 8 * g + 4 * (lane >> 5);
           float x[4] = {0.f, 0.f, 0.f, 0.f};
-          if (c < dim) load_heads<4>(row + c, x);
+          if (c < p.dim) load_heads<4>(row + c, x);
 #pragma unroll
           for (int n = 0; n < kNq; ++n)
 #pragma unroll
@@ -350,52 +484,67 @@ __device__ __forceinline__ void add_nonfinite(C& core, const char* base, int64_t
     }
 }
 
-// Weights from scores, in place, with the running maximum and sum.  The
-// maximum in use follows the true one only where that has grown by more than
-// 2^kSlack: the weights stay below 2^kSlack, sums of 2^31 of them stay finite
-// in float, and most tiles need no rescaling of the output.
-constexpr float kSlack = 8.f;
+// Masked places' scores.
+template <int kNq, int kKeyBlocks>
+__device__ __forceinline__ void mask(Scores<kNq, kKeyBlocks>& s, int key0, const int (&limit)[kNq], int lane) {
+#pragma unroll
+  for (int n = 0; n < kNq; ++n)
+#pragma unroll
+    for (int b = 0; b < kKeyBlocks; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (key0 + 32 * b + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= limit[n]) s.s[n][b][i] = -__builtin_inff();
+}
 
-template <bool kMasked, class C, int kNq, int kKeyBlocks>
-__device__ __forceinline__ void softmax_tile(C& core, f32x16 (&s)[kNq][kKeyBlocks], float c, int key0, const int (&limit)[kNq],
-                                             int lane) {
+template <int kNq, int kKeyBlocks>
+__device__ __forceinline__ void maximum(const Scores<kNq, kKeyBlocks>& s, float (&mx)[kNq]) {
 #pragma unroll
   for (int n = 0; n < kNq; ++n) {
-    if constexpr (kMasked) {
+    mx[n] = s.s[n][0][0];
 #pragma unroll
-      for (int b = 0; b < kKeyBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (key0 + 32 * b + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= limit[n]) s[n][b][i] = -__builtin_inff();
-    }
-    float mx = s[n][0][0];
-#pragma unroll
-    for (int b = 0; b < kKeyBlocks; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[n][b][i]);
-    mx = max_halves(mx) * c;
-    // (row by row, so that a row's rounding does not depend on the others')
-    const bool grown = mx > core.m[n] + kSlack;
-    if (__any(grown)) {
-      const float f = grown ? exp2_hw(core.m[n] - mx) : 1.f;
-      if (grown) core.m[n] = mx;
-      core.l[n] *= f;
-#pragma unroll
-      for (int d = 0; d < C::kOut; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) core.o[n][d][i] *= f;
-    }
-    const float ms = core.m[n] == -__builtin_inff() ? 0.f : core.m[n];
-    float sum = 0.f;
-#pragma unroll
-    for (int b = 0; b < kKeyBlocks; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[n][b][i] = exp2_hw(__builtin_fmaf(s[n][b][i], c, -ms));
-        sum += s[n][b][i];
-      }
-    core.l[n] += sum;
+    for (int e = 1; e < 16 * kKeyBlocks; ++e) mx[n] = fmaxf(mx[n], s.s[n][e / 16][e % 16]);
   }
+}
+
+// The running maximum.  The one in use follows the true one only where that
+// has grown by more than kSlack (in powers of two): the weights stay far
+// below float's range, and most tiles need no rescaling of the output.  Row
+// by row, so that a row's rounding does not depend on the others'.
+constexpr float kSlack = 8.f;
+
+template <class C, int kNq>
+__device__ __forceinline__ void rescale(C& core, const bool (&grown)[kNq], const float (&top)[kNq]) {
+#pragma unroll
+  for (int n = 0; n < kNq; ++n) {
+    const float f = grown[n] ? exp2_hw(core.m[n] - top[n]) : 1.f;
+    if (grown[n]) core.m[n] = top[n];
+    core.l[n] *= f;
+#pragma unroll
+    for (int d = 0; d < C::kOut; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) core.o[n][d][i] *= f;
+  }
+}
+
+template <class C, int kNq>
+__device__ __forceinline__ void exponent_offsets(const C& core, float (&ms)[kNq]) {
+#pragma unroll
+  for (int n = 0; n < kNq; ++n) ms[n] = core.m[n] == -__builtin_inff() ? 0.f : core.m[n];
+}
+
+// With a tile's largest scores mx (a lane's own); ms: what the weights' exponents are taken against.
+template <class C, int kNq>
+__device__ __forceinline__ void update_maximum(C& core, const float (&mx)[kNq], float c, float (&ms)[kNq]) {
+  float top[kNq];
+  bool grown[kNq], any = false;
+#pragma unroll
+  for (int n = 0; n < kNq; ++n) {
+    top[n] = max_halves(mx[n]) * c;
+    grown[n] = top[n] > core.m[n] + kSlack;
+    any = any || grown[n];
+  }
+  if (__any(any)) rescale(core, grown, top);
+  exponent_offsets(core, ms);
 }
 
 }  // namespace gc

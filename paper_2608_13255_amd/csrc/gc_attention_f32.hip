@@ -6,16 +6,9 @@ namespace {
 
 template <int kDim>
 void launch(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream) {
-  constexpr int kBlocks = kDim <= 128 ? 2 : 1;
   constexpr int kWaves = attention_keys_waves(kDim, 4);
-  if constexpr (kDim <= 96) {
-    if (kind == kAttnRows8) {
-      hipLaunchKernelGGL((k_attention_rows<float, kDim, 1, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);
-      return;
-    }
-  }
   if (kind == kAttnKeys) hipLaunchKernelGGL((k_attention_keys<float, kDim, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, stream, p);
-  else hipLaunchKernelGGL((k_attention_rows<float, kDim, 1, kBlocks, 4, 1>), dim3(blocks), dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((k_attention_rows_f32<kDim, kDim <= 96 ? 2 : 1>), dim3(blocks), dim3(256), 0, stream, p);
 }
 
 }  // namespace

@@ -24,10 +24,32 @@ __device__ __forceinline__ void wait_lds() {
   asm volatile("" ::: "memory");
 }
 
+// A barrier that waits for no memory operation itself (__syncthreads waits
+// for all loads to LDS, the next tiles' among them).
+__device__ __forceinline__ void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Four channels of a finished row.
 __device__ __forceinline__ void store4(float* p, f32x4 x) { *reinterpret_cast<f32x4*>(p) = x; }
 __device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
   *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+}
+
+// Partial results pass between blocks on different dies, whose caches do not
+// follow each other's plain stores.  Relaxed atomics of device scope do not
+// stay in those caches, two floats at a time.
+__device__ __forceinline__ void share2(float* p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p),
+                     (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32, __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void shared2(const float* p, float& a, float& b) {
+  const unsigned long long x =
+      __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  a = __uint_as_float((uint32_t)x), b = __uint_as_float((uint32_t)(x >> 32));
 }
 
 // One row's result from its weighted sum (by four channels), maximum and sum.
@@ -48,7 +70,7 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& p, const Attenti
   const int half = lane >> 5;
 #pragma unroll
   for (int n = 0; n < kNq; ++n) {
-    const int local = first_row + n * 32 + (lane & 31);
+    const int local = first_row + 32 * n + (lane & 31);
     if (it.parts > 1) {
       float* part = p.partial + ((int64_t)it.slot * p.kv_heads + kv_head) * ((int64_t)tile_rows * (kDim + 2));
       float* row = part + (int64_t)local * kDim;
@@ -56,71 +78,79 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& p, const Attenti
       for (int d = 0; d < C::kOut; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          store4(row + 32 * d + 8 * g + 4 * half,
-                 f32x4{core.o[n][d][4 * g], core.o[n][d][4 * g + 1], core.o[n][d][4 * g + 2], core.o[n][d][4 * g + 3]});
-      if (half == 0) {
-        float* ml = part + (int64_t)tile_rows * kDim + 2 * local;
-        ml[0] = core.m[n];
-        ml[1] = l[n];
-      }
-    } else {
-      const RowOf r = row_of(p, it, kv_head, it.row0 + local);
-      if (!r.live) continue;
-      const Normaliser z(core.m[n], l[n]);
-      T* row = (T*)p.out + r.token * p.o_token + (int64_t)r.head * p.o_head;
-#pragma unroll
-      for (int d = 0; d < C::kOut; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int c = 32 * d + 8 * g + 4 * half;
-          if (c < p.dim) {
-            f32x4 x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = z.inv == 0.f && l[n] == 0.f ? 0.f : core.o[n][d][4 * g + j] * z.inv;
-            store4(row + c, x);
-          }
-        }
-      if (p.lse && half == 0) p.lse[(int64_t)r.head * p.total_q + r.token] = z.lse;
+          for (int j = 0; j < 4; j += 2)
+            share2(row + 32 * d + 8 * g + 4 * half + j, core.o[n][d][4 * g + j], core.o[n][d][4 * g + j + 1]);
+      if (half == 0) share2(part + (int64_t)tile_rows * kDim + 2 * local, core.m[n], l[n]);
+      continue;
     }
+    const RowOf r = row_of(p, it, kv_head, it.row0 + local);
+    if (!r.live) continue;
+    const Normaliser z(core.m[n], l[n]);
+    T* row = (T*)p.out + r.token * p.o_token + (int64_t)r.head * p.o_head;
+#pragma unroll
+    for (int d = 0; d < C::kOut; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = 32 * d + 8 * g + 4 * half;
+        if (c < p.dim) {
+          f32x4 x;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = l[n] == 0.f ? 0.f : core.o[n][d][4 * g + j] * z.inv;
+          store4(row + c, x);
+        }
+      }
+    if (p.lse && half == 0) p.lse[(int64_t)r.head * p.total_q + r.token] = z.lse;
   }
 }
 
 // After a block has written its part of split rows: the last of the tile's
 // blocks to finish adds the parts, in their order, and leaves the counter at
-// zero for the next call.  Every block's stores are complete and
-// released before its count; the last one's reads come after it has acquired
-// all of them.
+// zero for the next call.  A wave's stores have reached memory when its count
+// of outstanding ones is zero, a block's after the barrier that follows; only
+// then does the block count itself.  (A release fence of device scope would
+// write back the die's whole cache instead, block by block: 2048 tokens x 16 heads x 64 in
+// two parts took 94 us with it.)
 template <class T, int kDim>
 __device__ __forceinline__ void join_parts(const AttentionArgs& p, const AttentionItem& it, int kv_head, int tile_rows) {
   __shared__ uint32_t last;
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+  wait_loads<0>();
   __syncthreads();
   uint32_t* counter = p.counters + (int64_t)it.group_id * p.kv_heads + kv_head;
   if (threadIdx.x == 0)
-    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)it.parts;
+    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)it.parts;
   __syncthreads();
   if (!last) return;
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  const int64_t stride = (int64_t)tile_rows * (kDim + 2);
-  const float* first = p.partial + ((int64_t)it.slot0 * p.kv_heads + kv_head) * stride;
+  const int64_t stride = (int64_t)tile_rows * (kDim + 2) * p.kv_heads;   // from part to part
+  const float* first = p.partial + ((int64_t)it.slot0 * p.kv_heads + kv_head) * ((int64_t)tile_rows * (kDim + 2));
   const int rows = it.rows - it.row0 < tile_rows ? it.rows - it.row0 : tile_rows;
   for (int e = threadIdx.x; e < rows * (kDim / 4); e += blockDim.x) {
     const int local = e / (kDim / 4), c = (e % (kDim / 4)) * 4;
     if (c >= p.dim) continue;
     const float* ml = first + (int64_t)tile_rows * kDim + 2 * local;
-    float m = -__builtin_inff();
-    for (int i = 0; i < it.parts; ++i) m = fmaxf(m, ml[i * stride * p.kv_heads]);
-    const float ms = m == -__builtin_inff() ? 0.f : m;
-    float l = 0.f;
+    const float* row = first + (int64_t)local * kDim + c;
+    // the parts' maxima one by one as they come, four parts' loads together
+    float m = -__builtin_inff(), l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < it.parts; ++i) {
-      const int64_t at = i * stride * p.kv_heads;
-      const float f = exp2_hw(ml[at] - ms);
-      l += ml[at + 1] * f;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(first + at + (int64_t)local * kDim + c);
+    for (int i0 = 0; i0 < it.parts; i0 += 4) {
+      float mi[4], li[4], x[4][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] += x[j] * f;
+      for (int i = 0; i < 4; ++i) {
+        const int64_t at = (i0 + i < it.parts ? i0 + i : i0) * stride;
+        shared2(ml + at, mi[i], li[i]);
+        shared2(row + at, x[i][0], x[i][1]);
+        shared2(row + at + 2, x[i][2], x[i][3]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i0 + i >= it.parts) continue;
+        const float mn = fmaxf(m, mi[i]), ms = mn == -__builtin_inff() ? 0.f : mn;
+        const float f = exp2_hw(m - ms), g = exp2_hw(mi[i] - ms);
+        m = mn;
+        l = l * f + li[i] * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[i][j] * g;
+      }
     }
     const RowOf r = row_of(p, it, kv_head, it.row0 + local);
     const Normaliser z(m, l);
@@ -131,48 +161,46 @@ __device__ __forceinline__ void join_parts(const AttentionArgs& p, const Attenti
   }
 }
 
-// The weights of one tile and their values.  Without kMasked every row of the
-// wave sees all of the tile.  Returns whether values were left out
-// (add_nonfinite).
-template <bool kMasked, int kKeyBlocks, class C, int kNq>
-__device__ __forceinline__ uint32_t tile_step(C& core, const char* kt, const char* vt, float c, int key0, const int (&limit)[kNq],
-                                              int lane) {
-  f32x16 s[kNq][kKeyBlocks];
-  core.scores(kt, lane, s);
-  softmax_tile<kMasked>(core, s, c, key0, limit, lane);
-  return core.template add_values<kMasked>(vt, lane, s);
-}
-
 // ---------------------------------------------------------------------------
-// rows: the waves of a block hold 32 kNq rows each and walk the same keys,
-// two tiles in LDS: one is worked on while the next arrives.
+// rows, bfloat16: the waves of a block hold 32 rows each and walk the same
+// keys.  A wave's work at tile i has two parts, each of matrix products beside
+// vector work that does not need them: tile i - 1's values with tile i's
+// maximum, then tile i + 1's scores with tile i's weights
+// (values_and_maximum, weights_and_scores).  K tiles lie in two places in
+// turn, V tiles in four.
+//
+// At tile i the block has passed a barrier after which K of i + 1 and V of i
+// are there, and nobody reads K of i or V of i - 2 any more: K of i + 2 and V
+// of i + 2 are asked for in their places.  The next barrier waits for that K
+// and for the V asked for a tile before; the last V may be outstanding.
 // ---------------------------------------------------------------------------
-template <class T, int kDim, int kNq, int kKeyBlocks, int kWaves, int kPerSimd>
-__global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const AttentionArgs p) {
+template <int kDim, int kNq, int kKeyBlocks, int kWaves>
+__device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
+  using T = uint16_t;
   constexpr int kKeys = 32 * kKeyBlocks, kTile = kKeys * kDim * (int)sizeof(T), kRows = 32 * kNq * kWaves;
-  __shared__ __attribute__((aligned(1024))) char lds[4 * kTile];
+  // an array a tile: the compiler then sees that a read of one does not wait for the loads to another
+  __shared__ __attribute__((aligned(1024))) char k0[kTile], k1[kTile], v0[kTile], v1[kTile], v2[kTile], v3[kTile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv_head = blockIdx.x % p.kv_heads;
   const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
 
-  TileLoader<T, kDim, kKeys, kWaves> kl, vl;
-  kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, wave, lane);
-  vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, wave, lane);
-
-  Core<T, kDim, kNq, kKeyBlocks> core;
+  using C = Core<T, kDim, kNq, kKeyBlocks>;
+  C core;
   core.init();
   const int first_row = wave * 32 * kNq;
   int limit[kNq];
 #pragma unroll
   for (int n = 0; n < kNq; ++n) {
-    const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + n * 32 + (lane & 31));
+    const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + 32 * n + (lane & 31));
     limit[n] = r.limit < it.k_end ? r.limit : it.k_end;
     core.load_q(n, (const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
   }
-  if (it.k_begin < it.k_end) {
-    kl.load(lds, it.k_begin, it.k_len, wave);
-    vl.load(lds + kTile, it.k_begin, it.k_len, wave);
-  }
+
+  using Loader = TileLoader<T, kDim, kKeys, kWaves>;
+  Loader kl, vl;
+  // (to the sequence's end, not the part's: what a part's last tile holds past it is masked)
+  kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, it.k_begin, it.k_len, wave, lane);
+  vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, it.k_begin, it.k_len, wave, lane);
   // the wave's rows see at most high keys, the block's rows at least low (limits grow with the row)
   const int high = __builtin_amdgcn_readlane(limit[kNq - 1], 31);
   int low = it.k_end;
@@ -182,39 +210,168 @@ __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const 
   }
   const float c = p.scale * kLog2e;
 
-  int stage = 0;
-  // the tile at key0 is there and nobody reads the other one, which the next one goes to
-  const auto next = [&](int key0) {
+  int key0 = it.k_begin;
+  typename C::S even, odd;   // scores of even and odd tiles
+  typename C::Weights w;
+  typename C::Operands x;
+  float mx[kNq], ms[kNq];
+  uint32_t bad = 0;
+  int first_masked = key0;
+
+  if (key0 < it.k_end) {
+    kl.load(k0, wave);
+    kl.load(k1, wave);
+    vl.load(v0, wave);
+    vl.load(v1, wave);
     wait_loads<0>();
     __syncthreads();
-    char* kt = lds + stage * 2 * kTile;
-    stage ^= 1;
-    if (key0 + kKeys < it.k_end) {
-      kl.load(lds + stage * 2 * kTile, key0 + kKeys, it.k_len, wave);
-      vl.load(lds + stage * 2 * kTile + kTile, key0 + kKeys, it.k_len, wave);
-    }
-    return kt;
-  };
-  int key0 = it.k_begin;
-  for (; key0 + kKeys <= low; key0 += kKeys) {
-    const char* kt = next(key0);
-    tile_step<false, kKeyBlocks>(core, kt, kt + kTile, c, key0, limit, lane);
+    core.scores(k0, lane, even);
+    __syncthreads();
+    kl.load(k0, wave);
+    vl.load(v2, wave);
+    mask(even, key0, limit, lane);
+    maximum(even, mx);
+    update_maximum(core, mx, c, ms);
+    core.weights(even, c, ms, w);
+    core.scores(k1, lane, odd);
+    key0 += kKeys;
   }
-  const int first_masked = key0;
-  uint32_t bad = 0;
-  for (; key0 < it.k_end; key0 += kKeys) {
-    const char* kt = next(key0);
-    if (key0 < high) bad |= tile_step<true, kKeyBlocks>(core, kt, kt + kTile, c, key0, limit, lane);
+  const auto arrive = [&] {
+    wait_loads<Loader::kMine>();
+    barrier_only();
+  };
+  // tile i at key0, nothing masked in it nor before it
+  const auto tile = [&](typename C::S& now, typename C::S& next, char* k_now, char* k_next, char* v_before, char* v_now, char* v_after) {
+    arrive();
+    kl.load(k_now, wave);
+    vl.load(v_after, wave);
+    core.values_and_maximum(x, v_before, w, now, k_next, lane, mx);
+    update_maximum(core, mx, c, ms);
+    core.weights_and_scores(x, now, c, ms, w, k_next, next, v_now, lane);
+    key0 += kKeys;
+  };
+  int phase = 1;   // i % 4
+  if (key0 + kKeys <= low) {
+    C::first_values(v0, lane, x);
+    while (key0 + 4 * kKeys <= low) {
+      tile(odd, even, k1, k0, v0, v1, v3);
+      tile(even, odd, k0, k1, v1, v2, v0);
+      tile(odd, even, k1, k0, v2, v3, v1);
+      tile(even, odd, k0, k1, v3, v0, v2);
+    }
+  }
+  // the other tiles: scores are masked, and values that are not finite left out
+  if (it.k_begin < it.k_end) {
+    first_masked = key0 - kKeys;
+    if (phase & 1) even = odd;
+    while (key0 < it.k_end) {
+      arrive();
+      char* const k_now = phase & 1 ? k1 : k0;
+      kl.load(k_now, wave);
+      vl.load(phase == 0 ? v2 : phase == 1 ? v3 : phase == 2 ? v0 : v1, wave);
+      if (key0 - kKeys < high) bad |= core.add_masked(phase == 0 ? v3 : phase == 1 ? v0 : phase == 2 ? v1 : v2, lane, w);
+      if (key0 < high) {
+        mask(even, key0, limit, lane);
+        maximum(even, mx);
+        update_maximum(core, mx, c, ms);
+        core.weights(even, c, ms, w);
+        core.scores(phase & 1 ? k0 : k1, lane, even);
+      }
+      key0 += kKeys;
+      phase = (phase + 1) & 3;
+    }
+    wait_loads<0>();
+    __syncthreads();
+    if (key0 - kKeys < high) bad |= core.add_masked(phase == 0 ? v3 : phase == 1 ? v0 : phase == 2 ? v1 : v2, lane, w);
   }
 
-  if (__any(bad != 0)) {
-    add_nonfinite<T>(core, vl.base, vl.stride, p.dim, first_masked, high, kKeys, kKeys, limit, lane);
-  }
+  if (__any(bad != 0)) add_nonfinite<T>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
   float l[kNq];
 #pragma unroll
   for (int n = 0; n < kNq; ++n) l[n] = sum_halves(core.l[n]);
   store_rows<T, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
   if (it.parts > 1) join_parts<T, kDim>(p, it, kv_head, kRows);
+}
+
+template <int kDim, int kNq, int kKeyBlocks, int kWaves, int kPerSimd>
+__global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const AttentionArgs p) {
+  attention_rows<kDim, kNq, kKeyBlocks, kWaves>(p);
+}
+
+// ---------------------------------------------------------------------------
+// rows, float32: a product takes sixteen times as long as bfloat16's, so a
+// tile's parts follow one another and the blocks of a compute unit (or its
+// four waves) fill the gaps.  Two places for K and V each: one tile is worked
+// on while the next arrives.
+// ---------------------------------------------------------------------------
+template <int kDim, int kPerSimd>
+__global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const AttentionArgs p) {
+  constexpr int kWaves = 4, kKeys = 32, kTile = kKeys * kDim * 4, kRows = 32 * kWaves;
+  __shared__ __attribute__((aligned(1024))) char k0[kTile], k1[kTile], v0[kTile], v1[kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kv_head = blockIdx.x % p.kv_heads;
+  const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
+
+  using C = Core<float, kDim, 1, 1>;
+  C core;
+  core.init();
+  const int first_row = wave * 32;
+  const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + (lane & 31));
+  const int limit[1] = {r.limit < it.k_end ? r.limit : it.k_end};
+  core.load_q(0, (const float*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
+
+  TileLoader<float, kDim, kKeys, kWaves> kl, vl;
+  kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, it.k_begin, it.k_len, wave, lane);
+  vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, it.k_begin, it.k_len, wave, lane);
+  const int high = __builtin_amdgcn_readlane(limit[0], 31);
+  int low = it.k_end;
+  if (p.causal) {
+    const int least = it.row0 / p.group + it.reach;
+    low = least < low ? least : low;
+  }
+  const float c = p.scale * kLog2e;
+
+  int key0 = it.k_begin;
+  uint32_t bad = 0;
+  const auto tile = [&](auto masked, const char* k_now, const char* v_now, char* k_next, char* v_next) {
+    constexpr bool kMasked = decltype(masked)::value;
+    wait_loads<0>();
+    __syncthreads();   // this tile is there, and nobody reads the other one
+    kl.load(k_next, wave);
+    vl.load(v_next, wave);
+    if (!kMasked || key0 < high) {
+      typename C::S s;
+      typename C::Weights w;
+      float mx[1], ms[1];
+      core.scores(k_now, lane, s);
+      if constexpr (kMasked) mask(s, key0, limit, lane);
+      maximum(s, mx);
+      update_maximum(core, mx, c, ms);
+      core.weights(s, c, ms, w);
+      if constexpr (kMasked) bad |= core.add_masked(v_now, lane, w);
+      else core.add_values(v_now, lane, w);
+    }
+    key0 += kKeys;
+  };
+  if (key0 < it.k_end) {
+    kl.load(k0, wave);
+    vl.load(v0, wave);
+  }
+  while (key0 + 2 * kKeys <= low) {
+    tile(std::false_type{}, k0, v0, k1, v1);
+    tile(std::false_type{}, k1, v1, k0, v0);
+  }
+  const int first_masked = key0;
+  for (bool other = false; key0 < it.k_end; other = !other) {
+    if (other) tile(std::true_type{}, k1, v1, k0, v0);
+    else tile(std::true_type{}, k0, v0, k1, v1);
+  }
+  wait_loads<0>();   // before the block's LDS is given up
+
+  if (__any(bad != 0)) add_nonfinite<float>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
+  const float l[1] = {sum_halves(core.l[0])};
+  store_rows<float, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
+  if (it.parts > 1) join_parts<float, kDim>(p, it, kv_head, kRows);
 }
 
 // ---------------------------------------------------------------------------
@@ -239,25 +396,22 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   // Tile i of the wave: K at mine + i % 2 * 2 kTile, V behind it.  Two tiles
   // are on their way at any time: a K tile's successor but one is asked for as soon
   // as its scores are in registers, a V tile's as soon as its products are issued.
-  TileLoader<T, kDim, kKeys, 1> kl, vl;
-  kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, 0, lane);
-  vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, 0, lane);
+  TileLoader<T, kDim, kKeys, 1, kWaves> kl, vl;
   const int first = it.k_begin + wave * kKeys;
   constexpr int kStep = kWaves * kKeys;
-  const int last_key = it.k_len - 1;
-  // past the wave's last tile the loads go on, from a tile that is there, so that the counts below hold
-  const auto load_k = [&](int key0, int stage) { kl.load(mine + stage * 2 * kTile, key0 < it.k_end ? key0 : last_key, it.k_len, 0); };
-  const auto load_v = [&](int key0, int stage) { vl.load(mine + stage * 2 * kTile + kTile, key0 < it.k_end ? key0 : last_key, it.k_len, 0); };
-  Core<T, kDim, 1, 1> core;
+  kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, first, it.k_len, 0, lane);
+  vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, first, it.k_len, 0, lane);
+  using C = Core<T, kDim, 1, 1>;
+  C core;
   core.init();
   const RowOf r = row_of(p, it, kv_head, it.row0 + (lane & 31));
   const int limit[1] = {r.limit < it.k_end ? r.limit : it.k_end};
   core.load_q(0, (const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
   if (first < it.k_end) {
-    load_k(first, 0);
-    load_v(first, 0);
-    load_k(first + kStep, 1);
-    load_v(first + kStep, 1);
+    kl.load(mine, 0);
+    vl.load(mine + kTile, 0);
+    kl.load(mine + 2 * kTile, 0);
+    vl.load(mine + 3 * kTile, 0);
   }
   const int low = __builtin_amdgcn_readfirstlane(limit[0]);
   const int high = __builtin_amdgcn_readlane(limit[0], 31);
@@ -267,16 +421,23 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   const auto tile = [&](int key0, auto masked) {
     constexpr bool kMasked = decltype(masked)::value;
     char* kt = mine + stage * 2 * kTile;
-    f32x16 s[1][1];
+    typename C::S s;
+    typename C::Weights w;
+    float mx[1], ms[1];
     wait_loads<kLeft>();
     core.scores(kt, lane, s);
     wait_lds();
-    load_k(key0 + 2 * kStep, stage);
-    softmax_tile<kMasked>(core, s, c, key0, limit, lane);
+    kl.load(kt, 0);
+    if constexpr (kMasked) mask(s, key0, limit, lane);
+    maximum(s, mx);
+    update_maximum(core, mx, c, ms);
+    core.weights(s, c, ms, w);
     wait_loads<kLeft>();
-    const uint32_t left_out = core.template add_values<kMasked>(kt + kTile, lane, s);
+    uint32_t left_out = 0;
+    if constexpr (kMasked) left_out = core.add_masked(kt + kTile, lane, w);
+    else core.add_values(kt + kTile, lane, w);
     wait_lds();
-    load_v(key0 + 2 * kStep, stage);
+    vl.load(kt + kTile, 0);
     stage ^= 1;
     return left_out;
   };
@@ -286,7 +447,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   uint32_t bad = 0;
   for (; key0 < high; key0 += kStep) bad |= tile(key0, std::true_type{});
   if (__any(bad != 0))
-    add_nonfinite<T>(core, vl.base, vl.stride, p.dim, first_masked, high, kKeys, kWaves * kKeys, limit, lane);
+    add_nonfinite<T>(p, it, kv_head, core, first_masked, high, kKeys, kWaves * kKeys, limit, lane);
   // the waves' results, added by the first wave in their order
   float l[1] = {sum_halves(core.l[0])};
   wait_loads<0>();   // (also before the block's LDS is given up)

@@ -25,17 +25,16 @@ struct AttentionItem {
 static_assert(sizeof(AttentionItem) == GC_ATTENTION_ITEM_WORDS * 4, "item words");
 
 // Kernel variants (gc_attention_info.kind) and their rows an item.
-enum AttentionKind { kAttnRows8 = 0, kAttnRows4 = 1, kAttnKeys = 2, kAttnKinds = 3 };
-inline int attention_tile_rows(int kind) { return kind == kAttnRows8 ? 256 : kind == kAttnRows4 ? 128 : 32; }
+enum AttentionKind { kAttnRows256 = 0, kAttnRows128 = 1, kAttnKeys = 2, kAttnKinds = 3 };
+inline int attention_tile_rows(int kind) { return kind == kAttnRows256 ? 256 : kind == kAttnRows128 ? 128 : 32; }
 
 // Head dims are padded to the next of these in LDS and registers.
 inline int attention_padded_dim(int dim) {
   return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;
 }
 
-// Whether eight waves' rows fit the registers at two waves a SIMD; wider
-// heads take four waves with a SIMD's registers each.
-inline bool attention_has_rows8(int dim, int dtype) { return attention_padded_dim(dim) <= (dtype == GC_F32 ? 96 : 128); }
+// Whether two waves' rows a SIMD fit the registers with eight waves a block.
+inline bool attention_has_rows256(int dim, int dtype) { return dtype == GC_BF16 && attention_padded_dim(dim) <= 128; }
 
 // The waves of a block of kAttnKeys: two tiles of 32 keys and values each, in
 // at most 128 KiB; and the blocks of a compute unit (160 KiB of LDS).
