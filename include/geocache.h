@@ -729,10 +729,10 @@ int gc_qk_norm_rope(const gc_heads* q, int heads, const gc_heads* k, int kv_head
  *   info     host, as gc_attention_plan filled it
  *   items    device int32, a copy of the plan's items, 16-byte aligned
  *   scale    finite, > 0
- *   workspace  device, info->workspace_bytes, 16-byte aligned, zero before its
- *            first use; a call leaves it ready for the next.  Calls in flight
- *            at the same time need workspaces of their own.  May be NULL if
- *            info->workspace_bytes is 0.
+ *   workspace  device, info->workspace_bytes, 16-byte aligned; its contents
+ *            are of no consequence.  Calls in flight at the same time need
+ *            workspaces of their own.  May be NULL if info->workspace_bytes
+ *            is 0.
  * The result does not depend on the order in which blocks run.
  */
 #define GC_ATTENTION_ITEM_WORDS 12

@@ -1157,8 +1157,7 @@ def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, 
                       dtype: torch.dtype, causal: bool = False, device="cuda", stream=None) -> AttentionPlan:
     """Work of attention over packed sequences of these lengths (host lists),
     for gc_attention: made once and kept while the lengths stay.  The items
-    are copied and the workspace cleared on `stream` (default: torch's current
-    stream)."""
+    are copied on `stream` (default: torch's current stream)."""
     if len(q_lens) != len(k_lens):
         raise ValueError("q_lens and k_lens must have the same length")
     code = _HEAD_CODES.get(dtype)
@@ -1180,7 +1179,7 @@ def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, 
     s = _side_stream(stream)
     with torch.cuda.stream(s if s is not None else torch.cuda.current_stream()):
         items = torch.from_numpy(host).to(device)
-        ws = (torch.zeros(info.workspace_bytes, dtype=torch.uint8, device=device) if info.workspace_bytes else None)
+        ws = (torch.empty(info.workspace_bytes, dtype=torch.uint8, device=device) if info.workspace_bytes else None)
     return AttentionPlan(info, items, ws)
 
 

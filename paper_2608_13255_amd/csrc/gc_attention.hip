@@ -71,8 +71,11 @@ void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
     const int64_t n = keys_seen(b, s, r, tile);
     work += n, most = std::max(most, n);
   });
-  // the shortest parts with which all blocks are there at once, so that they end together
-  int64_t low = std::max<int64_t>(work * b.kv_heads / blocks + 1, *kind == kAttnKeys ? 256 : 512), high = std::max(low, most);
+  // The shortest parts with which all blocks are there at once, so that they end together, but none shorter than pays for
+  // joining it: 512 keys of bfloat16 (1024 tokens x 16 heads x 64: 19.2 us against 22.5 with 256), 256 of float, whose
+  // products take longer, and of single tokens (8 x 1000 keys: 14.3 us against 16.4 with 512).
+  const int64_t least = *kind == kAttnKeys || dtype == GC_F32 ? 256 : 512;
+  int64_t low = std::max<int64_t>(work * b.kv_heads / blocks + 1, least), high = std::max(low, most);
   while (low < high) {
     const int64_t mid = (low + high) / 2;
     if (items_of(b, tile, (int)mid) * b.kv_heads <= blocks) high = mid;
@@ -81,8 +84,6 @@ void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
   low = (low + kPartKeys - 1) / kPartKeys * kPartKeys;
   *part = (int)std::min<int64_t>(low, 0x7fffffc0);
 }
-
-int64_t counter_bytes(int64_t n_groups, int kv_heads) { return (n_groups * kv_heads * 4 + 255) / 256 * 256; }
 
 }  // namespace
 }  // namespace gc
@@ -124,8 +125,7 @@ extern "C" int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, i
   info->n_seq = n_seq, info->total_q = (int32_t)total_q, info->total_k = (int32_t)total_k;
   info->kind = kind, info->tile_rows = tile, info->n_items = (int32_t)n_items;
   info->n_slots = (int32_t)n_slots, info->n_groups = (int32_t)n_groups;
-  info->workspace_bytes = n_slots == 0 ? 0 : counter_bytes(n_groups, kv_heads) +
-                          n_slots * kv_heads * tile * (int64_t)(attention_padded_dim(dim) + 2) * 4;
+  info->workspace_bytes = n_slots * kv_heads * tile * (int64_t)(attention_padded_dim(dim) + 2) * 4;
   if (!items) return GC_OK;
   if (capacity_words < n_items * GC_ATTENTION_ITEM_WORDS)
     return fail(GC_ERR_CAPACITY, "%s: %lld words for %lld items of %d", who, (long long)capacity_words, (long long)n_items, GC_ATTENTION_ITEM_WORDS);
@@ -159,8 +159,7 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
   if (info->kv_heads < 1 || info->heads % info->kv_heads || info->kind < 0 || info->kind >= kAttnKinds ||
       (info->kind == kAttnRows256 && !attention_has_rows256(info->dim, info->dtype)) || info->tile_rows != attention_tile_rows(info->kind) ||
       info->n_items < 0 || info->total_q < 0 || info->total_k < 0 || info->n_slots < 0 || info->n_groups < 0 ||
-      info->workspace_bytes < (info->n_slots == 0 ? 0 : counter_bytes(info->n_groups, info->kv_heads) + (int64_t)info->n_slots *
-                               info->kv_heads * info->tile_rows * (attention_padded_dim(info->dim) + 2) * 4))
+      info->workspace_bytes < (int64_t)info->n_slots * info->kv_heads * info->tile_rows * (attention_padded_dim(info->dim) + 2) * 4)
     return fail(GC_ERR_ARG, "%s: info is not gc_attention_plan's", who);
   if (!(scale > 0.0) || !std::isfinite(scale)) return fail(GC_ERR_ARG, "%s: scale must be finite and above 0", who);
   if (info->n_items == 0) return GC_OK;
@@ -209,10 +208,7 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
   p.total_q = info->total_q, p.total_k = info->total_k;
   p.causal = info->causal;
   p.scale = (float)scale;
-  if (info->n_slots > 0) {
-    p.counters = reinterpret_cast<uint32_t*>(workspace);
-    p.partial = reinterpret_cast<float*>((char*)workspace + counter_bytes(info->n_groups, info->kv_heads));
-  }
+  if (info->n_slots > 0) p.partial = reinterpret_cast<float*>(workspace);
   const unsigned blocks = (unsigned)(info->n_items * info->kv_heads);
   const bool known = dtype == GC_F32 ? launch_attention_f32(p, info->kind, blocks, stream)
                                      : launch_attention_bf16(p, info->kind, blocks, stream);

@@ -8,7 +8,8 @@ template <int kDim>
 void launch(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream) {
   constexpr int kWaves = attention_keys_waves(kDim, 4);
   if (kind == kAttnKeys) hipLaunchKernelGGL((k_attention_keys<float, kDim, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, stream, p);
-  else hipLaunchKernelGGL((k_attention_rows_f32<kDim, kDim <= 96 ? 2 : 1>), dim3(blocks), dim3(256), 0, stream, p);
+  else if (kind == kAttnRows128) hipLaunchKernelGGL((k_attention_rows_f32<kDim, kDim <= 96 ? 2 : 1>), dim3(blocks), dim3(256), 0, stream, p);
+  launch_join<float, kDim>(p, attention_tile_rows(kind), blocks, stream);
 }
 
 }  // namespace

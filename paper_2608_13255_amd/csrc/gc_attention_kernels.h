@@ -38,20 +38,6 @@ __device__ __forceinline__ void store4(uint16_t* p, f32x4 x) {
   *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
 }
 
-// Partial results pass between blocks on different dies, whose caches do not
-// follow each other's plain stores.  Relaxed atomics of device scope do not
-// stay in those caches, two floats at a time.
-__device__ __forceinline__ void share2(float* p, float a, float b) {
-  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p),
-                     (unsigned long long)__float_as_uint(a) | (unsigned long long)__float_as_uint(b) << 32, __ATOMIC_RELAXED,
-                     __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void shared2(const float* p, float& a, float& b) {
-  const unsigned long long x =
-      __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  a = __uint_as_float((uint32_t)x), b = __uint_as_float((uint32_t)(x >> 32));
-}
-
 // One row's result from its weighted sum (by four channels), maximum and sum.
 struct Normaliser {
   float inv, lse;
@@ -78,9 +64,9 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& p, const Attenti
       for (int d = 0; d < C::kOut; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-          for (int j = 0; j < 4; j += 2)
-            share2(row + 32 * d + 8 * g + 4 * half + j, core.o[n][d][4 * g + j], core.o[n][d][4 * g + j + 1]);
-      if (half == 0) share2(part + (int64_t)tile_rows * kDim + 2 * local, core.m[n], l[n]);
+          store4(row + 32 * d + 8 * g + 4 * half,
+                 f32x4{core.o[n][d][4 * g], core.o[n][d][4 * g + 1], core.o[n][d][4 * g + 2], core.o[n][d][4 * g + 3]});
+      if (half == 0) *reinterpret_cast<float2*>(part + (int64_t)tile_rows * kDim + 2 * local) = float2{core.m[n], l[n]};
       continue;
     }
     const RowOf r = row_of(p, it, kv_head, it.row0 + local);
@@ -103,62 +89,61 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& p, const Attenti
   }
 }
 
-// After a block has written its part of split rows: the last of the tile's
-// blocks to finish adds the parts, in their order, and leaves the counter at
-// zero for the next call.  A wave's stores have reached memory when its count
-// of outstanding ones is zero, a block's after the barrier that follows; only
-// then does the block count itself.  (A release fence of device scope would
-// write back the die's whole cache instead, block by block: 2048 tokens x 16 heads x 64 in
-// two parts took 94 us with it.)
+// Adds the parts of split rows, in their order: a launch of its own after the
+// parts', one block for kJoin runs of four channels of one tile (blocks of
+// items that are not their tile's first part have nothing to do).  (Joined by the last of a
+// tile's blocks instead, 2048 tokens x 16 heads x 64 in two parts took 48 us, 160 rows over 9000 keys in 18
+// parts 74 us: that block alone waits for one load after the other.)
+constexpr int kJoin = 256;
+
 template <class T, int kDim>
-__device__ __forceinline__ void join_parts(const AttentionArgs& p, const AttentionItem& it, int kv_head, int tile_rows) {
-  __shared__ uint32_t last;
-  wait_loads<0>();
-  __syncthreads();
-  uint32_t* counter = p.counters + (int64_t)it.group_id * p.kv_heads + kv_head;
-  if (threadIdx.x == 0)
-    last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (uint32_t)it.parts;
-  __syncthreads();
-  if (!last) return;
-  if (threadIdx.x == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+__global__ __launch_bounds__(kJoin) void k_attention_join(const AttentionArgs p, int tile_rows) {
+  const int kv_head = blockIdx.x % p.kv_heads;
+  const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
+  if (it.parts < 2 || it.slot != it.slot0) return;
+  const int rows = it.rows - it.row0 < tile_rows ? it.rows - it.row0 : tile_rows;
+  const int e = blockIdx.y * kJoin + threadIdx.x, local = e / (kDim / 4), c = e % (kDim / 4) * 4;
+  if (local >= rows || c >= p.dim) return;
   const int64_t stride = (int64_t)tile_rows * (kDim + 2) * p.kv_heads;   // from part to part
   const float* first = p.partial + ((int64_t)it.slot0 * p.kv_heads + kv_head) * ((int64_t)tile_rows * (kDim + 2));
-  const int rows = it.rows - it.row0 < tile_rows ? it.rows - it.row0 : tile_rows;
-  for (int e = threadIdx.x; e < rows * (kDim / 4); e += blockDim.x) {
-    const int local = e / (kDim / 4), c = (e % (kDim / 4)) * 4;
-    if (c >= p.dim) continue;
-    const float* ml = first + (int64_t)tile_rows * kDim + 2 * local;
-    const float* row = first + (int64_t)local * kDim + c;
-    // the parts' maxima one by one as they come, four parts' loads together
-    float m = -__builtin_inff(), l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < it.parts; i0 += 4) {
-      float mi[4], li[4], x[4][4];
+  const float* ml = first + (int64_t)tile_rows * kDim + 2 * local;
+  const float* row = first + (int64_t)local * kDim + c;
+  // with the maxima as they come, four parts' loads together
+  float m = -__builtin_inff(), l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = 0; i0 < it.parts; i0 += 4) {
+    float2 x[4];
+    f32x4 y[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t at = (i0 + i < it.parts ? i0 + i : i0) * stride;
-        shared2(ml + at, mi[i], li[i]);
-        shared2(row + at, x[i][0], x[i][1]);
-        shared2(row + at + 2, x[i][2], x[i][3]);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (i0 + i >= it.parts) continue;
-        const float mn = fmaxf(m, mi[i]), ms = mn == -__builtin_inff() ? 0.f : mn;
-        const float f = exp2_hw(m - ms), g = exp2_hw(mi[i] - ms);
-        m = mn;
-        l = l * f + li[i] * g;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[i][j] * g;
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at = (i0 + i < it.parts ? i0 + i : i0) * stride;
+      x[i] = *reinterpret_cast<const float2*>(ml + at);
+      y[i] = *reinterpret_cast<const f32x4*>(row + at);
     }
-    const RowOf r = row_of(p, it, kv_head, it.row0 + local);
-    const Normaliser z(m, l);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] * z.inv;
-    store4((T*)p.out + r.token * p.o_token + (int64_t)r.head * p.o_head + c, o);
-    if (p.lse && c == 0) p.lse[(int64_t)r.head * p.total_q + r.token] = z.lse;
+    for (int i = 0; i < 4; ++i) {
+      if (i0 + i >= it.parts) continue;
+      const float mn = fmaxf(m, x[i].x), ms = mn == -__builtin_inff() ? 0.f : mn;
+      const float f = exp2_hw(m - ms), g = exp2_hw(x[i].x - ms);
+      m = mn;
+      l = l * f + x[i].y * g;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * f + y[i][j] * g;
+    }
   }
+  const RowOf r = row_of(p, it, kv_head, it.row0 + local);
+  const Normaliser z(m, l);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] * z.inv;
+  store4((T*)p.out + r.token * p.o_token + (int64_t)r.head * p.o_head + c, o);
+  if (p.lse && c == 0) p.lse[(int64_t)r.head * p.total_q + r.token] = z.lse;
+}
+
+template <class T, int kDim>
+void launch_join(const AttentionArgs& p, int tile_rows, unsigned blocks, hipStream_t stream) {
+  if (p.partial)
+    hipLaunchKernelGGL((k_attention_join<T, kDim>), dim3(blocks, (unsigned)(tile_rows * (kDim / 4) / kJoin)), dim3(kJoin), 0, stream,
+                       p, tile_rows);
 }
 
 // ---------------------------------------------------------------------------
@@ -290,7 +275,6 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
 #pragma unroll
   for (int n = 0; n < kNq; ++n) l[n] = sum_halves(core.l[n]);
   store_rows<T, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
-  if (it.parts > 1) join_parts<T, kDim>(p, it, kv_head, kRows);
 }
 
 template <int kDim, int kNq, int kKeyBlocks, int kWaves, int kPerSimd>
@@ -371,7 +355,6 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
   if (__any(bad != 0)) add_nonfinite<float>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
   const float l[1] = {sum_halves(core.l[0])};
   store_rows<float, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
-  if (it.parts > 1) join_parts<float, kDim>(p, it, kv_head, kRows);
 }
 
 // ---------------------------------------------------------------------------
@@ -396,7 +379,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   // Tile i of the wave: K at mine + i % 2 * 2 kTile, V behind it.  Two tiles
   // are on their way at any time: a K tile's successor but one is asked for as soon
   // as its scores are in registers, a V tile's as soon as its products are issued.
-  TileLoader<T, kDim, kKeys, 1, kWaves> kl, vl;
+  TileLoader<T, kDim, kKeys, 1, kWaves, true> kl, vl;
   const int first = it.k_begin + wave * kKeys;
   constexpr int kStep = kWaves * kKeys;
   kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, first, it.k_len, 0, lane);
@@ -485,7 +468,6 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
     }
   }
   if (wave == 0) store_rows<T, kDim>(p, it, kv_head, core, l, 0, 32, lane);
-  if (it.parts > 1) join_parts<T, kDim>(p, it, kv_head, 32);
 }
 
 }  // namespace gc

@@ -20,7 +20,7 @@ struct AttentionItem {
   int32_t slot;       // this part's partial result, -1: the item holds all of its rows' keys
   int32_t slot0;      // the tile's first part
   int32_t parts;      // its number of parts
-  int32_t group_id;   // its counter
+  int32_t group_id;   // its number among the split tiles
 };
 static_assert(sizeof(AttentionItem) == GC_ATTENTION_ITEM_WORDS * 4, "item words");
 
