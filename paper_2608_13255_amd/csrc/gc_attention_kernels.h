@@ -244,6 +244,19 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
       tile(odd, even, k1, k0, v2, v3, v1);
       tile(even, odd, k0, k1, v3, v0, v2);
     }
+    // up to three more
+    if (key0 + kKeys <= low) {
+      tile(odd, even, k1, k0, v0, v1, v3);
+      phase = 2;
+      if (key0 + kKeys <= low) {
+        tile(even, odd, k0, k1, v1, v2, v0);
+        phase = 3;
+        if (key0 + kKeys <= low) {
+          tile(odd, even, k1, k0, v2, v3, v1);
+          phase = 0;
+        }
+      }
+    }
   }
   // the other tiles: scores are masked, and values that are not finite left out
   if (it.k_begin < it.k_end) {
