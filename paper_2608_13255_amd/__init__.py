@@ -1172,10 +1172,14 @@ def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, 
     info = AttentionInfo()
     args = (ql.ctypes.data_as(_i32p), kl.ctypes.data_as(_i32p), n, int(heads), int(kv_heads), int(dim), code,
             int(bool(causal)), ctypes.byref(info))
-    _check(lib().gc_attention_plan(*args, None, 0), "gc_attention_plan")
+    host = np.empty(8192, np.int32)             # room for most plans; a longer one says how long
+    rc = lib().gc_attention_plan(*args, host.ctypes.data_as(_i32p), host.size)
     words = info.n_items * GC_ATTENTION_ITEM_WORDS
-    host = np.empty(max(1, words), np.int32)
-    _check(lib().gc_attention_plan(*args, host.ctypes.data_as(_i32p), words), "gc_attention_plan")
+    if rc == -6 and words > host.size:          # GC_ERR_CAPACITY
+        host = np.empty(words, np.int32)
+        rc = lib().gc_attention_plan(*args, host.ctypes.data_as(_i32p), host.size)
+    _check(rc, "gc_attention_plan")
+    host = host[:max(1, words)]
     s = _side_stream(stream)
     with torch.cuda.stream(s if s is not None else torch.cuda.current_stream()):
         items = torch.from_numpy(host).to(device)

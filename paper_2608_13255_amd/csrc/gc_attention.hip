@@ -5,6 +5,8 @@
 // lse = m + log l, all in float32.
 #include <algorithm>
 #include <cmath>
+#include <functional>
+#include <queue>
 #include <vector>
 
 #include "gc_attention_core.h"
@@ -43,46 +45,87 @@ void each_tile(const Batch& b, int tile, F f) {
   }
 }
 
-// Items of a variant with parts of at most `part` keys.
-int64_t items_of(const Batch& b, int tile, int part) {
-  int64_t n = 0;
-  each_tile(b, tile, [&](int s, int r, int, int, int) { n += parts_of(keys_seen(b, s, r, tile), part); });
-  return n;
+// What a variant takes, in microseconds, from timings on a full card: a block
+// alone on its compute unit goes through `rate` keys a microsecond, two that
+// share one through `share` times as many together; a block's first loads
+// and its results take kBlockTime.
+struct Cost {
+  int kind;
+  double rate, share;
+};
+constexpr double kBlockTime = 3.0;
+
+Cost cost_of(int kind, int dim, int dtype) {
+  const int padded = std::max(64, attention_padded_dim(dim));
+  if (kind == kAttnKeys) return {kind, 45.0 * 256 / (padded * dtype_bytes(dtype) / 2.0) / 2, 1.0};
+  if (dtype == GC_F32) return {kind, 14.6 * 64 / padded, padded <= 96 ? 1.3 : 1.0};
+  if (kind == kAttnRows256) return {kind, std::min(57.0, 4400.0 / padded), 1.0};
+  return {kind, std::min(85.0, 6400.0 / padded), padded <= 128 ? 1.3 : 1.0};
 }
 
-// The variant and the keys a part holds at most (what is longer is split).
+// The time of the tiles' keys in parts of at most `part`: parts are dealt, the
+// longest first, each to the compute unit with least to do (a kv head's
+// share of the units: all heads do the same), and joined in a launch of
+// its own, which takes 8 us, a quarter for each of a tile's parts, and the partial results' way out and back.
+double time_of(const std::vector<int>& tiles, int part, const Cost& c, int kv_heads, int dim) {
+  const size_t lanes = (size_t)std::max(1, kCus / kv_heads);
+  std::vector<int> pieces;
+  int64_t slots = 0;
+  int most = 1;
+  for (int keys : tiles) {
+    const int n = parts_of(keys, part);
+    for (int i = 0; i < n; ++i) pieces.push_back((keys + n - 1) / n);
+    if (n > 1) slots += n, most = std::max(most, n);
+  }
+  std::sort(pieces.begin(), pieces.end(), std::greater<int>());
+  std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
+  double last = 0;
+  for (int keys : pieces) {
+    double t = keys / c.rate + kBlockTime;
+    const bool first = busy.size() < lanes;
+    if (!first) t += busy.top(), busy.pop();
+    busy.push(t);
+    last = std::max(last, first ? t : t / c.share);
+  }
+  const double bytes = 4.0 * slots * kv_heads * attention_tile_rows(c.kind) * attention_padded_dim(dim);
+  return last + (slots ? 8.0 + 0.25 * most + 2 * bytes / 5e6 : 0.0);
+}
+
+// The variant and the keys a part holds at most (what is longer is split):
+// single tokens and other sequences of at most 32 rows share a block's
+// rows among its waves' keys; else 128 or 256 rows a block, whichever takes less time. (256 x 128:
+// 24576 tokens x 16 heads x 128 4.27 ms against 4.41 with 128 rows; not split, 2048 tokens x 16 x 64 27 us against 35 in
+// two parts; 160 rows over 9000 keys 22 us in 29 parts against 150 whole.)
 void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
-  int64_t most_rows = 0, tiles256 = 0;
-  for (int s = 0; s < b.n_seq; ++s) {
-    const int64_t rows = (int64_t)b.q_lens[s] * b.group;
-    most_rows = std::max(most_rows, rows);
-    tiles256 += (rows + 255) / 256;
+  int64_t most_rows = 0;
+  for (int s = 0; s < b.n_seq; ++s) most_rows = std::max(most_rows, (int64_t)b.q_lens[s] * b.group);
+  double best = 0;
+  *part = 0x7fffffc0;
+  *kind = most_rows <= 32 ? kAttnKeys : kAttnRows128;
+  for (int k = 0; k < kAttnKinds; ++k) {
+    if ((k == kAttnKeys) != (most_rows <= 32) || (k == kAttnRows256 && !attention_has_rows256(dim, dtype))) continue;
+    const Cost c = cost_of(k, dim, dtype);
+    const int tile = attention_tile_rows(k);
+    std::vector<int> tiles;
+    int64_t work = 0;
+    int most = 0;
+    each_tile(b, tile, [&](int s, int r, int, int, int) {
+      const int n = keys_seen(b, s, r, tile);
+      tiles.push_back(n), work += n, most = std::max(most, n);
+    });
+    const int64_t lanes = std::max(1, kCus / b.kv_heads);
+    // many rounds of whole tiles are even enough: only their sum counts
+    const bool many = (int64_t)tiles.size() >= 16 * lanes;
+    const double whole = many ? (work / c.rate + tiles.size() * kBlockTime) / lanes / c.share : time_of(tiles, 0x7fffffc0, c, b.kv_heads, dim);
+    if (best == 0 || whole < best) best = whole, *kind = k, *part = 0x7fffffc0;
+    if (many || most <= kPartKeys) continue;
+    for (const double rounds : {0.5, 0.75, 0.9, 1.0, 1.1, 1.25, 1.5, 1.75, 2.0, 2.5, 3.0, 4.0}) {
+      const int64_t keys = ((int64_t)((double)work / lanes / rounds) / kPartKeys + 1) * kPartKeys;
+      if (keys >= most) continue;
+      const double t = time_of(tiles, (int)keys, c, b.kv_heads, dim);
+      if (t < best) best = t, *kind = k, *part = (int)keys;
+    }
   }
-  if (most_rows <= 32) *kind = kAttnKeys;
-  // Tiles of 256 rows read keys and values half as often (24576 x 16 x 128: 4.27 ms against 4.41 with tiles of 128); those of
-  // 128 are evener where few rounds of blocks fill the card, and mask less under a causal mask (packed prompts: 709 us
-  // against 721).
-  else *kind = attention_has_rows256(dim, dtype) && !b.causal && tiles256 * b.kv_heads >= 2 * kCus ? kAttnRows256 : kAttnRows128;
-  // the blocks that the card holds at once
-  const int64_t blocks = *kind == kAttnKeys ? kCus * attention_keys_blocks(dim, dtype) : *kind == kAttnRows256 ? kCus : 2 * kCus;
-  const int tile = attention_tile_rows(*kind);
-  int64_t work = 0, most = 0;
-  each_tile(b, tile, [&](int s, int r, int, int, int) {
-    const int64_t n = keys_seen(b, s, r, tile);
-    work += n, most = std::max(most, n);
-  });
-  // The shortest parts with which all blocks are there at once, so that they end together, but none shorter than pays for
-  // joining it: 512 keys of bfloat16 (1024 tokens x 16 heads x 64: 19.2 us against 22.5 with 256), 256 of float, whose
-  // products take longer, and of single tokens (8 x 1000 keys: 14.3 us against 16.4 with 512).
-  const int64_t least = *kind == kAttnKeys || dtype == GC_F32 ? 256 : 512;
-  int64_t low = std::max<int64_t>(work * b.kv_heads / blocks + 1, least), high = std::max(low, most);
-  while (low < high) {
-    const int64_t mid = (low + high) / 2;
-    if (items_of(b, tile, (int)mid) * b.kv_heads <= blocks) high = mid;
-    else low = mid + 1;
-  }
-  low = (low + kPartKeys - 1) / kPartKeys * kPartKeys;
-  *part = (int)std::min<int64_t>(low, 0x7fffffc0);
 }
 
 }  // namespace
