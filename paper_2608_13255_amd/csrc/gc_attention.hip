@@ -162,7 +162,7 @@ extern "C" int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, i
     n_items += n;
     if (n > 1) n_slots += n, ++n_groups;
   });
-  if (n_items * kv_heads > 0x7fffffffLL) return fail(GC_ERR_CAPACITY, "%s: over 2^31-1 blocks", who);
+  if (n_items > 0x7fffffffLL) return fail(GC_ERR_CAPACITY, "%s: over 2^31-1 items", who);
   std::memset(info, 0, sizeof(*info));
   info->heads = heads, info->kv_heads = kv_heads, info->dim = dim, info->dtype = dtype, info->causal = causal != 0;
   info->n_seq = n_seq, info->total_q = (int32_t)total_q, info->total_k = (int32_t)total_k;
@@ -246,15 +246,21 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
   }
   p.out = out->data, p.o_token = out->token_stride, p.o_head = out->head_stride;
   p.lse = lse;
-  p.items = reinterpret_cast<const AttentionItem*>(items);
   p.heads = info->heads, p.kv_heads = info->kv_heads, p.group = info->heads / info->kv_heads, p.dim = dim;
   p.total_q = info->total_q, p.total_k = info->total_k;
   p.causal = info->causal;
   p.scale = (float)scale;
   if (info->n_slots > 0) p.partial = reinterpret_cast<float*>(workspace);
-  const unsigned blocks = (unsigned)(info->n_items * info->kv_heads);
-  const bool known = dtype == GC_F32 ? launch_attention_f32(p, info->kind, blocks, stream)
-                                     : launch_attention_bf16(p, info->kind, blocks, stream);
-  if (!known) return fail(GC_ERR_SHAPE, "%s: no kernel for dim=%d", who, dim);
+  const int most = std::max(1, kMostBlocks / info->kv_heads);
+  for (const bool join : {false, true}) {
+    if (join && !p.partial) break;
+    for (int i = 0; i < info->n_items; i += std::min(most, info->n_items - i)) {
+      p.items = reinterpret_cast<const AttentionItem*>(items) + i;
+      const unsigned blocks = (unsigned)(std::min(most, info->n_items - i) * info->kv_heads);
+      const bool known = dtype == GC_F32 ? launch_attention_f32(p, info->kind, join, blocks, stream)
+                                         : launch_attention_bf16(p, info->kind, join, blocks, stream);
+      if (!known) return fail(GC_ERR_SHAPE, "%s: no kernel for dim=%d", who, dim);
+    }
+  }
   return after_launch(stream, who);
 }

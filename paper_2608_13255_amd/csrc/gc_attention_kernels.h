@@ -141,9 +141,8 @@ __global__ __launch_bounds__(kJoin) void k_attention_join(const AttentionArgs p,
 
 template <class T, int kDim>
 void launch_join(const AttentionArgs& p, int tile_rows, unsigned blocks, hipStream_t stream) {
-  if (p.partial)
-    hipLaunchKernelGGL((k_attention_join<T, kDim>), dim3(blocks, (unsigned)(tile_rows * (kDim / 4) / kJoin)), dim3(kJoin), 0, stream,
-                       p, tile_rows);
+  hipLaunchKernelGGL((k_attention_join<T, kDim>), dim3(blocks, (unsigned)(tile_rows * (kDim / 4) / kJoin)), dim3(kJoin), 0, stream, p,
+                     tile_rows);
 }
 
 // ---------------------------------------------------------------------------

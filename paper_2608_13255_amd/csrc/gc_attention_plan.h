@@ -48,8 +48,11 @@ inline int attention_keys_blocks(int dim, int dtype) {
 }
 
 struct AttentionArgs;
-// Launches of one storage type (false: no such variant).
-bool launch_attention_bf16(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream);
-bool launch_attention_f32(const AttentionArgs& p, int kind, unsigned blocks, hipStream_t stream);
+// Blocks of a launch: its threads (at most 512 a block) are counted in 32 bits.
+constexpr int kMostBlocks = 1 << 22;
+// Launches of one storage type: the items' results, or (join) those of split rows from their parts.
+// false: no such variant.
+bool launch_attention_bf16(const AttentionArgs& p, int kind, bool join, unsigned blocks, hipStream_t stream);
+bool launch_attention_f32(const AttentionArgs& p, int kind, bool join, unsigned blocks, hipStream_t stream);
 
 }  // namespace gc

@@ -306,7 +306,6 @@ void launch_v(RopeArgs& p, int layout, hipStream_t stream) {
   const auto groups = [&](int heads) { return (int64_t)((total + (heads << p.slots_log2) - 1) / (heads << p.slots_log2)); };
   const bool many = sets * groups(4) >= 32 * 256;
   p.head_groups = (uint32_t)groups(many ? 4 : 1);
-  const dim3 grid((unsigned)((sets * p.head_groups + kBlock / 64 - 1) / (kBlock / 64)));
   bool whole = true;
   const int run = layout == GC_ROPE_HALF ? V : V / 2;   // columns that a lane takes from one row
   for (int a = 0; a < p.sec.n; ++a) whole = whole && p.sec.end[a] % run == 0;
@@ -316,13 +315,28 @@ void launch_v(RopeArgs& p, int layout, hipStream_t stream) {
   const int rest = p.dim / 2 - p.half;
   const bool once = 2 * p.n_tokens * total * p.dim * (int64_t)sizeof(T) >= kOnceBytes &&
                     p.half * (int)sizeof(T) % 128 == 0 && rest * (int)sizeof(T) % 128 == 0;
-  const auto go = [&](auto half, auto all, auto past) {
+  const auto launch_one = [&](auto half, auto all, auto past, dim3 grid) {
     if (many)
       hipLaunchKernelGGL((k_rope<T, V, 4, decltype(half)::value, kNorm, decltype(all)::value, decltype(past)::value>), grid,
                          dim3(kBlock), 0, stream, p);
     else
       hipLaunchKernelGGL((k_rope<T, V, 1, decltype(half)::value, kNorm, decltype(all)::value, false>), grid, dim3(kBlock), 0,
                          stream, p);
+  };
+  // a launch's threads are counted in 32 bits: at most 2^25 waves at a time
+  const int64_t most = ((int64_t)1 << 25) / p.head_groups << token_sets_log2, n_tokens = p.n_tokens;
+  const auto go = [&](auto half, auto all, auto past) {
+    for (int64_t done = 0; done < n_tokens; done += most) {
+      p.n_tokens = n_tokens - done < most ? n_tokens - done : most;
+      const int64_t waves = ((p.n_tokens + (1 << token_sets_log2) - 1) >> token_sets_log2) * p.head_groups;
+      launch_one(half, all, past, dim3((unsigned)((waves + kBlock / 64 - 1) / (kBlock / 64))));
+      p.positions += p.n_tokens * p.sec.n;
+      for (int i = 0; i < 2; ++i) {
+        if (p.heads[i] == 0) continue;
+        p.in[i] = (const T*)p.in[i] + p.n_tokens * p.in_token[i];
+        p.out[i] = (T*)p.out[i] + p.n_tokens * p.out_token[i];
+      }
+    }
   };
   const auto with = [&](auto half, auto all) { once ? go(half, all, std::true_type{}) : go(half, all, std::false_type{}); };
   const auto axes = [&](auto half) { whole ? with(half, std::true_type{}) : with(half, std::false_type{}); };

@@ -339,3 +339,12 @@ def test_graph_replays(gc, dtype):
         torch.cuda.synchronize()
         want = gc.gc_attention(*fresh, plan)
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_more_blocks_than_a_launch_has_threads_for(gc):
+    """600000 sequences of one token and one key: every result is its value, past the first launch's too."""
+    n, H, D = 600000, 16, 32
+    g = gen(41)
+    q, k, v = (torch.randn((n, H, D), generator=g, device=DEV).bfloat16() for _ in range(3))
+    plan = gc.gc_attention_plan([1] * n, [1] * n, H, H, D, torch.bfloat16, causal=True, device=DEV)
+    assert torch.equal(gc.gc_attention(q, k, v, plan)[0], v)

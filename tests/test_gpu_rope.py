@@ -221,3 +221,17 @@ def test_offsets_past_32_bits(gc):
     assert torch.equal(gc.gc_rope(view, pos, table), want)
     gc.gc_rope(view, pos, table, out=view)
     assert torch.equal(view, want)
+
+
+def test_more_tokens_than_a_launch_has_threads_for(gc):
+    """2^25 + 40 heads of 64 lanes each: over 2^31 threads, tokens past the first launch's among them."""
+    T, D = (1 << 25) + 40, 256
+    x = torch.zeros((T, 1, D), dtype=torch.bfloat16, device=DEV)
+    rows = torch.tensor([0, 1, T // 2, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, T - 1], device=DEV)
+    x[rows] = torch.randn((rows.numel(), 1, D), generator=gen(11), device=DEV).bfloat16()
+    pos = torch.arange(T, device=DEV).remainder_(64).int()
+    table = table_for(gc, 64, [2])
+    want = gc.gc_rope(x[rows], pos[rows].contiguous(), table)
+    gc.gc_rope(x, pos, table, out=x)
+    assert torch.equal(x[rows], want)
+    assert int(torch.count_nonzero(x.view(T, D).any(dim=1))) == rows.numel()
