@@ -728,7 +728,7 @@ int gc_qk_norm_rope(const gc_heads* q, int heads, const gc_heads* k, int kv_head
  *   lse      device float [heads][sum of q_lens], or NULL
  *   info     host, as gc_attention_plan filled it
  *   items    device int32, a copy of the plan's items, 16-byte aligned
- *   scale    finite, > 0
+ *   scale    finite and > 0, as a float32 too
  *   workspace  device, info->workspace_bytes, 16-byte aligned; its contents
  *            are of no consequence.  Calls in flight at the same time need
  *            workspaces of their own.  May be NULL if info->workspace_bytes

@@ -204,7 +204,9 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
       info->n_items < 0 || info->total_q < 0 || info->total_k < 0 || info->n_slots < 0 || info->n_groups < 0 ||
       info->workspace_bytes < (int64_t)info->n_slots * info->kv_heads * info->tile_rows * (attention_padded_dim(info->dim) + 2) * 4)
     return fail(GC_ERR_ARG, "%s: info is not gc_attention_plan's", who);
-  if (!(scale > 0.0) || !std::isfinite(scale)) return fail(GC_ERR_ARG, "%s: scale must be finite and above 0", who);
+  // (a scale that is 0 in float32 would make the masked scores' -inf NaN)
+  if (!((float)scale > 0.f) || !std::isfinite((float)scale * kLog2e))
+    return fail(GC_ERR_ARG, "%s: scale=%g must be finite and above 0 in float32", who, scale);
   if (info->n_items == 0) return GC_OK;
   if (!items) return fail(GC_ERR_ARG, "%s: items is null", who);
   if (!aligned16(items) || (reinterpret_cast<uintptr_t>(lse) & 3) || (workspace && !aligned16(workspace)))

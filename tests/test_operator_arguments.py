@@ -270,3 +270,22 @@ def test_binding_refusals(gc):
         gc.gc_attention_plan([-1], [1], 2, 2, 64, torch.float32, device="cpu")
     with pytest.raises(gc.GeoCacheError, match="multiple"):
         gc.gc_attention_plan([1], [1], 3, 2, 64, torch.float32, device="cpu")
+
+
+def test_attention_scale_in_float32(gc, L):
+    """A scale that float32 rounds to 0 or to infinity is refused: -inf (a masked score) times 0 is NaN."""
+    info = gc.AttentionInfo()
+    assert L.gc_attention_plan(i32(40), i32(90), 1, 4, 2, 64, 1, 0, ctypes.byref(info), None, 0) == 0
+    t = [heads(gc, A[0]), heads(gc, A[1], n=2), heads(gc, A[2], n=2), heads(gc, A[3])]
+    for scale in (1e-60, 5e-324, 3e38, 1e39, 1e300):
+        refused(L, L.gc_attention(*map(ctypes.byref, t), A[4], ctypes.byref(info), A[5], scale, A[6], 1 << 40, None), "ARG", "scale")
+
+
+def test_attention_tokens_that_share_memory(gc, L):
+    info = gc.AttentionInfo()
+    assert L.gc_attention_plan(i32(40), i32(90), 1, 4, 2, 64, 1, 0, ctypes.byref(info), None, 0) == 0
+    for name in "kv":
+        t = dict(q=heads(gc, A[0]), k=heads(gc, A[1], n=2), v=heads(gc, A[2], n=2), o=heads(gc, A[3]))
+        t[name].token_stride = 56
+        refused(L, L.gc_attention(*(ctypes.byref(t[n]) for n in "qkvo"), A[4], ctypes.byref(info), A[5], 0.125, A[6], 1 << 40, None),
+                "SHAPE", "token strides of k and v")
