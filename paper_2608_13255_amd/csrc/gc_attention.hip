@@ -2,7 +2,20 @@
 //
 // For each query row, over the keys it sees: s_j = scale q.k_j, the running
 // maximum m and sum l of exp(s_j - m), out = sum exp(s_j - m) v_j / l and
-// lse = m + log l, all in float32.
+// lse = m + log l, all in float32 (bfloat16 heads: the weights are rounded to
+// bfloat16 for the second product, and the results on their way out).
+//
+// A call cannot do without reading q, k and v and writing out once, and 4 dim
+// operations a head and visible pair: single tokens are bound by the read,
+// everything else by the operations.  Measured, us, with the time of the
+// bound at a large read's 7.0 TB/s or a large product's 1378 (bfloat16) and
+// 153 (float32) TFLOP/s:
+//   8 single tokens, 32 heads on 8 of 128, 495 MB of keys and values     90   71
+//   1024 + 1 + 517 + 770 tokens, 8 heads of 64, float32                  51   25
+//   10403 tokens in 4 sequences, 16 heads of 64, among themselves       152   83
+//   the same over 31070 keys, 16 heads of 80 (worked on as 96)          509  308
+//   15427 causal tokens in 7 sequences, 32 heads on 8 of 128            707  527
+//   24576 tokens, 16 heads of 128                                      4270 3592
 #include <algorithm>
 #include <cmath>
 #include <functional>
@@ -16,7 +29,7 @@ namespace {
 
 // Keys per part: a multiple of every variant's tile.
 constexpr int kPartKeys = 64;
-// Blocks to fill the card with: one for each of 256 compute units, two of the smaller ones.
+// Compute units.
 constexpr int kCus = 256;
 
 struct Batch {
@@ -93,9 +106,13 @@ double time_of(const std::vector<int>& tiles, int part, const Cost& c, int kv_he
 
 // The variant and the keys a part holds at most (what is longer is split):
 // single tokens and other sequences of at most 32 rows share a block's
-// rows among its waves' keys; else 128 or 256 rows a block, whichever takes less time. (256 x 128:
-// 24576 tokens x 16 heads x 128 4.27 ms against 4.41 with 128 rows; not split, 2048 tokens x 16 x 64 27 us against 35 in
-// two parts; 160 rows over 9000 keys 22 us in 29 parts against 150 whole.)
+// rows among its waves' keys; else 128 or 256 rows a block, whichever takes
+// less time.  256 rows read each tile of keys half as often, 128 leave less
+// over at a sequence's and at the launch's end.  256 against 128: 24576 tokens
+// x 16 heads x 128 4.34 ms and 4.54, 16384 causal x 8 x 128 530 us and 562,
+// 4096 x 16 x 64 83 and 89; 2048 x 16 x 64 36 and 27, 6000 x 12 x 96 228 and
+// 219, 4096 causal x 8 x 128 64 and 60.  Parts: 160 rows over 9000 keys 22 us
+// in 29 against 150 whole; 2048 x 16 x 64 27 whole against 35 in two.
 void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
   int64_t most_rows = 0;
   for (int s = 0; s < b.n_seq; ++s) most_rows = std::max(most_rows, (int64_t)b.q_lens[s] * b.group);

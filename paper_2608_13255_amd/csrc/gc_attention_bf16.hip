@@ -12,11 +12,11 @@ void launch(const AttentionArgs& p, int kind, bool join, unsigned blocks, hipStr
   constexpr int kBlocks = kDim <= 96 ? 2 : 1, kPerSimd = kDim <= 128 ? 2 : 1;
   if constexpr (kDim <= 128) {
     if (kind == kAttnRows256) {
-      hipLaunchKernelGGL((k_attention_rows<kDim, 1, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);
+      hipLaunchKernelGGL((k_attention_rows<kDim, kBlocks, 8, 2>), dim3(blocks), dim3(512), 0, stream, p);
     }
   }
   if (kind == kAttnKeys) hipLaunchKernelGGL((k_attention_keys<uint16_t, kDim, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, stream, p);
-  else if (kind == kAttnRows128) hipLaunchKernelGGL((k_attention_rows<kDim, 1, kBlocks, 4, kPerSimd>), dim3(blocks), dim3(256), 0, stream, p);
+  else if (kind == kAttnRows128) hipLaunchKernelGGL((k_attention_rows<kDim, kBlocks, 4, kPerSimd>), dim3(blocks), dim3(256), 0, stream, p);
 }
 
 }  // namespace

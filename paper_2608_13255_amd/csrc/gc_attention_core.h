@@ -8,6 +8,12 @@
 // (h = lane / 32) is row 8 (i / 4) + 4 h + i % 4; the order of the keys inside
 // a product is free, so the values are read in the order in which the weights lie.
 //
+// Why 32 x 32 blocks: an operand read from LDS feeds 32 x 32 x 16 products,
+// half the LDS traffic of 16 x 16 blocks; with 32 rows a wave holds 64 keys'
+// scores twice (or 32 of 128 channels) beside the output within the 256
+// registers of two waves a SIMD.  64 rows a wave would halve the LDS reads
+// again but spill (8.8 ms where 32 rows take 4.3).
+//
 // K and V tiles lie in LDS as rows of 16-byte chunks, chunk c of row r at
 // place c ^ f(r): with f below, 16 rows' same chunk lie in 16 different
 // places of the 256 bytes that the banks span, and so do four rows' same
@@ -138,58 +144,55 @@ __device__ __forceinline__ RowOf row_of(const AttentionArgs& p, const AttentionI
 // ---------------------------------------------------------------------------
 // bfloat16
 // ---------------------------------------------------------------------------
-// What one wave holds: the queries of kNq blocks of 32 rows (an operand of
+// What one wave holds: the queries of 32 rows (an operand of
 // S^T), O^T, and the rows' maximum in use and sum.  A tile is kKeyBlocks * 32
 // keys.
-template <class T, int kDim, int kNq, int kKeyBlocks>
+template <class T, int kDim, int kKeyBlocks>
 struct Core;
 
-// S^T: key 32 b + 8 (i / 4) + 4 half + i % 4 of row block n
-template <int kNq, int kKeyBlocks>
+// S^T: key 32 b + 8 (i / 4) + 4 half + i % 4
+template <int kKeyBlocks>
 struct Scores {
-  f32x16 s[kNq][kKeyBlocks];
+  f32x16 s[kKeyBlocks];
 };
 
-template <int kNq, int kOut>
+template <int kOut>
 struct Accumulators {
-  f32x16 o[kNq][kOut];
-  float m[kNq], l[kNq];   // maximum in use (score times scale times log2 e) and this lane's part of the sum
+  f32x16 o[kOut];
+  float m, l;   // maximum in use (score times scale times log2 e) and this lane's part of the sum
   __device__ __forceinline__ void init() {
 #pragma unroll
-    for (int n = 0; n < kNq; ++n) {
+    for (int d = 0; d < kOut; ++d)
 #pragma unroll
-      for (int d = 0; d < kOut; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[n][d][i] = 0.f;
-      m[n] = -__builtin_inff();
-      l[n] = 0.f;
-    }
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    m = -__builtin_inff();
+    l = 0.f;
   }
 };
 
-template <int kDim, int kNq, int kKeyBlocks>
-struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
+template <int kDim, int kKeyBlocks>
+struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
   static constexpr int kChunks = kDim / 8, kSteps = kDim / 16, kOut = kDim / 32;
-  // operands of the scores and of the output, kNq products each
+  // operands of the scores and of the output, a product each
   static constexpr int kOperands = kKeyBlocks * kSteps, kAhead = kOperands < 4 ? kOperands : 4;
   static_assert(kOperands == 2 * kKeyBlocks * kOut, "as many of either kind");
-  using Accumulators<kNq, kOut>::o;
-  using Accumulators<kNq, kOut>::l;
-  using S = Scores<kNq, kKeyBlocks>;
-  bf16x8 q[kNq][kSteps];
+  using Accumulators<kOut>::o;
+  using Accumulators<kOut>::l;
+  using S = Scores<kKeyBlocks>;
+  bf16x8 q[kSteps];
 
   // Weights as an operand of O^T = V^T P^T: element j of group g is key 16 g + 8 (j / 4) + 4 half + j % 4.  Rounded to
   // bfloat16, the type that the matrix units take; the sum l is of the unrounded ones.
   struct Weights {
-    bf16x8 w[kNq][2 * kKeyBlocks];
+    bf16x8 w[2 * kKeyBlocks];
   };
 
-  __device__ __forceinline__ void load_q(int n, const uint16_t* row, int dim, int half) {
+  __device__ __forceinline__ void load_q(const uint16_t* row, int dim, int half) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       u32x4 w = {0u, 0u, 0u, 0u};
       if ((2 * s + half) * 8 < dim) w = *reinterpret_cast<const u32x4*>(row + (2 * s + half) * 8);
-      q[n][s] = __builtin_bit_cast(bf16x8, w);
+      q[s] = __builtin_bit_cast(bf16x8, w);
     }
   }
 
@@ -199,17 +202,13 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
     return *reinterpret_cast<const bf16x8*>(kt + place<kChunks>(row, 2 * (i / kKeyBlocks) + (lane >> 5)));
   }
   __device__ __forceinline__ void score(S& s, bf16x8 k, int i) const {
-#pragma unroll
-    for (int n = 0; n < kNq; ++n)
-      s.s[n][i % kKeyBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[n][i / kKeyBlocks], s.s[n][i % kKeyBlocks], 0, 0, 0);
+      s.s[i % kKeyBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i / kKeyBlocks], s.s[i % kKeyBlocks], 0, 0, 0);
   }
   __device__ __forceinline__ static void clear(S& s) {
 #pragma unroll
-    for (int n = 0; n < kNq; ++n)
-#pragma unroll
       for (int b = 0; b < kKeyBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s.s[n][b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) s.s[b][i] = 0.f;
   }
   __device__ __forceinline__ void scores(const char* kt, int lane, S& s) const {
     clear(s);
@@ -234,9 +233,7 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
     return w;
   }
   __device__ __forceinline__ void add(const Weights& w, u32x4 v, int i) {
-#pragma unroll
-    for (int n = 0; n < kNq; ++n)
-      o[n][i % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w.w[n][i / kOut], o[n][i % kOut], 0, 0, 0);
+      o[i % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w.w[i / kOut], o[i % kOut], 0, 0, 0);
   }
 
   // Two values with those that are not finite replaced by zeros.
@@ -268,20 +265,16 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
     for (int i = 0; i < kOperands; ++i) add(w, values(vt, lane, i), i);
   }
 
-  // Weight e of row block n.
-  __device__ __forceinline__ void weight(const S& s, float c, float ms, Weights& w, int n, int e, float& sum) const {
-    const float x = exp2_hw(__builtin_fmaf(s.s[n][e / 16][e % 16], c, -ms));
+  __device__ __forceinline__ void weight(const S& s, float c, float ms, Weights& w, int e, float& sum) const {
+    const float x = exp2_hw(__builtin_fmaf(s.s[e / 16][e % 16], c, -ms));
     sum += x;
-    w.w[n][e / 8][e % 8] = (__bf16)x;
+    w.w[e / 8][e % 8] = (__bf16)x;
   }
-  __device__ __forceinline__ void weights(const S& s, float c, const float (&ms)[kNq], Weights& w) {
+  __device__ __forceinline__ void weights(const S& s, float c, float ms, Weights& w) {
+    float sum = 0.f;
 #pragma unroll
-    for (int n = 0; n < kNq; ++n) {
-      float sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16 * kKeyBlocks; ++e) weight(s, c, ms[n], w, n, e, sum);
-      l[n] += sum;
-    }
+    for (int e = 0; e < 16 * kKeyBlocks; ++e) weight(s, c, ms, w, e, sum);
+    l += sum;
   }
 
   // The two parts of a tile's work when nothing is masked.  Each runs matrix
@@ -299,47 +292,41 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
 
   // the values of the tile before, and this tile's largest scores (of this lane's)
   __device__ __forceinline__ void values_and_maximum(Operands& x, const char* vt, const Weights& w, const S& s, const char* kt,
-                                                     int lane, float (&mx)[kNq]) {
+                                                     int lane, float& mx) {
     u32x4 v[kOperands];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) v[i] = x.v[i];
-    constexpr int kSteps2 = 8 * kKeyBlocks * kNq;   // two scores a step
-#pragma unroll
-    for (int n = 0; n < kNq; ++n) mx[n] = s.s[n][0][0];
+    constexpr int kPairs = 8 * kKeyBlocks;   // of scores
+    mx = s.s[0][0];
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
       if (i + kAhead < kOperands) v[i + kAhead] = values(vt, lane, i + kAhead);
       else x.k[i + kAhead - kOperands] = keys(kt, lane, i + kAhead - kOperands);
       add(w, v[i], i);
 #pragma unroll
-      for (int e = i * kSteps2 / kOperands; e < (i + 1) * kSteps2 / kOperands; ++e) {
-        const int n = e % kNq, y = 2 * (e / kNq);
-        mx[n] = fmaxf(fmaxf(mx[n], s.s[n][y / 16][y % 16]), s.s[n][y / 16][y % 16 + 1]);
+      for (int e = i * kPairs / kOperands; e < (i + 1) * kPairs / kOperands; ++e) {
+        const int y = 2 * e;
+        mx = fmaxf(fmaxf(mx, s.s[y / 16][y % 16]), s.s[y / 16][y % 16 + 1]);
       }
     }
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
       if (i + kAhead < kOperands) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
       else __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-#pragma unroll
-      for (int n = 0; n < kNq; ++n) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, (8 * kKeyBlocks + kOperands - 1) / kOperands, 0);
-      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, (8 * kKeyBlocks + kOperands - 1) / kOperands, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
 
   // this tile's weights, and the next tile's scores
-  __device__ __forceinline__ void weights_and_scores(Operands& x, const S& s, float c, const float (&ms)[kNq], Weights& w,
+  __device__ __forceinline__ void weights_and_scores(Operands& x, const S& s, float c, float ms, Weights& w,
                                                      const char* kt, S& next, const char* vt, int lane) {
     bf16x8 k[kOperands];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) k[i] = x.k[i];
-    constexpr int kWeights = 16 * kKeyBlocks * kNq;
-    float sum[kNq];
-#pragma unroll
-    for (int n = 0; n < kNq; ++n) sum[n] = 0.f;
+    constexpr int kWeights = 16 * kKeyBlocks;
+    float sum = 0.f;
     clear(next);
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
@@ -348,24 +335,18 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
       score(next, k[i], i);
 #pragma unroll
       for (int e = i * kWeights / kOperands; e < (i + 1) * kWeights / kOperands; ++e)
-        weight(s, c, ms[e / (16 * kKeyBlocks)], w, e / (16 * kKeyBlocks), e % (16 * kKeyBlocks), sum[e / (16 * kKeyBlocks)]);
+        weight(s, c, ms, w, e, sum);
     }
+    l += sum;
+    // here and not where they are used, in the next part
 #pragma unroll
-    for (int n = 0; n < kNq; ++n) {
-      l[n] += sum[n];
-      // here and not where they are used, in the next part
-#pragma unroll
-      for (int g = 0; g < 2 * kKeyBlocks; ++g) asm volatile("" : "+v"(w.w[n][g]));
-    }
+    for (int g = 0; g < 2 * kKeyBlocks; ++g) asm volatile("" : "+v"(w.w[g]));
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
       if (i + kAhead < kOperands) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-      for (int n = 0; n < kNq; ++n) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, 7 * 8 * kKeyBlocks / kOperands, 0);
-      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 7 * 8 * kKeyBlocks / kOperands, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -374,34 +355,32 @@ struct Core<uint16_t, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
 // ---------------------------------------------------------------------------
 // float32
 // ---------------------------------------------------------------------------
-template <int kDim, int kNq, int kKeyBlocks>
-struct Core<float, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
+template <int kDim, int kKeyBlocks>
+struct Core<float, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
   static constexpr int kChunks = kDim / 4, kSteps = kDim / 8, kOut = kDim / 32;
-  using Accumulators<kNq, kOut>::o;
-  using Accumulators<kNq, kOut>::l;
-  using S = Scores<kNq, kKeyBlocks>;
-  f32x4 q[kNq][kSteps];
+  using Accumulators<kOut>::o;
+  using Accumulators<kOut>::l;
+  using S = Scores<kKeyBlocks>;
+  f32x4 q[kSteps];
 
   struct Weights {
-    f32x16 w[kNq][kKeyBlocks];   // in the scores' order, a key a product
+    f32x16 w[kKeyBlocks];   // in the scores' order, a key a product
   };
 
-  __device__ __forceinline__ void load_q(int n, const float* row, int dim, int half) {
+  __device__ __forceinline__ void load_q(const float* row, int dim, int half) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      q[n][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if ((2 * s + half) * 4 < dim) q[n][s] = *reinterpret_cast<const f32x4*>(row + (2 * s + half) * 4);
+      q[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if ((2 * s + half) * 4 < dim) q[s] = *reinterpret_cast<const f32x4*>(row + (2 * s + half) * 4);
     }
   }
 
   // A lane's chunk holds channels 8 t + 4 half + j: product j of step t takes channels 8 t + j and 8 t + 4 + j.
   __device__ __forceinline__ void scores(const char* kt, int lane, S& s) const {
 #pragma unroll
-    for (int n = 0; n < kNq; ++n)
-#pragma unroll
       for (int b = 0; b < kKeyBlocks; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s.s[n][b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) s.s[b][i] = 0.f;
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
@@ -409,24 +388,20 @@ struct Core<float, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
         const f32x4 k = *reinterpret_cast<const f32x4*>(kt + place<kChunks>(b * 32 + (lane & 31), 2 * t + (lane >> 5)));
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int n = 0; n < kNq; ++n) s.s[n][b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j], q[n][t][j], s.s[n][b], 0, 0, 0);
+          s.s[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k[j], q[t][j], s.s[b], 0, 0, 0);
       }
   }
 
-  __device__ __forceinline__ void weights(const S& s, float c, const float (&ms)[kNq], Weights& w) {
+  __device__ __forceinline__ void weights(const S& s, float c, float ms, Weights& w) {
+    float sum = 0.f;
 #pragma unroll
-    for (int n = 0; n < kNq; ++n) {
-      float sum = 0.f;
+    for (int b = 0; b < kKeyBlocks; ++b)
 #pragma unroll
-      for (int b = 0; b < kKeyBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          w.w[n][b][i] = exp2_hw(__builtin_fmaf(s.s[n][b][i], c, -ms[n]));
-          sum += w.w[n][b][i];
-        }
-      l[n] += sum;
-    }
+      for (int i = 0; i < 16; ++i) {
+        w.w[b][i] = exp2_hw(__builtin_fmaf(s.s[b][i], c, -ms));
+        sum += w.w[b][i];
+      }
+    l += sum;
   }
 
   // channel 32 d + lane % 32 of key 32 b + 8 (i / 4) + 4 half + i % 4
@@ -451,8 +426,7 @@ struct Core<float, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
             bad |= !fin;
             v = fin ? v : 0.f;
           }
-#pragma unroll
-          for (int n = 0; n < kNq; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.w[n][b][i], o[n][d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, w.w[b][i], o[d], 0, 0, 0);
         }
     return bad;
   }
@@ -463,9 +437,9 @@ struct Core<float, kDim, kNq, kKeyBlocks> : Accumulators<kNq, kDim / 32> {
 // The values that add_masked left out, for the rows that see them: a
 // positive weight times NaN or infinity is that value.  Keys [first, end),
 // of which `keys` of every `step` are this wave's.
-template <class T, class C, int kNq>
+template <class T, class C>
 __device__ __forceinline__ void add_nonfinite(const AttentionArgs& p, const AttentionItem& it, int kv_head, C& core, int first,
-                                              int end, int keys, int step, const int (&limit)[kNq], int lane) {
+                                              int end, int keys, int step, int limit, int lane) {
   for (int key0 = first; key0 < end; key0 += step)
     for (int key = key0; key < key0 + keys && key < end; ++key) {
       const T* row = (const T*)p.v + ((int64_t)it.k_token0 + key) * p.v_token + kv_head * p.v_head;
@@ -477,33 +451,26 @@ __device__ __forceinline__ void add_nonfinite(const AttentionArgs& p, const Atte
           float x[4] = {0.f, 0.f, 0.f, 0.f};
           if (c < p.dim) load_heads<4>(row + c, x);
 #pragma unroll
-          for (int n = 0; n < kNq; ++n)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) core.o[n][d][4 * g + j] += key < limit[n] && !finite_f(x[j]) ? x[j] : 0.f;
+            for (int j = 0; j < 4; ++j) core.o[d][4 * g + j] += key < limit && !finite_f(x[j]) ? x[j] : 0.f;
         }
     }
 }
 
 // Masked places' scores.
-template <int kNq, int kKeyBlocks>
-__device__ __forceinline__ void mask(Scores<kNq, kKeyBlocks>& s, int key0, const int (&limit)[kNq], int lane) {
-#pragma unroll
-  for (int n = 0; n < kNq; ++n)
+template <int kKeyBlocks>
+__device__ __forceinline__ void mask(Scores<kKeyBlocks>& s, int key0, int limit, int lane) {
 #pragma unroll
     for (int b = 0; b < kKeyBlocks; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (key0 + 32 * b + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= limit[n]) s.s[n][b][i] = -__builtin_inff();
+        if (key0 + 32 * b + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= limit) s.s[b][i] = -__builtin_inff();
 }
 
-template <int kNq, int kKeyBlocks>
-__device__ __forceinline__ void maximum(const Scores<kNq, kKeyBlocks>& s, float (&mx)[kNq]) {
+template <int kKeyBlocks>
+__device__ __forceinline__ void maximum(const Scores<kKeyBlocks>& s, float& mx) {
+  mx = s.s[0][0];
 #pragma unroll
-  for (int n = 0; n < kNq; ++n) {
-    mx[n] = s.s[n][0][0];
-#pragma unroll
-    for (int e = 1; e < 16 * kKeyBlocks; ++e) mx[n] = fmaxf(mx[n], s.s[n][e / 16][e % 16]);
-  }
+  for (int e = 1; e < 16 * kKeyBlocks; ++e) mx = fmaxf(mx, s.s[e / 16][e % 16]);
 }
 
 // The running maximum.  The one in use follows the true one only where that
@@ -512,39 +479,24 @@ __device__ __forceinline__ void maximum(const Scores<kNq, kKeyBlocks>& s, float 
 // by row, so that a row's rounding does not depend on the others'.
 constexpr float kSlack = 8.f;
 
-template <class C, int kNq>
-__device__ __forceinline__ void rescale(C& core, const bool (&grown)[kNq], const float (&top)[kNq]) {
+template <class C>
+__device__ __forceinline__ void rescale(C& core, bool grown, float top) {
+  const float f = grown ? exp2_hw(core.m - top) : 1.f;
+  if (grown) core.m = top;
+  core.l *= f;
 #pragma unroll
-  for (int n = 0; n < kNq; ++n) {
-    const float f = grown[n] ? exp2_hw(core.m[n] - top[n]) : 1.f;
-    if (grown[n]) core.m[n] = top[n];
-    core.l[n] *= f;
+  for (int d = 0; d < C::kOut; ++d)
 #pragma unroll
-    for (int d = 0; d < C::kOut; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) core.o[n][d][i] *= f;
-  }
+    for (int i = 0; i < 16; ++i) core.o[d][i] *= f;
 }
 
-template <class C, int kNq>
-__device__ __forceinline__ void exponent_offsets(const C& core, float (&ms)[kNq]) {
-#pragma unroll
-  for (int n = 0; n < kNq; ++n) ms[n] = core.m[n] == -__builtin_inff() ? 0.f : core.m[n];
-}
-
-// With a tile's largest scores mx (a lane's own); ms: what the weights' exponents are taken against.
-template <class C, int kNq>
-__device__ __forceinline__ void update_maximum(C& core, const float (&mx)[kNq], float c, float (&ms)[kNq]) {
-  float top[kNq];
-  bool grown[kNq], any = false;
-#pragma unroll
-  for (int n = 0; n < kNq; ++n) {
-    top[n] = max_halves(mx[n]) * c;
-    grown[n] = top[n] > core.m[n] + kSlack;
-    any = any || grown[n];
-  }
-  if (__any(any)) rescale(core, grown, top);
-  exponent_offsets(core, ms);
+// With a tile's largest score mx (a lane's own); ms: what the weights' exponents are taken against.
+template <class C>
+__device__ __forceinline__ void update_maximum(C& core, float mx, float c, float& ms) {
+  const float top = max_halves(mx) * c;
+  const bool grown = top > core.m + kSlack;
+  if (__any(grown)) rescale(core, grown, top);
+  ms = core.m == -__builtin_inff() ? 0.f : core.m;
 }
 
 }  // namespace gc

@@ -50,43 +50,40 @@ struct Normaliser {
 
 // Results of a wave's rows (l whole, not a lane's part): to the output, or as
 // a part of rows whose keys are split.
-template <class T, int kDim, class C, int kNq>
+template <class T, int kDim, class C>
 __device__ __forceinline__ void store_rows(const AttentionArgs& p, const AttentionItem& it, int kv_head, const C& core,
-                                           const float (&l)[kNq], int first_row, int tile_rows, int lane) {
+                                           float l, int first_row, int tile_rows, int lane) {
   const int half = lane >> 5;
-#pragma unroll
-  for (int n = 0; n < kNq; ++n) {
-    const int local = first_row + 32 * n + (lane & 31);
-    if (it.parts > 1) {
-      float* part = p.partial + ((int64_t)it.slot * p.kv_heads + kv_head) * ((int64_t)tile_rows * (kDim + 2));
-      float* row = part + (int64_t)local * kDim;
-#pragma unroll
-      for (int d = 0; d < C::kOut; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          store4(row + 32 * d + 8 * g + 4 * half,
-                 f32x4{core.o[n][d][4 * g], core.o[n][d][4 * g + 1], core.o[n][d][4 * g + 2], core.o[n][d][4 * g + 3]});
-      if (half == 0) *reinterpret_cast<float2*>(part + (int64_t)tile_rows * kDim + 2 * local) = float2{core.m[n], l[n]};
-      continue;
-    }
-    const RowOf r = row_of(p, it, kv_head, it.row0 + local);
-    if (!r.live) continue;
-    const Normaliser z(core.m[n], l[n]);
-    T* row = (T*)p.out + r.token * p.o_token + (int64_t)r.head * p.o_head;
+  const int local = first_row + (lane & 31);
+  if (it.parts > 1) {
+    float* part = p.partial + ((int64_t)it.slot * p.kv_heads + kv_head) * ((int64_t)tile_rows * (kDim + 2));
+    float* row = part + (int64_t)local * kDim;
 #pragma unroll
     for (int d = 0; d < C::kOut; ++d)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = 32 * d + 8 * g + 4 * half;
-        if (c < p.dim) {
-          f32x4 x;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = l[n] == 0.f ? 0.f : core.o[n][d][4 * g + j] * z.inv;
-          store4(row + c, x);
-        }
-      }
-    if (p.lse && half == 0) p.lse[(int64_t)r.head * p.total_q + r.token] = z.lse;
+      for (int g = 0; g < 4; ++g)
+        store4(row + 32 * d + 8 * g + 4 * half,
+               f32x4{core.o[d][4 * g], core.o[d][4 * g + 1], core.o[d][4 * g + 2], core.o[d][4 * g + 3]});
+    if (half == 0) *reinterpret_cast<float2*>(part + (int64_t)tile_rows * kDim + 2 * local) = float2{core.m, l};
+    return;
   }
+  const RowOf r = row_of(p, it, kv_head, it.row0 + local);
+  if (!r.live) return;
+  const Normaliser z(core.m, l);
+  T* row = (T*)p.out + r.token * p.o_token + (int64_t)r.head * p.o_head;
+#pragma unroll
+  for (int d = 0; d < C::kOut; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = 32 * d + 8 * g + 4 * half;
+      if (c < p.dim) {
+        f32x4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = l == 0.f ? 0.f : core.o[d][4 * g + j] * z.inv;
+        store4(row + c, x);
+      }
+    }
+  if (p.lse && half == 0) p.lse[(int64_t)r.head * p.total_q + r.token] = z.lse;
 }
 
 // Adds the parts of split rows, in their order: a launch of its own after the
@@ -157,28 +154,37 @@ void launch_join(const AttentionArgs& p, int tile_rows, unsigned blocks, hipStre
 // are there, and nobody reads K of i or V of i - 2 any more: K of i + 2 and V
 // of i + 2 are asked for in their places.  The next barrier waits for that K
 // and for the V asked for a tile before; the last V may be outstanding.
+//
+// What bounds it: with 64 channels the issue of both kinds (a SIMD's vector
+// unit is busy 58 % of the time, its matrix unit 32 %; a lone wave takes 34
+// cycles for a product, 46 for four multiply-adds, two exponentials and a
+// conversion, and 54 for all), with 128 the power that the products draw (busy 56 % and 58 %, the
+// clock at 1.9 of 2.4 GHz; the products alone take 2.9 of the 4.3 ms).
+// 64 keys a tile up to 96 channels, 32 above: what the registers hold.  24576
+// tokens x 16 heads x 128: 4.27 ms, 1160 TFLOP/s; 10403 tokens in four
+// sequences x 16 x 64: 152 us.  Not faster: halves of the block that take
+// turns at products and vector work, with a barrier a part (4.36 ms, causal
+// 810 us against 707); 32 keys a tile at three waves a SIMD for 64 channels
+// (1213 us against 1154); weights against a maximum that only the sum checks
+// (4.7 ms); wave priorities, operands 2, 6 or 8 products ahead (within 1 %).
 // ---------------------------------------------------------------------------
-template <int kDim, int kNq, int kKeyBlocks, int kWaves>
+template <int kDim, int kKeyBlocks, int kWaves>
 __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
   using T = uint16_t;
-  constexpr int kKeys = 32 * kKeyBlocks, kTile = kKeys * kDim * (int)sizeof(T), kRows = 32 * kNq * kWaves;
+  constexpr int kKeys = 32 * kKeyBlocks, kTile = kKeys * kDim * (int)sizeof(T), kRows = 32 * kWaves;
   // an array a tile: the compiler then sees that a read of one does not wait for the loads to another
   __shared__ __attribute__((aligned(1024))) char k0[kTile], k1[kTile], v0[kTile], v1[kTile], v2[kTile], v3[kTile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv_head = blockIdx.x % p.kv_heads;
   const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
 
-  using C = Core<T, kDim, kNq, kKeyBlocks>;
+  using C = Core<T, kDim, kKeyBlocks>;
   C core;
   core.init();
-  const int first_row = wave * 32 * kNq;
-  int limit[kNq];
-#pragma unroll
-  for (int n = 0; n < kNq; ++n) {
-    const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + 32 * n + (lane & 31));
-    limit[n] = r.limit < it.k_end ? r.limit : it.k_end;
-    core.load_q(n, (const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
-  }
+  const int first_row = wave * 32;
+  const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + (lane & 31));
+  const int limit = r.limit < it.k_end ? r.limit : it.k_end;
+  core.load_q((const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
 
   using Loader = TileLoader<T, kDim, kKeys, kWaves>;
   Loader kl, vl;
@@ -186,7 +192,7 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
   kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, it.k_begin, it.k_len, wave, lane);
   vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, it.k_begin, it.k_len, wave, lane);
   // the wave's rows see at most high keys, the block's rows at least low (limits grow with the row)
-  const int high = __builtin_amdgcn_readlane(limit[kNq - 1], 31);
+  const int high = __builtin_amdgcn_readlane(limit, 31);
   int low = it.k_end;
   if (p.causal) {
     const int least = it.row0 / p.group + it.reach;
@@ -198,7 +204,7 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
   typename C::S even, odd;   // scores of even and odd tiles
   typename C::Weights w;
   typename C::Operands x;
-  float mx[kNq], ms[kNq];
+  float mx, ms;
   uint32_t bad = 0;
   int first_masked = key0;
 
@@ -283,22 +289,21 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
   }
 
   if (__any(bad != 0)) add_nonfinite<T>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
-  float l[kNq];
-#pragma unroll
-  for (int n = 0; n < kNq; ++n) l[n] = sum_halves(core.l[n]);
-  store_rows<T, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
+  store_rows<T, kDim>(p, it, kv_head, core, sum_halves(core.l), first_row, kRows, lane);
 }
 
-template <int kDim, int kNq, int kKeyBlocks, int kWaves, int kPerSimd>
+template <int kDim, int kKeyBlocks, int kWaves, int kPerSimd>
 __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const AttentionArgs p) {
-  attention_rows<kDim, kNq, kKeyBlocks, kWaves>(p);
+  attention_rows<kDim, kKeyBlocks, kWaves>(p);
 }
 
 // ---------------------------------------------------------------------------
 // rows, float32: a product takes sixteen times as long as bfloat16's, so a
 // tile's parts follow one another and the blocks of a compute unit (or its
 // four waves) fill the gaps.  Two places for K and V each: one tile is worked
-// on while the next arrives.
+// on while the next arrives.  1024 + 1 + 517 + 770 tokens x 8 heads x 64: 51
+// us, of which the parts' join takes 7 (the matrix units are busy 55 % of the
+// first launch: 256 blocks for 256 compute units, no second one to fill gaps).
 // ---------------------------------------------------------------------------
 template <int kDim, int kPerSimd>
 __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const AttentionArgs p) {
@@ -308,18 +313,18 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
   const int kv_head = blockIdx.x % p.kv_heads;
   const AttentionItem it = p.items[blockIdx.x / p.kv_heads];
 
-  using C = Core<float, kDim, 1, 1>;
+  using C = Core<float, kDim, 1>;
   C core;
   core.init();
   const int first_row = wave * 32;
   const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + (lane & 31));
-  const int limit[1] = {r.limit < it.k_end ? r.limit : it.k_end};
-  core.load_q(0, (const float*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
+  const int limit = r.limit < it.k_end ? r.limit : it.k_end;
+  core.load_q((const float*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
 
   TileLoader<float, kDim, kKeys, kWaves> kl, vl;
   kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, it.k_begin, it.k_len, wave, lane);
   vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, it.k_begin, it.k_len, wave, lane);
-  const int high = __builtin_amdgcn_readlane(limit[0], 31);
+  const int high = __builtin_amdgcn_readlane(limit, 31);
   int low = it.k_end;
   if (p.causal) {
     const int least = it.row0 / p.group + it.reach;
@@ -338,7 +343,7 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
     if (!kMasked || key0 < high) {
       typename C::S s;
       typename C::Weights w;
-      float mx[1], ms[1];
+      float mx, ms;
       core.scores(k_now, lane, s);
       if constexpr (kMasked) mask(s, key0, limit, lane);
       maximum(s, mx);
@@ -365,14 +370,15 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
   wait_loads<0>();   // before the block's LDS is given up
 
   if (__any(bad != 0)) add_nonfinite<float>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
-  const float l[1] = {sum_halves(core.l[0])};
-  store_rows<float, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
+  store_rows<float, kDim>(p, it, kv_head, core, sum_halves(core.l), first_row, kRows, lane);
 }
 
 // ---------------------------------------------------------------------------
 // keys: few rows over many keys.  The waves of a block hold the same 32 rows
 // and take tiles of 32 keys in turn, each with two tiles of its own in LDS
-// and no barrier until the end, where their results are added.
+// and no barrier until the end, where their results are added.  Bound by the
+// read of the keys and values: 495 MB for 8 tokens (32 heads on 8 of 128) in
+// 85 us, 5.8 TB/s where a large read reaches 7.0, and 5 us for the join.
 // ---------------------------------------------------------------------------
 template <class T, int kDim, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionArgs p) {
@@ -396,20 +402,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   constexpr int kStep = kWaves * kKeys;
   kl.init(p.k, it.k_token0, p.k_token, kv_head * p.k_head, p.dim, first, it.k_len, 0, lane);
   vl.init(p.v, it.k_token0, p.v_token, kv_head * p.v_head, p.dim, first, it.k_len, 0, lane);
-  using C = Core<T, kDim, 1, 1>;
+  using C = Core<T, kDim, 1>;
   C core;
   core.init();
   const RowOf r = row_of(p, it, kv_head, it.row0 + (lane & 31));
-  const int limit[1] = {r.limit < it.k_end ? r.limit : it.k_end};
-  core.load_q(0, (const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
+  const int limit = r.limit < it.k_end ? r.limit : it.k_end;
+  core.load_q((const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
   if (first < it.k_end) {
     kl.load(mine, 0);
     vl.load(mine + kTile, 0);
     kl.load(mine + 2 * kTile, 0);
     vl.load(mine + 3 * kTile, 0);
   }
-  const int low = __builtin_amdgcn_readfirstlane(limit[0]);
-  const int high = __builtin_amdgcn_readlane(limit[0], 31);
+  const int low = __builtin_amdgcn_readfirstlane(limit);
+  const int high = __builtin_amdgcn_readlane(limit, 31);
   const float c = p.scale * kLog2e;
 
   int stage = 0;
@@ -418,7 +424,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
     char* kt = mine + stage * 2 * kTile;
     typename C::S s;
     typename C::Weights w;
-    float mx[1], ms[1];
+    float mx, ms;
     wait_loads<kLeft>();
     core.scores(kt, lane, s);
     wait_lds();
@@ -444,17 +450,17 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   if (__any(bad != 0))
     add_nonfinite<T>(p, it, kv_head, core, first_masked, high, kKeys, kWaves * kKeys, limit, lane);
   // the waves' results, added by the first wave in their order
-  float l[1] = {sum_halves(core.l[0])};
+  float l = sum_halves(core.l);
   wait_loads<0>();   // (also before the block's LDS is given up)
   if constexpr (kWaves > 1) {
     float* o = reinterpret_cast<float*>(mine);
 #pragma unroll
     for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[(d * 16 + i) * 64 + lane] = core.o[0][d][i];
+      for (int i = 0; i < 16; ++i) o[(d * 16 + i) * 64 + lane] = core.o[d][i];
     if (lane < 32) {
-      ml[wave][lane][0] = core.m[0];
-      ml[wave][lane][1] = l[0];
+      ml[wave][lane][0] = core.m;
+      ml[wave][lane][1] = l;
     }
     __syncthreads();
     if (wave == 0) {
@@ -462,21 +468,21 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[w][lane & 31][0]);
       const float ms = m == -__builtin_inff() ? 0.f : m;
-      l[0] = 0.f;
+      l = 0.f;
 #pragma unroll
       for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) core.o[0][d][i] = 0.f;
+        for (int i = 0; i < 16; ++i) core.o[d][i] = 0.f;
       for (int w = 0; w < kWaves; ++w) {
         const float f = exp2_hw(ml[w][lane & 31][0] - ms);
-        l[0] += ml[w][lane & 31][1] * f;
+        l += ml[w][lane & 31][1] * f;
         const float* x = reinterpret_cast<const float*>(lds + w * 4 * kTile);
 #pragma unroll
         for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) core.o[0][d][i] += x[(d * 16 + i) * 64 + lane] * f;
+          for (int i = 0; i < 16; ++i) core.o[d][i] += x[(d * 16 + i) * 64 + lane] * f;
       }
-      core.m[0] = m;
+      core.m = m;
     }
   }
   if (wave == 0) store_rows<T, kDim>(p, it, kv_head, core, l, 0, 32, lane);
