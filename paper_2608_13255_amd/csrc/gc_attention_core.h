@@ -218,14 +218,26 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
 
   // Operand i of the output: group i / kOut of the weights' keys, channels 32 (i % kOut) + lane % 32.  Two reads that
   // transpose: four rows of 16 channels a group of 16 lanes, from rows first .. first + 3 and first + 8 .. first + 11
-  // (first 4 half further).
-  __device__ __forceinline__ static u32x4 values(const char* vt, int lane, int i) {
+  // (first 4 half further).  A lane's places in the first group are kept in registers, since the permutation hides from
+  // the compiler that the other groups' are whole rows further (with places computed where they are needed the
+  // reads came late: 10403 tokens in four sequences x 16 heads x 64 152 us).
+  int value_at[2][kOut];
+  __device__ __forceinline__ void init_values(int lane) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int d = 0; d < kOut; ++d) {
+        const int row = 8 * j + 4 * (lane >> 5) + ((lane >> 2) & 3);
+        const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+        value_at[j][d] = place<kChunks>(row, chunk) + (lane & 1) * 8;
+        asm volatile("" : "+v"(value_at[j][d]));
+      }
+  }
+  __device__ __forceinline__ u32x4 values(const char* vt, int i) const {
     u32x4 w;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int row = 16 * (i / kOut) + 8 * j + 4 * (lane >> 5) + ((lane >> 2) & 3);
-      const int chunk = 4 * (i % kOut) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-      const char* at = vt + place<kChunks>(row, chunk) + (lane & 1) * 8;
+      const char* at = vt + value_at[j][i % kOut] + i / kOut * (16 * kChunks * 16);
       const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at);
       const u32x2 y = __builtin_bit_cast(u32x2, x);
       w[2 * j] = y[0], w[2 * j + 1] = y[1];
@@ -245,11 +257,11 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
 
   // A tile's values, where rows may be masked: those that are not finite enter as zeros (a masked row's weight 0 times NaN
   // or infinity would be NaN).  Returns whether there were any (add_nonfinite).
-  __device__ __forceinline__ uint32_t add_masked(const char* vt, int lane, const Weights& w) {
+  __device__ __forceinline__ uint32_t add_masked(const char* vt, int, const Weights& w) {
     uint32_t bad = 0;
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
-      u32x4 v = values(vt, lane, i);
+      u32x4 v = values(vt, i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t x = finite_pair(v[j]);
@@ -260,9 +272,9 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
     }
     return bad;
   }
-  __device__ __forceinline__ void add_values(const char* vt, int lane, const Weights& w) {
+  __device__ __forceinline__ void add_values(const char* vt, int, const Weights& w) {
 #pragma unroll
-    for (int i = 0; i < kOperands; ++i) add(w, values(vt, lane, i), i);
+    for (int i = 0; i < kOperands; ++i) add(w, values(vt, i), i);
   }
 
   __device__ __forceinline__ void weight(const S& s, float c, float ms, Weights& w, int e, float& sum) const {
@@ -285,9 +297,9 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
     bf16x8 k[kAhead];
     u32x4 v[kAhead];
   };
-  __device__ __forceinline__ static void first_values(const char* vt, int lane, Operands& x) {
+  __device__ __forceinline__ void first_values(const char* vt, Operands& x) const {
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) x.v[i] = values(vt, lane, i);
+    for (int i = 0; i < kAhead; ++i) x.v[i] = values(vt, i);
   }
 
   // the values of the tile before, and this tile's largest scores (of this lane's)
@@ -300,7 +312,7 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
     mx = s.s[0][0];
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
-      if (i + kAhead < kOperands) v[i + kAhead] = values(vt, lane, i + kAhead);
+      if (i + kAhead < kOperands) v[i + kAhead] = values(vt, i + kAhead);
       else x.k[i + kAhead - kOperands] = keys(kt, lane, i + kAhead - kOperands);
       add(w, v[i], i);
 #pragma unroll
@@ -331,7 +343,7 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
 #pragma unroll
     for (int i = 0; i < kOperands; ++i) {
       if (i + kAhead < kOperands) k[i + kAhead] = keys(kt, lane, i + kAhead);
-      else x.v[i + kAhead - kOperands] = values(vt, lane, i + kAhead - kOperands);
+      else x.v[i + kAhead - kOperands] = values(vt, i + kAhead - kOperands);
       score(next, k[i], i);
 #pragma unroll
       for (int e = i * kWeights / kOperands; e < (i + 1) * kWeights / kOperands; ++e)
@@ -404,6 +416,7 @@ struct Core<float, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
     l += sum;
   }
 
+  __device__ __forceinline__ void init_values(int) {}
   // channel 32 d + lane % 32 of key 32 b + 8 (i / 4) + 4 half + i % 4
   __device__ __forceinline__ static float value(const char* vt, int b, int i, int d, int lane) {
     const int row = 32 * b + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;

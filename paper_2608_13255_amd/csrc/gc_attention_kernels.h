@@ -181,6 +181,7 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
   using C = Core<T, kDim, kKeyBlocks>;
   C core;
   core.init();
+  core.init_values(lane);
   const int first_row = wave * 32;
   const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + (lane & 31));
   const int limit = r.limit < it.k_end ? r.limit : it.k_end;
@@ -242,7 +243,7 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
   };
   int phase = 1;   // i % 4
   if (key0 + kKeys <= low) {
-    C::first_values(v0, lane, x);
+    core.first_values(v0, x);
     while (key0 + 4 * kKeys <= low) {
       tile(odd, even, k1, k0, v0, v1, v3);
       tile(even, odd, k0, k1, v1, v2, v0);
@@ -316,6 +317,7 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
   using C = Core<float, kDim, 1>;
   C core;
   core.init();
+  core.init_values(lane);
   const int first_row = wave * 32;
   const RowOf r = row_of(p, it, kv_head, it.row0 + first_row + (lane & 31));
   const int limit = r.limit < it.k_end ? r.limit : it.k_end;
@@ -405,6 +407,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   using C = Core<T, kDim, 1>;
   C core;
   core.init();
+  core.init_values(lane);
   const RowOf r = row_of(p, it, kv_head, it.row0 + (lane & 31));
   const int limit = r.limit < it.k_end ? r.limit : it.k_end;
   core.load_q((const T*)p.q + r.token * p.q_token + (int64_t)r.head * p.q_head, p.dim, lane >> 5);
