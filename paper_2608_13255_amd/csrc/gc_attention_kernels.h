@@ -160,9 +160,9 @@ void launch_join(const AttentionArgs& p, int tile_rows, unsigned blocks, hipStre
 // cycles for a product, 46 for four multiply-adds, two exponentials and a
 // conversion, and 54 for all), with 128 the power that the products draw (busy 56 % and 58 %, the
 // clock at 1.9 of 2.4 GHz; the products alone take 2.9 of the 4.3 ms).
-// 64 keys a tile up to 96 channels, 32 above: what the registers hold.  24576
-// tokens x 16 heads x 128: 4.27 ms, 1160 TFLOP/s; 10403 tokens in four
-// sequences x 16 x 64: 152 us.  Not faster: halves of the block that take
+// 64 keys a tile up to 128 channels, 32 above (and with four waves a block
+// above 96): what registers and LDS hold.  24576 tokens x 16 heads x 128: 4.1
+// ms, 1205 TFLOP/s; 10403 tokens in four sequences x 16 x 64: 149 us.  Not faster: halves of the block that take
 // turns at products and vector work, with a barrier a part (4.36 ms, causal
 // 810 us against 707); 32 keys a tile at three waves a SIMD for 64 channels
 // (1213 us against 1154); weights against a maximum that only the sum checks
