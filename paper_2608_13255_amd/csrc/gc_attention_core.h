@@ -256,19 +256,35 @@ struct Core<uint16_t, kDim, kKeyBlocks> : Accumulators<kDim / 32> {
   }
 
   // A tile's values, where rows may be masked: those that are not finite enter as zeros (a masked row's weight 0 times NaN
-  // or infinity would be NaN).  Returns whether there were any (add_nonfinite).
+  // or infinity would be NaN).  Returns whether there were any (add_nonfinite).  The largest magnitude, as an
+  // integer, tells of a few operands at a time whether one is to be replaced (two instructions a pair of values
+  // against ten: 4096 causal tokens x 8 heads x 128 53.8 us against 56.9).
   __device__ __forceinline__ uint32_t add_masked(const char* vt, int, const Weights& w) {
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    constexpr int kGroup = kOperands % 4 == 0 ? 4 : 2;
     uint32_t bad = 0;
 #pragma unroll
-    for (int i = 0; i < kOperands; ++i) {
-      u32x4 v = values(vt, i);
+    for (int i0 = 0; i0 < kOperands; i0 += kGroup) {
+      u32x4 v[kGroup];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t x = finite_pair(v[j]);
-        bad |= v[j] ^ x;
-        v[j] = x;
+      for (int i = 0; i < kGroup; ++i) v[i] = values(vt, i0 + i);
+      u16x2 top = {0, 0};
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[i][j] & 0x7fff7fffu));
+      if (__any(top[0] >= 0x7f80 || top[1] >= 0x7f80)) {
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t x = finite_pair(v[i][j]);
+            bad |= v[i][j] ^ x;
+            v[i][j] = x;
+          }
       }
-      add(w, v, i);
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) add(w, v[i], i0 + i);
     }
     return bad;
   }
