@@ -18,6 +18,7 @@
 //   24576 tokens, 16 heads of 128                                      4270 3592
 #include <algorithm>
 #include <cmath>
+#include <exception>
 #include <functional>
 #include <queue>
 #include <vector>
@@ -150,10 +151,10 @@ void choose(const Batch& b, int dim, int dtype, int* kind, int* part) {
 
 using namespace gc;
 
-extern "C" int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, int n_seq, int heads, int kv_heads, int dim,
-                                 int dtype, int causal, gc_attention_info* info, int32_t* items, int64_t capacity_words) {
-  clear_error();
-  const char* who = "gc_attention_plan";
+namespace {
+
+int make_plan(const int32_t* q_lens, const int32_t* k_lens, int n_seq, int heads, int kv_heads, int dim, int dtype,
+              int causal, gc_attention_info* info, int32_t* items, int64_t capacity_words, const char* who) {
   if (!info) return fail(GC_ERR_ARG, "%s: info is null", who);
   int rc = check_head_sizes(heads, dim, dtype, who);
   if (rc) return rc;
@@ -206,6 +207,19 @@ extern "C" int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, i
   AttentionItem* first = reinterpret_cast<AttentionItem*>(items);
   std::stable_sort(first, it, [](const AttentionItem& x, const AttentionItem& y) { return x.k_end - x.k_begin > y.k_end - y.k_begin; });
   return GC_OK;
+}
+
+}  // namespace
+
+extern "C" int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, int n_seq, int heads, int kv_heads, int dim,
+                                 int dtype, int causal, gc_attention_info* info, int32_t* items, int64_t capacity_words) {
+  clear_error();
+  const char* who = "gc_attention_plan";
+  try {
+    return make_plan(q_lens, k_lens, n_seq, heads, kv_heads, dim, dtype, causal, info, items, capacity_words, who);
+  } catch (const std::exception&) {   // the lists of tiles and parts
+    return fail(GC_ERR_CAPACITY, "%s: no host memory for %d sequences", who, n_seq);
+  }
 }
 
 extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads* v, const gc_heads* out, float* lse,

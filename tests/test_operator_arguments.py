@@ -2,6 +2,9 @@
 the attention plan's items (no GPU)."""
 import ctypes
 import math
+import subprocess
+import sys
+from pathlib import Path
 
 import numpy as np
 import pytest
@@ -289,3 +292,27 @@ def test_attention_tokens_that_share_memory(gc, L):
         t[name].token_stride = 56
         refused(L, L.gc_attention(*(ctypes.byref(t[n]) for n in "qkvo"), A[4], ctypes.byref(info), A[5], 0.125, A[6], 1 << 40, None),
                 "SHAPE", "token strides of k and v")
+
+
+def test_attention_plan_without_host_memory(gc, L):
+    """A batch whose lists of tiles do not fit the process's memory is refused, and the next plan is as ever."""
+    code = """if True:
+        import ctypes, resource, sys
+        import numpy as np
+        import paper_2608_13255_amd as gc
+        L = gc.lib()
+        n = 1 << 24
+        ones = np.ones(n, np.int32)
+        p = ones.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+        info = gc.AttentionInfo()
+        used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+        resource.setrlimit(resource.RLIMIT_AS, (used + (32 << 20), resource.getrlimit(resource.RLIMIT_AS)[1]))
+        rc = L.gc_attention_plan(p, p, n, 2, 2, 64, 1, 0, ctypes.byref(info), None, 0)
+        text = L.gc_last_error().decode()
+        assert L.gc_attention_plan(p, p, 3, 2, 2, 64, 1, 0, ctypes.byref(info), None, 0) == 0
+        assert info.n_items == 3
+        print(rc, text)
+    """
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=Path(__file__).parent.parent)
+    assert done.returncode == 0, done.stderr
+    assert done.stdout.startswith(f"{CODE['CAPACITY']} ") and "host memory" in done.stdout, done.stdout
