@@ -225,6 +225,7 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
     update_maximum(core, mx, c, ms);
     core.weights(even, c, ms, w);
     core.scores(k1, lane, odd);
+    wait_lds();   // (a product, and its operand's wait, may be moved past a barrier that waits for nothing)
     key0 += kKeys;
   }
   const auto arrive = [&] {
@@ -269,6 +270,7 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
     first_masked = key0 - kKeys;
     if (phase & 1) even = odd;
     while (key0 < it.k_end) {
+      wait_lds();   // as above, for this loop's reads
       arrive();
       char* const k_now = phase & 1 ? k1 : k0;
       kl.load(k_now, wave);
