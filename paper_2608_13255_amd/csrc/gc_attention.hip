@@ -12,10 +12,10 @@
 // 153 (float32) TFLOP/s:
 //   8 single tokens, 32 heads on 8 of 128, 495 MB of keys and values     90   71
 //   1024 + 1 + 517 + 770 tokens, 8 heads of 64, float32                  51   25
-//   10403 tokens in 4 sequences, 16 heads of 64, among themselves       152   83
-//   the same over 31070 keys, 16 heads of 80 (worked on as 96)          509  308
-//   15427 causal tokens in 7 sequences, 32 heads on 8 of 128            707  527
-//   24576 tokens, 16 heads of 128                                      4270 3592
+//   10403 tokens in 4 sequences, 16 heads of 64, among themselves       148   83
+//   the same over 31070 keys, 16 heads of 80 (worked on as 96)          508  308
+//   15427 causal tokens in 7 sequences, 32 heads on 8 of 128            677  527
+//   24576 tokens, 16 heads of 128                                      4054 3592
 #include <algorithm>
 #include <cmath>
 #include <exception>
@@ -110,7 +110,7 @@ double time_of(const std::vector<int>& tiles, int part, const Cost& c, int kv_he
 // rows among its waves' keys; else 128 or 256 rows a block, whichever takes
 // less time.  256 rows read each tile of keys half as often, 128 leave less
 // over at a sequence's and at the launch's end.  256 against 128: 24576 tokens
-// x 16 heads x 128 4.34 ms and 4.54, 16384 causal x 8 x 128 530 us and 562,
+// x 16 heads x 128 4.05 ms and 4.54, 16384 causal x 8 x 128 491 us and 562,
 // 4096 x 16 x 64 83 and 89; 2048 x 16 x 64 36 and 27, 6000 x 12 x 96 228 and
 // 219, 4096 causal x 8 x 128 64 and 60.  Parts: 160 rows over 9000 keys 22 us
 // in 29 against 150 whole; 2048 x 16 x 64 27 whole against 35 in two.

@@ -12,7 +12,7 @@
 // half the LDS traffic of 16 x 16 blocks; with 32 rows a wave holds 64 keys'
 // scores twice (or 32 of 128 channels) beside the output within the 256
 // registers of two waves a SIMD.  64 rows a wave would halve the LDS reads
-// again but spill (8.8 ms where 32 rows take 4.3).
+// again but spill (8.8 ms where 32 rows took 4.3).
 //
 // K and V tiles lie in LDS as rows of 16-byte chunks, chunk c of row r at
 // place c ^ f(r): with f below, 16 rows' same chunk lie in 16 different

@@ -156,15 +156,15 @@ void launch_join(const AttentionArgs& p, int tile_rows, unsigned blocks, hipStre
 // and for the V asked for a tile before; the last V may be outstanding.
 //
 // What bounds it: with 64 channels the issue of both kinds (a SIMD's vector
-// unit is busy 58 % of the time, its matrix unit 32 %; a lone wave takes 34
+// unit is busy 55 % of the time, its matrix unit 34 %; a lone wave takes 34
 // cycles for a product, 46 for four multiply-adds, two exponentials and a
-// conversion, and 54 for all), with 128 the power that the products draw (busy 56 % and 58 %, the
-// clock at 1.9 of 2.4 GHz; the products alone take 2.9 of the 4.3 ms).
+// conversion, and 54 for all), with 128 the power that the products draw (busy 54 % and 65 %, the
+// clock at 1.8 of 2.4 GHz; the products alone take 2.9 of the 4.1 ms).
 // 64 keys a tile up to 128 channels, 32 above (and with four waves a block
 // above 96): what registers and LDS hold.  24576 tokens x 16 heads x 128: 4.1
-// ms, 1205 TFLOP/s; 10403 tokens in four sequences x 16 x 64: 149 us.  Not faster: halves of the block that take
-// turns at products and vector work, with a barrier a part (4.36 ms, causal
-// 810 us against 707); 32 keys a tile at three waves a SIMD for 64 channels
+// ms, 1220 TFLOP/s; 10403 tokens in four sequences x 16 x 64: 148 us.  Not faster (against 4.27 ms and 707 us at the time):
+// halves of the block that take turns at products and vector work, with a
+// barrier a part (4.36 ms, causal 810 us); 32 keys a tile at three waves a SIMD for 64 channels
 // (1213 us against 1154); weights against a maximum that only the sum checks
 // (4.7 ms); wave priorities, operands 2, 6 or 8 products ahead (within 1 %).
 // ---------------------------------------------------------------------------
@@ -307,6 +307,9 @@ __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const 
 // on while the next arrives.  1024 + 1 + 517 + 770 tokens x 8 heads x 64: 51
 // us, of which the parts' join takes 7 (the matrix units are busy 55 % of the
 // first launch: 256 blocks for 256 compute units, no second one to fill gaps).
+// Slower: the next tile's scores beside this tile's weights (60 us; 2000
+// tokens x 8 x 256 404 against 289): the compiler then waits for the loads to
+// LDS inside a tile.
 // ---------------------------------------------------------------------------
 template <int kDim, int kPerSimd>
 __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const AttentionArgs p) {
