@@ -1140,13 +1140,10 @@ def gc_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain: torch.Tensor, k_ga
 
 @dataclass
 class AttentionPlan:
-    """Output of gc_attention_plan: the sizes, the items on the device and the
-    workspace (None where no keys are split).  Calls in flight at the same
-    time (on different streams) need a plan of their own each where there is a
-    workspace."""
+    """Output of gc_attention_plan: the sizes and the items on the device.
+    Calls only read it, so calls in flight at the same time may share it."""
     info: AttentionInfo
     items: torch.Tensor
-    workspace: Optional[torch.Tensor]
 
     def __post_init__(self):
         i = self.info
@@ -1183,17 +1180,18 @@ def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, 
     s = _side_stream(stream)
     with torch.cuda.stream(s if s is not None else torch.cuda.current_stream()):
         items = torch.from_numpy(host).to(device)
-        ws = (torch.empty(info.workspace_bytes, dtype=torch.uint8, device=device) if info.workspace_bytes else None)
-    return AttentionPlan(info, items, ws)
+    return AttentionPlan(info, items)
 
 
 def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: AttentionPlan,
                  scale: Optional[float] = None, out: torch.Tensor = None, lse: torch.Tensor = None,
-                 stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+                 stream=None, workspace: torch.Tensor = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Attention of q [sum of q_lens, heads, dim] over k, v [sum of k_lens,
     kv_heads, dim] with the plan of their lengths; scale defaults to
-    1 / sqrt(dim).  Returns (out like q, lse float32 [heads, sum of q_lens])."""
-    info, ws = plan.info, plan.workspace
+    1 / sqrt(dim).  Returns (out like q, lse float32 [heads, sum of q_lens]).
+    workspace: plan.info.workspace_bytes for this call (allocated if None);
+    calls in flight at the same time need one each."""
+    info, need = plan.info, plan.info.workspace_bytes
     H, Hk, D, T, S = plan.sizes
     if q.shape != (T, H, D) or _head_code(q) != info.dtype:
         raise ValueError(f"q must be [{T}, {H}, {D}] of the plan's type (got {q.dtype} {list(q.shape)})")
@@ -1215,9 +1213,16 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
         fresh.append(lse)
     elif lse.dtype != torch.float32 or lse.shape != (H, T) or lse.get_device() != device:
         raise ValueError(f"lse must be float32 [{H}, {T}] on {q.device}")
+    at, size = None, 0
+    if need:
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            fresh.append(workspace)
+        elif workspace.get_device() != device:
+            raise ValueError(f"workspace must be on {q.device} (got {workspace.device})")
+        at, size = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
     _check(lib().gc_attention(hq, hk, hv, ho, _dev(lse, "lse"), info, plan.items.data_ptr(),
-                              1.0 / math.sqrt(D) if scale is None else scale, None if ws is None else ws.data_ptr(),
-                              0 if ws is None else ws.numel(), _stream(stream)), "gc_attention")
+                              1.0 / math.sqrt(D) if scale is None else scale, at, size, _stream(stream)), "gc_attention")
     if stream is not None:
-        _keep(stream, fresh + [plan.items] + ([] if ws is None else [ws]))
+        _keep(stream, fresh + [plan.items])
     return out, lse

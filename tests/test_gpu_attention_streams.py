@@ -1,0 +1,123 @@
+"""Attention plans and the multi-view layer used on several streams: a plan is
+only read, so calls in flight at the same time may share it, whatever it
+splits."""
+import threading
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def gc():
+    import paper_2608_13255_amd as gc
+    return gc
+
+
+class Recorder:
+    """The library, with the workspace that each gc_attention call gets."""
+
+    def __init__(self, real):
+        self.real, self.workspaces = real, []
+
+    def __getattr__(self, name):
+        return getattr(self.real, name)
+
+    def gc_attention(self, *args):
+        self.workspaces.append((args[8], args[9]))
+        return self.real.gc_attention(*args)
+
+
+def heads(n, H, Hk, D, seed, dtype=torch.bfloat16):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return [torch.randn((n, h, D), generator=g, device=DEV).to(dtype) for h in (H, Hk, Hk)]
+
+
+def on_threads(jobs):
+    """Runs the jobs on threads of their own, each under a stream of its own."""
+    errors = []
+
+    def worker(job):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                job()
+            s.synchronize()
+        except Exception as e:   # surfaced in the main thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=worker, args=(j,)) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    torch.cuda.synchronize()
+
+
+def test_a_call_on_another_stream_has_another_workspace(gc, monkeypatch):
+    n, H, D = 5000, 8, 128
+    plan = gc.gc_attention_plan([n], [n], H, H, D, torch.bfloat16, device=DEV)
+    need = plan.info.workspace_bytes
+    assert need > 0
+    q, k, v = heads(n, H, H, D, 1)
+    seen = Recorder(gc.lib())
+    monkeypatch.setattr(gc, "lib", lambda: seen)
+    torch.cuda.synchronize()
+    kept = torch.empty(need + 64, dtype=torch.uint8, device=DEV)
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(a):
+        first = gc.gc_attention(q, k, v, plan)
+    with torch.cuda.stream(b):
+        second = gc.gc_attention(q, k, v, plan)
+    third = gc.gc_attention(q, k, v, plan, workspace=kept)
+    torch.cuda.synchronize()
+    (pa, na), (pb, nb), (pc, nc) = seen.workspaces
+    assert min(na, nb) >= need and (pa + na <= pb or pb + nb <= pa)
+    assert (pc, nc) == (kept.data_ptr(), need + 64)
+    assert all(torch.equal(first[i], other[i]) for other in (second, third) for i in (0, 1))
+
+
+def test_workspace_refusals(gc):
+    plan = gc.gc_attention_plan([1], [50000], 8, 2, 128, torch.bfloat16, device=DEV)
+    need = plan.info.workspace_bytes
+    q, k, v = heads(1, 8, 2, 128, 2)[0], *heads(50000, 8, 2, 128, 3)[1:]
+    with pytest.raises(gc.GeoCacheError, match="workspace"):
+        gc.gc_attention(q, k, v, plan, workspace=torch.empty(need - 1, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError, match="workspace"):
+        gc.gc_attention(q, k, v, plan, workspace=torch.empty(need, dtype=torch.uint8))
+
+
+def test_one_plan_on_two_threads(gc):
+    n, H, Hk, D = 3000, 4, 2, 64
+    plan = gc.gc_attention_plan([n], [n], H, Hk, D, torch.bfloat16, device=DEV)
+    assert plan.info.n_slots > 0
+    inputs = [heads(n, H, Hk, D, seed) for seed in (4, 5)]
+    alone = [gc.gc_attention(*x, plan) for x in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    on_threads([lambda i=i: got[i].extend(gc.gc_attention(*inputs[i], plan) for _ in range(20)) for i in (0, 1)])
+    for i in (0, 1):
+        assert all(torch.equal(o, alone[i][0]) and torch.equal(e, alone[i][1]) for o, e in got[i])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_one_layer_on_two_threads(dtype):
+    """One layer, the same views: 1536 tokens, whose keys are split."""
+    from paper_2608_13255_amd.multiview import MultiViewAttention
+    g = torch.Generator(device=DEV)
+    g.manual_seed(6)
+    pos = torch.randn((1, 6, 16, 16, 3), generator=g, device=DEV)
+    layer = MultiViewAttention(pos, 64, 4, 2, 64, dtype, generator=g)
+    views = list(range(6))
+    assert layer.slice(views).plan.info.n_slots > 0
+    inputs = [torch.randn((1, 6, 16, 16, 64), generator=g, device=DEV).to(dtype) for _ in range(2)]
+    alone = [layer(x, views) for x in inputs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    on_threads([lambda i=i: got[i].extend(layer(inputs[i], views) for _ in range(20)) for i in (0, 1)])
+    for i in (0, 1):
+        assert all(torch.equal(y, alone[i]) for y in got[i])
