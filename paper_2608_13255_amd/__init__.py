@@ -1148,6 +1148,18 @@ class AttentionPlan:
     def __post_init__(self):
         i = self.info
         self.sizes = (i.heads, i.kv_heads, i.dim, i.total_q, i.total_k)
+        # handles of the streams after whose work torch's allocator reuses the items' memory
+        self.known_streams = set()
+
+    def used_on(self, handle: int, stream) -> None:
+        """Calls on this stream read the items: their memory stays theirs
+        until those are done, also where the plan is dropped before."""
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        elif not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(handle)
+        self.items.record_stream(stream)
+        self.known_streams.add(handle)
 
 
 def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, kv_heads: int, dim: int,
@@ -1179,8 +1191,10 @@ def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, 
     host = host[:max(1, words)]
     s = _side_stream(stream)
     with torch.cuda.stream(s if s is not None else torch.cuda.current_stream()):
-        items = torch.from_numpy(host).to(device)
-    return AttentionPlan(info, items)
+        plan = AttentionPlan(info, torch.from_numpy(host).to(device))
+        if plan.items.is_cuda:
+            plan.known_streams.add(torch.cuda.current_stream(plan.items.device).cuda_stream)
+    return plan
 
 
 def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: AttentionPlan,
@@ -1221,8 +1235,10 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
         elif workspace.get_device() != device:
             raise ValueError(f"workspace must be on {q.device} (got {workspace.device})")
         at, size = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    handle = _stream(stream)
+    if handle not in plan.known_streams:
+        plan.used_on(handle, stream)
     _check(lib().gc_attention(hq, hk, hv, ho, _dev(lse, "lse"), info, plan.items.data_ptr(),
-                              1.0 / math.sqrt(D) if scale is None else scale, at, size, _stream(stream)), "gc_attention")
-    if stream is not None:
-        _keep(stream, fresh + [plan.items])
+                              1.0 / math.sqrt(D) if scale is None else scale, at, size, handle), "gc_attention")
+    _keep(stream, fresh)
     return out, lse

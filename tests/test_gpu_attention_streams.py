@@ -121,3 +121,33 @@ def test_one_layer_on_two_threads(dtype):
     on_threads([lambda i=i: got[i].extend(layer(inputs[i], views) for _ in range(20)) for i in (0, 1)])
     for i in (0, 1):
         assert all(torch.equal(y, alone[i]) for y in got[i])
+
+
+@pytest.mark.parametrize("how", ["current", "argument", "handle", "both"])
+def test_a_plan_dropped_while_another_stream_reads_it(gc, how):
+    """Made under one stream, used on another that is behind, and dropped: its
+    memory is not handed out again while the call has yet to read the items."""
+    n, H, D = 700, 4, 64
+    q, k, v = heads(n, H, H, D, 7)
+    home, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(home):
+        plan = gc.gc_attention_plan([n], [n], H, H, D, torch.bfloat16, device=DEV)
+    want = gc.gc_attention(q, k, v, plan)
+    with torch.cuda.stream(home):
+        plan = gc.gc_attention_plan([n], [n], H, H, D, torch.bfloat16, device=DEV)
+    torch.cuda.synchronize()
+    given = {"current": None, "argument": other, "handle": other.cuda_stream, "both": other}[how]
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(20_000_000)
+        if how in ("current", "both"):
+            got = gc.gc_attention(q, k, v, plan, stream=given)
+    if how in ("argument", "handle"):
+        got = gc.gc_attention(q, k, v, plan, stream=given)
+    at, size = plan.items.data_ptr(), plan.items.numel()
+    del plan
+    with torch.cuda.stream(home):
+        later = [torch.empty(size, dtype=torch.int32, device=DEV) for _ in range(4)]
+    assert not other.query()
+    assert at not in [t.data_ptr() for t in later]
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
