@@ -83,6 +83,10 @@ class MultiViewAttention:
     def __call__(self, x: torch.Tensor, views: Sequence[int]) -> torch.Tensor:
         """x [B, len(views), H, W, width] of the layer's type -> the layer's
         output on foreground tokens, zeros on the background."""
+        shape = (self.B, len(views), self.H, self.W, self.width)
+        if x.shape != shape or x.dtype != self.dtype or x.device != self.foreground.device:
+            raise ValueError(f"x must be {self.dtype} {list(shape)} on {self.foreground.device} (got {x.dtype} "
+                             f"{list(x.shape)} on {x.device})")
         s = self.slice(views)
         H, Hk, D = self.heads, self.kv_heads, self.dim
         tokens = x.reshape(-1, self.width)[s.index]

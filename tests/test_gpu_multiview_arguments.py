@@ -1,0 +1,45 @@
+"""What the multi-view attention layer takes and refuses."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def layer_for(B=2, N=5, H=6, W=8, width=32, dtype=torch.bfloat16, background=True):
+    from paper_2608_13255_amd.multiview import MultiViewAttention
+    g = gen(1)
+    pos = torch.randn((B, N, H, W, 3), generator=g, device=DEV)
+    if background:
+        pos[torch.rand((B, N, H, W), generator=g, device=DEV) < 0.4] = float("nan")
+    return MultiViewAttention(pos, width, 4, 2, 32, dtype, generator=g)
+
+
+def hidden(layer, n, seed=2):
+    shape = (layer.B, n, layer.H, layer.W, layer.width)
+    return torch.randn(shape, generator=gen(seed), device=DEV).to(layer.dtype)
+
+
+@pytest.mark.parametrize("shape", [
+    (2, 5, 6, 8, 32),      # all views' states with two of them named
+    (2, 1, 6, 8, 32), (1, 2, 6, 8, 32), (2, 2, 5, 8, 32), (2, 2, 6, 7, 32), (2, 2, 8, 6, 32), (2, 2, 6, 8, 16),
+    (2, 2, 6, 8, 64), (2, 2, 48, 32), (2, 2, 6, 8, 32, 1), (0, 2, 6, 8, 32)], ids=str)
+def test_other_shapes_are_refused(shape):
+    layer = layer_for()
+    with pytest.raises(ValueError, match="x must be"):
+        layer(torch.zeros(shape, dtype=layer.dtype, device=DEV), [1, 4])
+
+
+def test_other_types_and_devices_are_refused():
+    layer = layer_for()
+    x = hidden(layer, 2)
+    for bad in (x.float(), x.half(), x.cpu()):
+        with pytest.raises(ValueError, match="x must be"):
+            layer(bad, [1, 4])
+    assert layer(x, [1, 4]).shape == x.shape
