@@ -68,6 +68,8 @@ class MultiViewAttention:
         """The tokens of a list of views, built on first use (one read-back of
         the assets' token counts)."""
         key = tuple(int(v) for v in views)
+        if any(not 0 <= v < self.N for v in key):
+            raise ValueError(f"views must lie in [0, {self.N}) (got {list(key)})")
         got = self._slices.get(key)
         if got is None:
             fg = self.foreground[:, list(key)]                            # [B, n, H, W]

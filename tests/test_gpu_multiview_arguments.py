@@ -43,3 +43,17 @@ def test_other_types_and_devices_are_refused():
         with pytest.raises(ValueError, match="x must be"):
             layer(bad, [1, 4])
     assert layer(x, [1, 4]).shape == x.shape
+
+
+@pytest.mark.parametrize("views", [[-1], [1, -5], [5], [0, 1, 7]], ids=str)
+def test_views_outside_the_set_are_refused(views):
+    layer = layer_for()
+    with pytest.raises(ValueError, match="views must lie"):
+        layer.slice(views)
+    with pytest.raises(ValueError, match="views must lie"):
+        layer(hidden(layer, len(views)), views)
+
+
+def test_no_views():
+    layer = layer_for()
+    assert layer(hidden(layer, 0), []).shape == (2, 0, 6, 8, 32)
