@@ -97,6 +97,6 @@ class MultiViewAttention:
         gc_qk_norm_rope(q, k, self.q_gain, self.k_gain, s.positions, self.table, sections=self.sections,
                         layout=GC_ROPE_HALF, q_out=q, k_out=k)            # where the projection left them
         out, _ = gc_attention(q, k, v, s.plan)
-        y = torch.zeros_like(x)
+        y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)          # (zeros_like keeps a permuted x's order)
         y.view(-1, self.width)[s.index] = out.view(-1, H * D) @ self.w_out
         return y

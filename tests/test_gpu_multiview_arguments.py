@@ -57,3 +57,16 @@ def test_views_outside_the_set_are_refused(views):
 def test_no_views():
     layer = layer_for()
     assert layer(hidden(layer, 0), []).shape == (2, 0, 6, 8, 32)
+
+
+@pytest.mark.parametrize("order", [(0, 1, 4, 2, 3), (4, 0, 1, 2, 3), (1, 0, 2, 3, 4)], ids=str)
+def test_hidden_states_in_another_order(order):
+    """Dense states whose channels, or views, lie elsewhere in memory: as the contiguous ones, bit for bit."""
+    layer = layer_for()
+    x = hidden(layer, 3)
+    other = x.permute(order).contiguous().permute([order.index(i) for i in range(5)])
+    assert torch.equal(other, x) and not other.is_contiguous()
+    assert torch.equal(layer(other, [3, 0, 2]), layer(x, [3, 0, 2]))
+    wide = torch.full((2, 3, 6, 8, 40), float("nan"), dtype=x.dtype, device=DEV)
+    wide[..., 4:36] = x
+    assert torch.equal(layer(wide[..., 4:36], [3, 0, 2]), layer(x, [3, 0, 2]))
