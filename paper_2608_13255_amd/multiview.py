@@ -8,19 +8,22 @@ form one sequence, the assets' sequences lie end to end without padding, and a
 token's rotary position is its (view, row, column) in the full set of views.
 
 What follows from the views alone (token indexes, positions, the attention
-plan) is built on first use and kept by the list of views, as the runner keeps
-its correspondence operators: a rotation has few distinct anchor sets, and a
-denoiser has many layers and steps for each of them.
+plan) is built on first use and kept by the list of views for a layer's later
+steps, as the runner keeps its correspondence operators.  A layer keeps the
+lists used last, as many as a rotation of the most views has distinct sets:
+an adaptive choice of anchors seldom repeats one.
 """
 from __future__ import annotations
 
 import math
-from dataclasses import dataclass
-from typing import Dict, List, Optional, Sequence, Tuple
+from collections import OrderedDict
+from dataclasses import dataclass, field
+from typing import List, Optional, Sequence, Set, Tuple
 
 import torch
 
-from . import (GC_ROPE_HALF, AttentionPlan, gc_attention, gc_attention_plan, gc_qk_norm_rope, gc_rope_table)
+from . import (GC_MAX_VIEWS, GC_ROPE_HALF, AttentionPlan, gc_attention, gc_attention_plan, gc_qk_norm_rope,
+               gc_rope_table)
 
 
 @dataclass
@@ -33,12 +36,28 @@ class TokenSlice:
     lens: List[int]
     positions: torch.Tensor
     plan: AttentionPlan
+    # handles of the streams after whose work torch's allocator reuses the tensors' memory
+    known_streams: Set[int] = field(default_factory=set)
+
+    def used_here(self) -> None:
+        """Work on the current stream reads the slice: its memory stays its
+        own until that is done, also where the slice is dropped before."""
+        stream = torch.cuda.current_stream(self.index.device)
+        if stream.cuda_stream not in self.known_streams:
+            self.index.record_stream(stream)
+            self.positions.record_stream(stream)
+            self.known_streams.add(stream.cuda_stream)
+
+    def __getstate__(self):   # a copy's memory is another, known on no stream
+        return {**self.__dict__, "known_streams": set()}
 
 
 class MultiViewAttention:
     """softmax(q k) v of each asset's foreground tokens, with per-head RMS
     norms of queries and keys and rotary positions, between a fused input
     projection and an output projection."""
+
+    MOST_SLICES = GC_MAX_VIEWS + 1   # a rotation's distinct sets, and all views
 
     def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int,
                  dtype: torch.dtype = torch.bfloat16, sections: Optional[Sequence[int]] = None, base: float = 10000.0,
@@ -62,15 +81,16 @@ class MultiViewAttention:
         self.w_out = (rand(heads * dim, width) / math.sqrt(heads * dim)).to(dtype)
         self.q_gain = torch.ones(dim, dtype=torch.float32, device=dev)
         self.k_gain = torch.ones(dim, dtype=torch.float32, device=dev)
-        self._slices: Dict[Tuple[int, ...], TokenSlice] = {}
+        self._slices: OrderedDict[Tuple[int, ...], TokenSlice] = OrderedDict()   # the one used last at the end
 
     def slice(self, views: Sequence[int]) -> TokenSlice:
-        """The tokens of a list of views, built on first use (one read-back of
-        the assets' token counts)."""
+        """The tokens of a list of views, built where it is not among the
+        MOST_SLICES lists used last (one read-back of the assets' token
+        counts)."""
         key = tuple(int(v) for v in views)
         if any(not 0 <= v < self.N for v in key):
             raise ValueError(f"views must lie in [0, {self.N}) (got {list(key)})")
-        got = self._slices.get(key)
+        got = self._slices.pop(key, None)   # (each dict operation is whole under threads; at worst a list is built twice)
         if got is None:
             fg = self.foreground[:, list(key)]                            # [B, n, H, W]
             at = fg.nonzero()                                             # asset, place in the list, row, column
@@ -78,8 +98,12 @@ class MultiViewAttention:
             index = ((at[:, 0] * len(key) + at[:, 1]) * self.H + at[:, 2]) * self.W + at[:, 3]
             view = torch.tensor(key, dtype=torch.int64, device=fg.device)[at[:, 1]]
             positions = torch.stack([view, at[:, 2], at[:, 3]], 1).to(torch.int32)
+            # (last: its copy of the items waits for the stream, so any stream may read all of the slice)
             plan = gc_attention_plan(lens, lens, self.heads, self.kv_heads, self.dim, self.dtype, device=fg.device)
-            got = self._slices[key] = TokenSlice(index, lens, positions, plan)
+            got = TokenSlice(index, lens, positions, plan, {torch.cuda.current_stream(fg.device).cuda_stream})
+        self._slices[key] = got
+        while len(self._slices) > self.MOST_SLICES:
+            self._slices.popitem(last=False)
         return got
 
     def __call__(self, x: torch.Tensor, views: Sequence[int]) -> torch.Tensor:
@@ -90,6 +114,7 @@ class MultiViewAttention:
             raise ValueError(f"x must be {self.dtype} {list(shape)} on {self.foreground.device} (got {x.dtype} "
                              f"{list(x.shape)} on {x.device})")
         s = self.slice(views)
+        s.used_here()
         H, Hk, D = self.heads, self.kv_heads, self.dim
         tokens = x.reshape(-1, self.width)[s.index]
         qkv = (tokens @ self.w_qkv).view(-1, H + 2 * Hk, D)

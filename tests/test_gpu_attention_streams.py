@@ -151,3 +151,34 @@ def test_a_plan_dropped_while_another_stream_reads_it(gc, how):
     assert at not in [t.data_ptr() for t in later]
     torch.cuda.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_slice_dropped_while_another_stream_reads_it():
+    """A slice that gives way to others while a stream that is behind has yet
+    to read it: its memory is not handed out again before."""
+    from paper_2608_13255_amd.multiview import MultiViewAttention
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    pos = torch.randn((1, 6, 16, 16, 3), generator=g, device=DEV)
+    layer = MultiViewAttention(pos, 64, 4, 2, 64, generator=g)
+    layer.MOST_SLICES = 2
+    x = torch.randn((1, 2, 16, 16, 64), generator=g, device=DEV).bfloat16()
+    want = layer(x, [0, 1])
+    layer.slice([2, 3]), layer.slice([4, 5])
+    torch.cuda.synchronize()
+    home, other = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(home):
+        s = layer.slice([0, 1])
+    torch.cuda.synchronize()
+    at = [s.index.data_ptr(), s.positions.data_ptr()]
+    del s
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(40_000_000)
+        got = layer(x, [0, 1])
+    with torch.cuda.stream(home):
+        others = [layer.slice(v) for v in ([2, 3], [4, 5], [1, 2], [3, 4])]
+    assert not other.query()
+    assert (0, 1) not in layer._slices
+    assert not set(at) & {t.data_ptr() for o in others for t in (o.index, o.positions)}
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)

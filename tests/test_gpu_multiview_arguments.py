@@ -70,3 +70,33 @@ def test_hidden_states_in_another_order(order):
     wide = torch.full((2, 3, 6, 8, 40), float("nan"), dtype=x.dtype, device=DEV)
     wide[..., 4:36] = x
     assert torch.equal(layer(wide[..., 4:36], [3, 0, 2]), layer(x, [3, 0, 2]))
+
+
+def test_the_lists_used_last_are_kept():
+    layer = layer_for(B=1, N=64, H=2, W=2)
+    most = layer.MOST_SLICES
+    assert most == 65                                     # a rotation of 64 views, and all of them
+    first, second = layer.slice([0]), layer.slice([0, 1])
+    lists = [[a, b] for a in range(1, 64) for b in range(a + 1, a + 3)][:most + 20]
+    for i, views in enumerate(lists):
+        layer.slice(views)
+        if i % 50 == 0:
+            assert layer.slice([0]) is first              # in use again and again
+        assert len(layer._slices) <= most
+    assert layer.slice([0]) is first and layer.slice([0, 1]) is not second
+    assert layer.slice(lists[-1]) is layer.slice(lists[-1])
+    x = hidden(layer, 2)
+    want = layer(x, [0, 1])
+    for views in lists:
+        layer.slice(views)
+    assert (0, 1) not in layer._slices and torch.equal(layer(x, [0, 1]), want)
+
+
+def test_a_copy_of_a_layer():
+    import copy
+    layer = layer_for()
+    x = hidden(layer, 2)
+    want = layer(x, [4, 1])
+    other = copy.deepcopy(layer)
+    assert not other.slice([4, 1]).known_streams          # another memory, whose use no stream's allocator knows
+    assert torch.equal(other(x, [4, 1]), want)
