@@ -1161,6 +1161,9 @@ class AttentionPlan:
         self.items.record_stream(stream)
         self.known_streams.add(handle)
 
+    def __getstate__(self):   # a copy's memory is another, known on no stream
+        return {**self.__dict__, "known_streams": set()}
+
 
 def gc_attention_plan(q_lens: Sequence[int], k_lens: Sequence[int], heads: int, kv_heads: int, dim: int,
                       dtype: torch.dtype, causal: bool = False, device="cuda", stream=None) -> AttentionPlan:

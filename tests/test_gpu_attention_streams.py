@@ -182,3 +182,17 @@ def test_a_slice_dropped_while_another_stream_reads_it():
     assert not set(at) & {t.data_ptr() for o in others for t in (o.index, o.positions)}
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_a_copy_of_a_plan(gc):
+    """The copy's items lie elsewhere: what is known of the original's streams does not hold for them."""
+    import copy
+    n, H, D = 300, 2, 64
+    q, k, v = heads(n, H, H, D, 9)
+    plan = gc.gc_attention_plan([n], [n], H, H, D, torch.bfloat16, device=DEV)
+    want = gc.gc_attention(q, k, v, plan)
+    other = copy.deepcopy(plan)
+    assert plan.known_streams and not other.known_streams
+    got = gc.gc_attention(q, k, v, other)
+    assert other.known_streams
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
