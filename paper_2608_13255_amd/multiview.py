@@ -55,7 +55,9 @@ class TokenSlice:
 class MultiViewAttention:
     """softmax(q k) v of each asset's foreground tokens, with per-head RMS
     norms of queries and keys and rotary positions, between a fused input
-    projection and an output projection."""
+    projection and an output projection.  The forward pass only: a call that
+    torch would record for a gradient is refused.  One layer may be called
+    under several streams and from several threads at the same time."""
 
     MOST_SLICES = GC_MAX_VIEWS + 1   # a rotation's distinct sets, and all views
 
@@ -113,6 +115,8 @@ class MultiViewAttention:
         if x.shape != shape or x.dtype != self.dtype or x.device != self.foreground.device:
             raise ValueError(f"x must be {self.dtype} {list(shape)} on {self.foreground.device} (got {x.dtype} "
                              f"{list(x.shape)} on {x.device})")
+        if torch.is_grad_enabled() and any(t.requires_grad for t in (x, self.w_qkv, self.w_out, self.q_gain, self.k_gain)):
+            raise ValueError("the layer has no gradient: call it under torch.no_grad(), or on tensors that require none")
         s = self.slice(views)
         s.used_here()
         H, Hk, D = self.heads, self.kv_heads, self.dim

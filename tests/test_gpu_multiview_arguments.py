@@ -100,3 +100,21 @@ def test_a_copy_of_a_layer():
     other = copy.deepcopy(layer)
     assert not other.slice([4, 1]).known_streams          # another memory, whose use no stream's allocator knows
     assert torch.equal(other(x, [4, 1]), want)
+
+
+@pytest.mark.parametrize("name", ["x", "w_qkv", "w_out", "q_gain", "k_gain"])
+def test_gradients_are_refused(name):
+    """The layer has no backward pass: it says so, and runs where none is asked for."""
+    layer = layer_for()
+    x = hidden(layer, 2)
+    want = layer(x, [1, 4])
+    if name == "x":
+        x.requires_grad_()
+    else:
+        getattr(layer, name).requires_grad_()
+    with pytest.raises(ValueError, match="no gradient"):
+        layer(x, [1, 4])
+    with torch.no_grad():
+        assert torch.equal(layer(x, [1, 4]), want)
+    with torch.inference_mode():
+        assert torch.equal(layer(x, [1, 4]), want)
