@@ -714,7 +714,8 @@ int gc_qk_norm_rope(const gc_heads* q, int heads, const gc_heads* k, int kv_head
  * over the keys it sees: all of its sequence, or with causal != 0 those with
  * j <= i + k_len - q_len (the last query sees the last key).  A row that sees
  * no key, or only scores of -inf, gets out = 0 and lse = -inf.  What a masked key or
- * value holds, NaN and infinities included, has no effect.
+ * value holds, NaN and infinities included, has no effect.  Where a row sees values that are not
+ * finite, their channel of out is their sum (an infinity, or NaN), however small their weights.
  *
  * gc_attention_plan lays out the work of such a batch (host; no device work):
  * once per set of lengths, whatever the number of layers and steps.  It fills

@@ -59,6 +59,9 @@ __device__ __forceinline__ int place(int row, int chunk) {
 typedef __attribute__((address_space(3))) void LdsVoid;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// The factor of a weighted sum whose maximum falls behind by x (in powers of two): never 0, which would make NaN of a
+// sum of infinity.
+__device__ __forceinline__ float sum_factor(float x) { return fmaxf(exp2_hw(x), 0x1p-149f); }
 
 // The larger of a lane's value and that of the lane 32 away; their sum.
 __device__ __forceinline__ float max_halves(float x) {
@@ -121,6 +124,15 @@ struct TileLoader {
     left -= kKeys * kStep;
   }
 };
+
+// Until at most kLeft of the wave's loads are outstanding.
+template <int kLeft>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(kLeft < 64, "the counter has 6 bits");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((kLeft & 15) | (7 << 4) | (15 << 8) | ((kLeft >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
 
 // A query row: its token, head and the keys that it sees.
 struct RowOf {
@@ -485,6 +497,77 @@ __device__ __forceinline__ void add_nonfinite(const AttentionArgs& p, const Atte
     }
 }
 
+// Whether one of a lane's sums is not finite: 0 times any of them is 0 else.
+template <class C>
+__device__ __forceinline__ bool any_nonfinite(const C& core) {
+  float x = 0.f;
+#pragma unroll
+  for (int d = 0; d < C::kOut; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x = __builtin_fmaf(core.o[d][i], 0.f, x);
+  return x != x;
+}
+
+// Values that are not finite leave infinity or NaN in their channel: NaN also
+// where a row's weight, against the maximum in use at the time, underflowed to
+// 0.  A row's channel is to hold the sum of such values that it sees, however
+// small their weights, so the channels that are NaN are looked up again.  Not
+// where l is NaN: the row's scores are.
+// Keys [first, end), of which `keys` (at most 64) of every `step` are this
+// wave's; each lane looks at one of them, the last ones first (the masked
+// tiles' have just been added).
+template <class T, class C>
+__device__ __forceinline__ void settle_nonfinite(const AttentionArgs& p, const AttentionItem& it, int kv_head, C& core, float l,
+                                                 int first, int end, int keys, int step, int limit, int lane) {
+  const auto is_nan = [](float x) { return x != x; };
+  if (first >= end || __builtin_expect(!__any(any_nonfinite(core) && !is_nan(l)), 1)) return;
+  const T* values = (const T*)p.v + (int64_t)it.k_token0 * p.v_token + kv_head * p.v_head;
+  for (int n = 0; 8 * n < p.dim; ++n) {   // channels 8 n .. 8 n + 7, the lane's own from 8 n + 4 half
+    float o[4];
+#pragma unroll
+    for (int i = 0; i < 4 * C::kOut; ++i)
+      if (i == n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = core.o[i / 4][i % 4 * 4 + j];
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t hit = 0;
+    const auto open = [&] {
+      bool x = false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x |= is_nan(o[j]) && !is_nan(sum[j]);
+      return __any(x && !is_nan(l)) != 0;
+    };
+    for (int key0 = first + (end - 1 - first) / step * step; key0 >= first && open(); key0 -= step) {
+      const int mine = key0 + lane;
+      bool some = false;
+      if (lane < keys && mine < end) {
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) {
+          float x[4];
+          load_heads<4>(values + (int64_t)mine * p.v_token + 8 * n + j, x);
+          some |= !(finite_f(x[0]) && finite_f(x[1]) && finite_f(x[2]) && finite_f(x[3]));
+        }
+      }
+      for (uint64_t left = __ballot(some); left; left &= left - 1) {
+        const int key = key0 + __builtin_ctzll(left);
+        float x[4];
+        load_heads<4>(values + (int64_t)key * p.v_token + 8 * n + 4 * (lane >> 5), x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (key < limit && !finite_f(x[j])) sum[j] += x[j], hit |= 1u << j;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * C::kOut; ++i)
+      if (i == n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (is_nan(o[j]) && (hit >> j & 1)) core.o[i / 4][i % 4 * 4 + j] = sum[j];
+  }
+  // (else the compiler waits for these loads, and so for earlier stores, between the stores of the results)
+  wait_loads<0>();
+}
+
 // Masked places' scores.
 template <int kKeyBlocks>
 __device__ __forceinline__ void mask(Scores<kKeyBlocks>& s, int key0, int limit, int lane) {
@@ -510,7 +593,7 @@ constexpr float kSlack = 8.f;
 
 template <class C>
 __device__ __forceinline__ void rescale(C& core, bool grown, float top) {
-  const float f = grown ? exp2_hw(core.m - top) : 1.f;
+  const float f = grown ? sum_factor(core.m - top) : 1.f;
   if (grown) core.m = top;
   core.l *= f;
 #pragma unroll

@@ -8,15 +8,6 @@
 
 namespace gc {
 
-// Until at most kLeft of the wave's loads are outstanding.
-template <int kLeft>
-__device__ __forceinline__ void wait_loads() {
-  static_assert(kLeft < 64, "the counter has 6 bits");
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((kLeft & 15) | (7 << 4) | (15 << 8) | ((kLeft >> 4) << 14));
-  asm volatile("" ::: "memory");
-}
-
 // Until the wave's reads of LDS have arrived.
 __device__ __forceinline__ void wait_lds() {
   asm volatile("" ::: "memory");
@@ -121,7 +112,7 @@ __global__ __launch_bounds__(kJoin) void k_attention_join(const AttentionArgs p,
     for (int i = 0; i < 4; ++i) {
       if (i0 + i >= it.parts) continue;
       const float mn = fmaxf(m, x[i].x), ms = mn == -__builtin_inff() ? 0.f : mn;
-      const float f = exp2_hw(m - ms), g = exp2_hw(x[i].x - ms);
+      const float f = sum_factor(m - ms), g = sum_factor(x[i].x - ms);
       m = mn;
       l = l * f + x[i].y * g;
 #pragma unroll
@@ -291,8 +282,10 @@ __device__ __forceinline__ void attention_rows(const AttentionArgs& p) {
     if (key0 - kKeys < high) bad |= core.add_masked(phase == 0 ? v3 : phase == 1 ? v0 : phase == 2 ? v1 : v2, lane, w);
   }
 
+  const float l = sum_halves(core.l);
   if (__any(bad != 0)) add_nonfinite<T>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
-  store_rows<T, kDim>(p, it, kv_head, core, sum_halves(core.l), first_row, kRows, lane);
+  settle_nonfinite<T>(p, it, kv_head, core, l, it.k_begin, high, 64, 64, limit, lane);
+  store_rows<T, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
 }
 
 template <int kDim, int kKeyBlocks, int kWaves, int kPerSimd>
@@ -376,8 +369,10 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
   }
   wait_loads<0>();   // before the block's LDS is given up
 
+  const float l = sum_halves(core.l);
   if (__any(bad != 0)) add_nonfinite<float>(p, it, kv_head, core, first_masked, high, kKeys, kKeys, limit, lane);
-  store_rows<float, kDim>(p, it, kv_head, core, sum_halves(core.l), first_row, kRows, lane);
+  settle_nonfinite<float>(p, it, kv_head, core, l, it.k_begin, high, 64, 64, limit, lane);
+  store_rows<float, kDim>(p, it, kv_head, core, l, first_row, kRows, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -388,7 +383,7 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
 // 85 us, 5.8 TB/s where a large read reaches 7.0, and 5 us for the join.
 // ---------------------------------------------------------------------------
 template <class T, int kDim, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionArgs p) {
+__global__ __launch_bounds__(64 * kWaves, kDim * sizeof(T) <= 64 ? 4 : 1) void k_attention_keys(const AttentionArgs p) {
   constexpr int kKeys = 32, kTile = kKeys * kDim * (int)sizeof(T);
   // the loads that may be outstanding where a tile is needed: the three asked for after it (the counter's
   // range is 63: where they are more, a few of them are waited for too)
@@ -457,8 +452,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
   for (; key0 < high; key0 += kStep) bad |= tile(key0, std::true_type{});
   if (__any(bad != 0))
     add_nonfinite<T>(p, it, kv_head, core, first_masked, high, kKeys, kWaves * kKeys, limit, lane);
-  // the waves' results, added by the first wave in their order
   float l = sum_halves(core.l);
+  settle_nonfinite<T>(p, it, kv_head, core, l, first, high, kKeys, kStep, limit, lane);
+  // the waves' results, added by the first wave in their order
   wait_loads<0>();   // (also before the block's LDS is given up)
   if constexpr (kWaves > 1) {
     float* o = reinterpret_cast<float*>(mine);
@@ -482,7 +478,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_attention_keys(const AttentionA
 #pragma unroll
         for (int i = 0; i < 16; ++i) core.o[d][i] = 0.f;
       for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2_hw(ml[w][lane & 31][0] - ms);
+        const float f = sum_factor(ml[w][lane & 31][0] - ms);
         l += ml[w][lane & 31][1] * f;
         const float* x = reinterpret_cast<const float*>(lds + w * 4 * kTile);
 #pragma unroll
