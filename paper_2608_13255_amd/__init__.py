@@ -983,9 +983,6 @@ def gc_sampler_alpha_bar(sampler: Sampler, t: int) -> float:
     return out.value
 
 
-lib()
-
-
 # ---------------------------------------------------------------------------
 # operators of the denoiser's own blocks
 # ---------------------------------------------------------------------------
@@ -1245,3 +1242,6 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
                               1.0 / math.sqrt(D) if scale is None else scale, at, size, handle), "gc_attention")
     _keep(stream, fresh)
     return out, lse
+
+
+lib()

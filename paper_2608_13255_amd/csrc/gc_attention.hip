@@ -279,8 +279,8 @@ extern "C" int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads
   }
   p.out = out->data, p.o_token = out->token_stride, p.o_head = out->head_stride;
   p.lse = lse;
-  p.heads = info->heads, p.kv_heads = info->kv_heads, p.group = info->heads / info->kv_heads, p.dim = dim;
-  p.total_q = info->total_q, p.total_k = info->total_k;
+  p.kv_heads = info->kv_heads, p.group = info->heads / info->kv_heads, p.dim = dim;
+  p.total_q = info->total_q;
   p.causal = info->causal;
   p.scale = (float)scale;
   if (info->n_slots > 0) p.partial = reinterpret_cast<float*>(workspace);

@@ -37,8 +37,8 @@ struct AttentionArgs {
   float* lse;
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;
   const AttentionItem* items;
-  int heads, kv_heads, group, dim;
-  int total_q, total_k;
+  int kv_heads, group, dim;
+  int total_q;
   int causal;
   float scale;
   float* partial;       // per slot and kv head: [tile_rows][dim padded] weighted sums, then [tile_rows][2] maxima and sums

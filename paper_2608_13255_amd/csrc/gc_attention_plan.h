@@ -20,7 +20,7 @@ struct AttentionItem {
   int32_t slot;       // this part's partial result, -1: the item holds all of its rows' keys
   int32_t slot0;      // the tile's first part
   int32_t parts;      // its number of parts
-  int32_t group_id;   // its number among the split tiles
+  int32_t group_id;   // its number among the split tiles (host: what info counts as n_groups)
 };
 static_assert(sizeof(AttentionItem) == GC_ATTENTION_ITEM_WORDS * 4, "item words");
 
@@ -36,15 +36,10 @@ inline int attention_padded_dim(int dim) {
 // Whether two waves' rows a SIMD fit the registers with eight waves a block.
 inline bool attention_has_rows256(int dim, int dtype) { return dtype == GC_BF16 && attention_padded_dim(dim) <= 128; }
 
-// The waves of a block of kAttnKeys: two tiles of 32 keys and values each, in
-// at most 128 KiB; and the blocks of a compute unit (160 KiB of LDS).
+// The waves of a block of kAttnKeys: two tiles of 32 keys and two of values
+// for each of them, in at most 128 of a compute unit's 160 KiB of LDS.
 constexpr int attention_keys_waves(int padded, int bytes) {
   return padded * bytes <= 256 ? 4 : padded * bytes <= 512 ? 2 : 1;
-}
-inline int attention_keys_blocks(int dim, int dtype) {
-  const int row = attention_padded_dim(dim) * dtype_bytes(dtype);
-  const int lds = attention_keys_waves(row, 1) * (4 * 32 * row + 256) + 64;
-  return 163840 / lds < 4 ? 163840 / lds : 4;
 }
 
 struct AttentionArgs;
