@@ -628,9 +628,11 @@ int gc_sampler_alpha_bar(const gc_sampler* smp, int t, double* abar);
  * contiguous, tokens and heads have strides of their own (in elements), so a
  * part of a fused projection's output is read or written where it lies.  The
  * data pointer must be 16-byte aligned and both strides a multiple of 16
- * bytes (GC_ERR_ALIGN).  Storage is GC_F32 or GC_BF16; arithmetic is float32
- * with one rounding at the end.  dim is a multiple of 8, at most
- * GC_MAX_HEAD_DIM; a tensor has at most GC_MAX_HEADS heads.
+ * bytes (GC_ERR_ALIGN); token strides are 0 to 2^22 elements, head strides 0 to 2^40 (GC_ERR_SHAPE), and no two
+ * elements of an output may share memory.  Storage is GC_F32 or GC_BF16; arithmetic is float32
+ * with one rounding at the end, but for one more in gc_attention: with GC_BF16 the weights exp(s_j - max s) are rounded to
+ * bfloat16 before they multiply the values (not in the sum l).  dim is a multiple of 8, at most
+ * GC_MAX_HEAD_DIM; a tensor has at most GC_MAX_HEADS heads.  There is no backward pass.
  */
 #define GC_MAX_HEAD_DIM 256
 #define GC_MAX_HEADS 1024
@@ -725,7 +727,8 @@ int gc_qk_norm_rope(const gc_heads* q, int heads, const gc_heads* k, int kv_head
  *   heads a multiple of kv_heads; dim a multiple of 8
  *
  * gc_attention runs it.
- *   q, out   [sum of q_lens][heads][dim];  k, v  [sum of k_lens][kv_heads][dim]
+ *   q, out   [sum of q_lens][heads][dim];  k, v  [sum of k_lens][kv_heads][dim], whose tokens may not share memory
+ *            (token strides of at least dim; heads may)
  *   lse      device float [heads][sum of q_lens], or NULL
  *   info     host, as gc_attention_plan filled it
  *   items    device int32, a copy of the plan's items, 16-byte aligned

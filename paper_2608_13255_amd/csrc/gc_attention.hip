@@ -9,13 +9,13 @@
 // operations a head and visible pair: single tokens are bound by the read,
 // everything else by the operations.  Measured, us, with the time of the
 // bound at a large read's 7.0 TB/s or a large product's 1378 (bfloat16) and
-// 153 (float32) TFLOP/s:
+// 153 (float32) TFLOP/s (boxes differ by up to 7 %: the slowest took 152, 527, 712 and 4311 for the last four):
 //   8 single tokens, 32 heads on 8 of 128, 495 MB of keys and values     90   71
 //   1024 + 1 + 517 + 770 tokens, 8 heads of 64, float32                  51   25
-//   10403 tokens in 4 sequences, 16 heads of 64, among themselves       148   83
-//   the same over 31070 keys, 16 heads of 80 (worked on as 96)          508  308
-//   15427 causal tokens in 7 sequences, 32 heads on 8 of 128            677  527
-//   24576 tokens, 16 heads of 128                                      4054 3592
+//   10403 tokens in 4 sequences, 16 heads of 64, among themselves       145   83
+//   the same over 31070 keys, 16 heads of 80 (worked on as 96)          504  308
+//   15427 causal tokens in 7 sequences, 32 heads on 8 of 128            672  527
+//   24576 tokens, 16 heads of 128                                      4048 3592
 #include <algorithm>
 #include <cmath>
 #include <exception>
@@ -62,7 +62,8 @@ void each_tile(const Batch& b, int tile, F f) {
 // What a variant takes, in microseconds, from timings on a full card: a block
 // alone on its compute unit goes through `rate` keys a microsecond, two that
 // share one through `share` times as many together; a block's first loads
-// and its results take kBlockTime.
+// and its results take kBlockTime.  (kAttnKeys by the bytes that it reads, also in float32 above 64 channels, where its
+// products take longer: its parts then differ in length alone.)
 struct Cost {
   int kind;
   double rate, share;

@@ -146,14 +146,15 @@ void launch_join(const AttentionArgs& p, int tile_rows, unsigned blocks, hipStre
 // of i + 2 are asked for in their places.  The next barrier waits for that K
 // and for the V asked for a tile before; the last V may be outstanding.
 //
-// What bounds it: with 64 channels the issue of both kinds (a SIMD's vector
-// unit is busy 55 % of the time, its matrix unit 34 %; a lone wave takes 34
+// What bounds it: with 64 channels the issue of both kinds (while a compute
+// unit has work its vector units are busy 67 % of the time, its matrix units 41 %; a lone wave takes 34
 // cycles for a product, 46 for four multiply-adds, two exponentials and a
-// conversion, and 54 for all), with 128 the power that the products draw (busy 54 % and 65 %, the
+// conversion, and 54 for all) and the launch's incomplete last round (688 blocks for 256 compute units that hold one
+// each: 2.7 rounds take 3), with 128 the power that the products draw (busy 56 % and 67 %, the
 // clock at 1.8 of 2.4 GHz; the products alone take 2.9 of the 4.1 ms).
 // 64 keys a tile up to 128 channels, 32 above (and with four waves a block
 // above 96): what registers and LDS hold.  24576 tokens x 16 heads x 128: 4.1
-// ms, 1220 TFLOP/s; 10403 tokens in four sequences x 16 x 64: 148 us.  Not faster (against 4.27 ms and 707 us at the time):
+// ms, 1220 TFLOP/s; 10403 tokens in four sequences x 16 x 64: 145 us (boxes differ by up to 7 %).  Not faster (against 4.27 ms and 707 us at the time):
 // halves of the block that take turns at products and vector work, with a
 // barrier a part (4.36 ms, causal 810 us); 32 keys a tile at three waves a SIMD for 64 channels
 // (1213 us against 1154); weights against a maximum that only the sum checks
@@ -298,8 +299,9 @@ __global__ __launch_bounds__(64 * kWaves, kPerSimd) void k_attention_rows(const 
 // tile's parts follow one another and the blocks of a compute unit (or its
 // four waves) fill the gaps.  Two places for K and V each: one tile is worked
 // on while the next arrives.  1024 + 1 + 517 + 770 tokens x 8 heads x 64: 51
-// us, of which the parts' join takes 7 (the matrix units are busy 55 % of the
-// first launch: 256 blocks for 256 compute units, no second one to fill gaps).
+// us, of which the parts' join takes 7.  There two blocks share a compute unit
+// (512 for 256), and while one has work its matrix units are busy 74 % of the time: two waves
+// a SIMD do not fill the gaps between scores, weights and values, and each tile has a barrier.
 // Slower: the next tile's scores beside this tile's weights (60 us; 2000
 // tokens x 8 x 256 404 against 289): the compiler then waits for the loads to
 // LDS inside a tile.
@@ -380,7 +382,10 @@ __global__ __launch_bounds__(256, kPerSimd) void k_attention_rows_f32(const Atte
 // and take tiles of 32 keys in turn, each with two tiles of its own in LDS
 // and no barrier until the end, where their results are added.  Bound by the
 // read of the keys and values: 495 MB for 8 tokens (32 heads on 8 of 128) in
-// 85 us, 5.8 TB/s where a large read reaches 7.0, and 5 us for the join.
+// 84 us, 5.9 TB/s where a large read reaches 7.0, and 5 us for the join.  Not
+// so in float32 above 64 channels, where two waves or one a compute unit are bound by their products on 32 rows:
+// 16 tokens (32 heads on 8) over 4096 keys each take 54, 144, 379 and 1065 us
+// at 64, 128, 192 and 256 channels (the last spills), where the reads take 38, 77, 115 and 153.
 // ---------------------------------------------------------------------------
 template <class T, int kDim, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, kDim * sizeof(T) <= 64 ? 4 : 1) void k_attention_keys(const AttentionArgs p) {

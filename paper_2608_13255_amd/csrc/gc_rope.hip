@@ -9,11 +9,12 @@
 //
 // Memory-bound: each value is read and written once, about 3 operations a
 // value (7 with the norm) against 4 or 8 bytes.  What counted: all of a
-// wave's loads issued before anything waits, the sixteen bytes of
+// wave's loads of heads issued before anything waits (the table's row and the norm's gains follow), the sixteen bytes of
 // neighbouring lanes side by side, and arguments chosen between queries
 // and keys in scalar registers.  196608 tokens x 32 heads x 128 bfloat16 with the
-// norms: 535 us (6.0 TB/s of a copy's 6.5); 196608 x 16 x 128, 64 channels turned: 289 us
-// (5.8 TB/s); 13823 x 16 x 64 float: 20.7 us (5.5 TB/s).
+// norms: 538 us (6.0 TB/s of a copy's 6.5); 196608 x 16 x 128, 64 channels turned: 289 us
+// (5.8 TB/s); 13823 x 16 x 64 float: 20.7 us (5.5 TB/s).  The table, in double: 4096 x 64 columns 5.2 us, 393216 x 64
+// 107 us (1.9 TB/s written: bound by the sines and cosines), scaled 136.
 #include <type_traits>
 
 #include "gc_heads.h"
