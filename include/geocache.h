@@ -698,7 +698,7 @@ int gc_rope(const gc_heads* x, int64_t n_tokens, int heads, int dim, int dtype, 
  * in one pass: y = x / sqrt(mean over dim of x^2 + eps) * gain, turned.
  *   q, q_out  [n_tokens][heads][dim];  k, k_out  [n_tokens][kv_heads][dim]
  *   q_gain, k_gain  device float [dim], 16-byte aligned
- *   eps       finite, >= 0
+ *   eps       finite, >= 0; as a float32 finite, and 0 only if it is 0
  * An output may be its own input; it may otherwise share no byte with an
  * input or the other output (columns of one fused buffer are apart).
  */

@@ -428,7 +428,9 @@ extern "C" int gc_qk_norm_rope(const gc_heads* q, int heads, const gc_heads* k, 
   RopeArgs p = {};
   rc = make_rope(&p, n_tokens, dim, positions, table, n_pos, sections, n_axes, layout, who);
   if (rc) return rc;
-  if (!(eps >= 0.0) || !__builtin_isfinite(eps)) return fail(GC_ERR_ARG, "%s: eps must be finite and not negative", who);
+  // (an eps that float32 rounds to 0 would make NaN of heads of zeros, one that it rounds to infinity would make 0 of all)
+  if (!(eps >= 0.0) || !__builtin_isfinite((float)eps) || (eps > 0.0 && (float)eps == 0.f))
+    return fail(GC_ERR_ARG, "%s: eps=%g must be finite and not negative, and as a float32 neither infinite nor 0 unless it is 0", who, eps);
   if (n_tokens == 0) return GC_OK;
   if (!q_gain || !k_gain) return fail(GC_ERR_ARG, "%s: a gain is null", who);
   if (!aligned16(q_gain) || !aligned16(k_gain)) return fail(GC_ERR_ALIGN, "%s: gains must be 16-byte aligned", who);

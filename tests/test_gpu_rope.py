@@ -235,3 +235,12 @@ def test_more_tokens_than_a_launch_has_threads_for(gc):
     gc.gc_rope(x, pos, table, out=x)
     assert torch.equal(x[rows], want)
     assert int(torch.count_nonzero(x.view(T, D).any(dim=1))) == rows.numel()
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-30, 1e-6])
+def test_rows_of_zeros_with_a_small_eps(gc, eps):
+    z = torch.zeros((2, 1, 32), device=DEV)
+    gain = torch.ones(32, device=DEV)
+    pos = torch.zeros(2, dtype=torch.int32, device=DEV)
+    q, k = gc.gc_qk_norm_rope(z, z, gain, gain, pos, table_for(gc, 1, [16]), eps=eps)
+    assert torch.equal(q, z) and torch.equal(k, z)

@@ -316,3 +316,15 @@ def test_attention_plan_without_host_memory(gc, L):
     done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=Path(__file__).parent.parent)
     assert done.returncode == 0, done.stderr
     assert done.stdout.startswith(f"{CODE['CAPACITY']} ") and "host memory" in done.stdout, done.stdout
+
+
+def test_norm_eps_in_float32(gc, L):
+    """An eps that float32 rounds to 0 would make NaN of heads of zeros (0 / sqrt(eps) is 0), one that it rounds to infinity 0 of all."""
+    t = [heads(gc, a) for a in (A[0], A[1], A[7], A[8])]
+    for eps in (1e-60, 5e-324, 7e-46, 3.5e38, 1e300):
+        refused(L, L.gc_qk_norm_rope(ctypes.byref(t[0]), 4, ctypes.byref(t[1]), 4, 10, 64, 1, A[5], A[6], eps, A[3], A[4], 16,
+                                     i32(32), 1, 0, ctypes.byref(t[2]), ctypes.byref(t[3]), None), "ARG", "eps")
+    # up to the gain's check (missing here) these are taken
+    for eps in (0.0, 1e-45, 1e-6, 3e38):
+        refused(L, L.gc_qk_norm_rope(ctypes.byref(t[0]), 4, ctypes.byref(t[1]), 4, 10, 64, 1, None, A[6], eps, A[3], A[4], 16,
+                                     i32(32), 1, 0, ctypes.byref(t[2]), ctypes.byref(t[3]), None), "ARG", "gain")
