@@ -28,6 +28,9 @@
  *   inside the denoiser  gc_rope_table, gc_rope   rotary positions of a slice of the views' tokens
  *                        gc_qk_norm_rope        per-head norms of queries and keys with the rotation
  *                        gc_attention_plan, gc_attention   attention over packed sequences
+ *                        gc_add_rms_norm        norm of the residual stream's sum, in 8 bits with scales if wanted
+ *                        gc_quantize_rows       rows in 8 bits with a scale each
+ *                        gc_linear              matrix product with bias, activation, gate and residual
  *
  * Conventions shared by every call
  *   - Every call returns GC_OK (0) or a negative GC_ERR_* code and never
@@ -759,6 +762,85 @@ int gc_attention_plan(const int32_t* q_lens, const int32_t* k_lens, int n_seq, i
 int gc_attention(const gc_heads* q, const gc_heads* k, const gc_heads* v, const gc_heads* out, float* lse,
                  const gc_attention_info* info, const int32_t* items, double scale, void* workspace, size_t ws_bytes,
                  hipStream_t stream);
+
+/*
+ * What a block of the denoiser runs around its attention: norms of the
+ * residual stream, and matrix products.
+ *
+ * Rows are matrices [rows][columns] described by gc_rows: columns are
+ * contiguous, rows have a stride (in elements, not negative; an input's may be 0 or
+ * less than its columns, an output's rows share no memory).  Storage is GC_F32, GC_BF16 or
+ * GC_E4M3 (8 bits: sign, 4 of exponent, 3 of mantissa, largest 448, no
+ * infinities).  Arithmetic, sums and statistics are float32, with one
+ * rounding (to nearest, ties to even) where a result is stored.  Pointers are aligned to their elements, scales, gains and
+ * biases to 4 bytes (GC_ERR_ALIGN).  rows = 0 is legal and does nothing.  There is no backward pass.
+ */
+#define GC_E4M3 2
+#define GC_MAX_WIDTH 32768   /* columns of gc_add_rms_norm and gc_quantize_rows */
+#define GC_MAX_INNER 1048576 /* n_in of gc_linear, and strides of its x and w */
+
+typedef struct gc_rows {
+  void* data;
+  int64_t stride;
+} gc_rows;
+
+/*
+ * h = x + residual;  total = h;  out = h / sqrt(mean over a row of h^2 + eps) * gain
+ * With out_dtype GC_E4M3 each row has a scale: with y as above,
+ *   out_scale = max(largest |y| of the row, 448 * 2^-126) / 448,  out = y / out_scale;
+ * a row in which some y is not finite has scale NaN and NaN throughout.
+ * The norm is of h before it is rounded to be stored.  Squares are summed in float32: a row whose
+ * values are near 10^19 or above, or near 10^-19 or below with eps = 0, is out of that sum's range.
+ *   x, residual, total  [n_rows][width] of dtype GC_F32 or GC_BF16; residual NULL: none; total NULL: not stored
+ *   gain       device float [width], NULL: ones
+ *   eps        finite, >= 0; as a float32 finite, and 0 only if it is 0
+ *   out        [n_rows][width] of out_dtype: dtype or GC_E4M3
+ *   out_scale  device float [n_rows] with GC_E4M3, else NULL
+ * total and, where it has their type, out may be x or residual itself (the same pointer and
+ * stride), and may otherwise share no byte with an input or another output
+ * (columns of one buffer are apart).
+ */
+int gc_add_rms_norm(const gc_rows* x, const gc_rows* residual, int64_t n_rows, int width, int dtype, const float* gain,
+                    double eps, const gc_rows* total, const gc_rows* out, int out_dtype, float* out_scale,
+                    hipStream_t stream);
+
+/*
+ * Rows in 8 bits: out_scale and out as gc_add_rms_norm has them, with y = x.
+ *   x    [n_rows][width] of dtype GC_F32 or GC_BF16;  out  GC_E4M3 [n_rows][width];  out_scale  device float [n_rows]
+ */
+int gc_quantize_rows(const gc_rows* x, int64_t n_rows, int width, int dtype, const gc_rows* out, float* out_scale,
+                     hipStream_t stream);
+
+/* activations of gc_linear: p;  p / (1 + e^-p);  p (1 + erf(p / sqrt 2)) / 2;
+ * p (1 + tanh(sqrt(2 / pi) (p + 0.044715 p^3))) / 2 */
+#define GC_ACT_NONE 0
+#define GC_ACT_SILU 1
+#define GC_ACT_GELU 2
+#define GC_ACT_GELU_TANH 3
+
+/*
+ * Matrix product with what follows it:
+ *   p[i][j] = x_scale[i] * w_scale[j] * sum over k of x[i][k] w[j][k] + bias[j]
+ *   out[i][j] = act(p[i][j]) + residual[i][j]
+ * and with gated != 0, where w, w_scale and bias have 2 n_out rows,
+ *   out[i][j] = act(p[i][j]) * p[i][n_out + j] + residual[i][j].
+ *   x         [n_rows][n_in] of dtype;  w  [n_out, or 2 n_out][n_in] of dtype.  Both are 16-byte aligned with strides of
+ *             whole 16 bytes (GC_ERR_ALIGN) and at most GC_MAX_INNER; n_in is 1 to GC_MAX_INNER, of whole 16 bytes
+ *   x_scale, w_scale  device float, with GC_E4M3 (NULL: ones), else NULL
+ *   bias      device float, NULL: none
+ *   residual  [n_rows][n_out] of out_dtype, NULL: none; out may be it (the same pointer and stride)
+ *   out       [n_rows][n_out] of out_dtype: dtype or, with GC_BF16 and GC_E4M3 operands, GC_BF16 or GC_F32
+ *   n_rows    0 to 2^31 - 1;  n_out  1 to 2^22
+ *   workspace  device, gc_linear_workspace_bytes(...) of the same sizes, 16-byte aligned; its contents are of no
+ *             consequence.  Calls in flight at the same time need workspaces of their own.  May be NULL where that is 0.
+ * out and workspace may otherwise share no byte with an input or each other (columns of one buffer are apart).
+ * The result does not depend on the order in which blocks run, but which products are added first depends on the sizes.
+ * gc_linear_workspace_bytes: -1 for sizes that gc_linear refuses.
+ */
+int64_t gc_linear_workspace_bytes(int64_t n_rows, int n_out, int n_in, int dtype, int gated);
+int gc_linear(const gc_rows* x, const float* x_scale, const gc_rows* w, const float* w_scale, int64_t n_rows, int n_out,
+              int n_in, int dtype, const float* bias, int act, int gated, const gc_rows* residual, const gc_rows* out,
+              int out_dtype, void* workspace, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -26,7 +26,7 @@ ABI_VERSION = 4   # GC_ABI_VERSION the binding is written for
 
 # constants mirrored from include/geocache.h
 GC_OK = 0
-GC_F32, GC_BF16 = 0, 1
+GC_F32, GC_BF16, GC_E4M3 = 0, 1, 2
 GC_DDIM, GC_FLOW_EULER = 0, 1
 GC_PRED_NONE, GC_PRED_EPS, GC_PRED_V, GC_PRED_VEL = 0, 1, 2, 3
 GC_FULL_PERIODIC, GC_FULL_HEAD_MID_TAIL, GC_FULL_HEAD_TAIL_E = 0, 1, 2
@@ -35,6 +35,8 @@ GC_NOALLOC_SCRATCH_BYTES = 1 << 20
 GC_MAX_HEAD_DIM, GC_MAX_HEADS, GC_MAX_AXES = 256, 1024, 4
 GC_ROPE_HALF, GC_ROPE_INTERLEAVED = 0, 1
 GC_ATTENTION_ITEM_WORDS = 12
+GC_MAX_WIDTH, GC_MAX_INNER = 32768, 1 << 20
+GC_ACT_NONE, GC_ACT_SILU, GC_ACT_GELU, GC_ACT_GELU_TANH = 0, 1, 2, 3
 ERRORS = {-1: "GC_ERR_ARG", -2: "GC_ERR_SHAPE", -3: "GC_ERR_DTYPE", -4: "GC_ERR_ALIGN",
           -5: "GC_ERR_ALIAS", -6: "GC_ERR_CAPACITY", -7: "GC_ERR_HIP"}
 
@@ -66,6 +68,10 @@ class UniPCStep(ctypes.Structure):
 
 class _Heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
 
 
 class RopeScaling(ctypes.Structure):
@@ -106,6 +112,7 @@ _i32p = ctypes.POINTER(ctypes.c_int32)
 _i = ctypes.c_int
 _i64 = ctypes.c_int64
 _headsp = ctypes.POINTER(_Heads)
+_rowsp = ctypes.POINTER(_Rows)
 
 
 def lib() -> ctypes.CDLL:
@@ -171,6 +178,11 @@ def lib() -> ctypes.CDLL:
                                   _i),
             "gc_attention": ([_headsp, _headsp, _headsp, _headsp, _vp, ctypes.POINTER(AttentionInfo), _vp,
                               ctypes.c_double, _vp, ctypes.c_size_t, _vp], _i),
+            "gc_add_rms_norm": ([_rowsp, _rowsp, _i64, _i, _i, _vp, ctypes.c_double, _rowsp, _rowsp, _i, _vp, _vp], _i),
+            "gc_quantize_rows": ([_rowsp, _i64, _i, _i, _rowsp, _vp, _vp], _i),
+            "gc_linear_workspace_bytes": ([_i64, _i, _i, _i, _i], _i64),
+            "gc_linear": ([_rowsp, _vp, _rowsp, _vp, _i64, _i, _i, _i, _vp, _i, _i, _rowsp, _rowsp, _i, _vp,
+                           ctypes.c_size_t, _vp], _i),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -1242,6 +1254,172 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
                               1.0 / math.sqrt(D) if scale is None else scale, at, size, handle), "gc_attention")
     _keep(stream, fresh)
     return out, lse
+
+
+# ---------------------------------------------------------------------------
+# norms and matrix products of the denoiser's blocks
+# ---------------------------------------------------------------------------
+
+# codes by torch type
+_ROW_CODES = {torch.float32: GC_F32, torch.bfloat16: GC_BF16, torch.float8_e4m3fn: GC_E4M3}
+
+
+def _rows(t: torch.Tensor, name: str) -> _Rows:
+    """gc_rows of a device tensor [rows, columns] whose columns are contiguous.
+    The stride of an axis of one element or none is of no consequence."""
+    if type(t) is not _Tensor and not isinstance(t, _Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor (got {t.device})")
+    strides = t.stride()
+    if len(strides) != 2:
+        raise ValueError(f"{name} must be [rows, columns] (got {tuple(t.shape)})")
+    n, c = t.shape
+    if strides[1] != 1 and c > 1:
+        raise ValueError(f"{name} must have contiguous columns")
+    return _Rows(t.data_ptr(), strides[0] if n > 1 else c)
+
+
+def _like_rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: int) -> _Rows:
+    if t.dtype != dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on cuda:{device} (got {t.dtype} {list(t.shape)} on "
+                         f"{t.device})")
+    return _rows(t, name)
+
+
+def _floats(t: Optional[torch.Tensor], name: str, n: int, device: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (n,) or t.get_device() != device:
+        raise ValueError(f"{name} must be float32 [{n}] on cuda:{device} (got {t.dtype} {list(t.shape)} on {t.device})")
+    return _dev(t, name)
+
+
+def gc_add_rms_norm(x: torch.Tensor, residual: torch.Tensor = None, gain: torch.Tensor = None, eps: float = 1e-6,
+                    out_dtype: torch.dtype = None, total: torch.Tensor = None, out: torch.Tensor = None,
+                    out_scale: torch.Tensor = None,
+                    stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor], torch.Tensor]:
+    """RMS norm of rows x + residual (float32 or bfloat16 [rows, width], any
+    strides of the rows) with a gain float32 [width], in the rows' type or as
+    torch.float8_e4m3fn with a float32 scale for each row.  Returns (out, its
+    scales or None, the sum; x itself without a residual).  total and out may
+    be x or residual."""
+    hx = _rows(x, "x")
+    code = _HEAD_CODES.get(x.dtype)
+    if code is None:
+        raise ValueError(f"rows must be float32 or bfloat16 (got {x.dtype})")
+    n, width = shape = x.shape
+    device = x.get_device()
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    out_code = _ROW_CODES.get(out_dtype)
+    if out_code is None:
+        raise ValueError(f"out_dtype must be {x.dtype} or {torch.float8_e4m3fn} (got {out_dtype})")
+    gain_at = _floats(gain, "gain", width, device)
+    fresh = []
+    hr = ht = None
+    if residual is not None:
+        hr = _like_rows(residual, "residual", shape, x.dtype, device)
+        if total is None:
+            total = torch.empty_like(x, memory_format=_CONTIGUOUS)
+            fresh.append(total)
+    if total is not None:
+        ht = _like_rows(total, "total", shape, x.dtype, device)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=x.device)
+        fresh.append(out)
+    ho = _like_rows(out, "out", shape, out_dtype, device)
+    if out_code == GC_E4M3 and out_scale is None:
+        out_scale = torch.empty((n,), dtype=torch.float32, device=x.device)
+        fresh.append(out_scale)
+    _check(lib().gc_add_rms_norm(hx, hr, n, width, code, gain_at, eps, ht, ho, out_code,
+                                 _floats(out_scale, "out_scale", n, device), _stream(stream)), "gc_add_rms_norm")
+    _keep(stream, fresh)
+    return out, out_scale, x if total is None else total
+
+
+def gc_quantize_rows(x: torch.Tensor, out: torch.Tensor = None, out_scale: torch.Tensor = None,
+                     stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows x (float32 or bfloat16 [rows, width], any stride of the rows) as
+    torch.float8_e4m3fn with a float32 scale for each: (out, out_scale)."""
+    hx = _rows(x, "x")
+    code = _HEAD_CODES.get(x.dtype)
+    if code is None:
+        raise ValueError(f"rows must be float32 or bfloat16 (got {x.dtype})")
+    n, width = shape = x.shape
+    device = x.get_device()
+    fresh = []
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
+        fresh.append(out)
+    if out_scale is None:
+        out_scale = torch.empty((n,), dtype=torch.float32, device=x.device)
+        fresh.append(out_scale)
+    _check(lib().gc_quantize_rows(hx, n, width, code, _like_rows(out, "out", shape, torch.float8_e4m3fn, device),
+                                  _floats(out_scale, "out_scale", n, device), _stream(stream)), "gc_quantize_rows")
+    _keep(stream, fresh)
+    return out, out_scale
+
+
+def gc_linear_workspace_bytes(n_rows: int, n_out: int, n_in: int, dtype: torch.dtype, gated: bool = False) -> int:
+    """Bytes of device memory that gc_linear needs beside its arguments."""
+    need = lib().gc_linear_workspace_bytes(n_rows, n_out, n_in, _ROW_CODES.get(dtype, -1), int(bool(gated)))
+    if need < 0:
+        _check(-2, "gc_linear_workspace_bytes")
+    return need
+
+
+def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: int = GC_ACT_NONE, gated: bool = False,
+              residual: torch.Tensor = None, x_scale: torch.Tensor = None, w_scale: torch.Tensor = None,
+              out_dtype: torch.dtype = None, out: torch.Tensor = None, stream=None,
+              workspace: torch.Tensor = None) -> torch.Tensor:
+    """act(x w^T + bias) + residual for x [rows, n_in] and w [n_out, n_in] of
+    one type: float32, bfloat16, or torch.float8_e4m3fn with a float32 scale
+    for each row of x and of w.  gated: w and bias have 2 n_out rows, and the
+    result is act(p of the first n_out) * p of the others + residual.  The
+    result is of out_dtype (default: residual's or out's type, else x's, bfloat16 for 8-bit
+    operands); float32 only with float32 operands.  out may be residual.
+    workspace: gc_linear_workspace_bytes for this call (allocated if None)."""
+    hx, hw = _rows(x, "x"), _rows(w, "w")
+    code = _ROW_CODES.get(x.dtype)
+    if code is None:
+        raise ValueError(f"x must be float32, bfloat16 or {torch.float8_e4m3fn} (got {x.dtype})")
+    n, n_in = x.shape
+    w_rows = w.shape[0]
+    device = x.get_device()
+    if w.dtype != x.dtype or w.shape[1] != n_in or w.get_device() != device:
+        raise ValueError(f"w must be {x.dtype} [n_out, {n_in}] on {x.device} (got {w.dtype} {list(w.shape)} on {w.device})")
+    n_out = w_rows
+    if gated:
+        if w_rows % 2:
+            raise ValueError(f"gated products need an even number of rows of w (got {w_rows})")
+        n_out = w_rows // 2
+    if out_dtype is None:
+        out_dtype = (out.dtype if out is not None else residual.dtype if residual is not None else
+                     torch.bfloat16 if code == GC_E4M3 else x.dtype)
+    out_code = _ROW_CODES.get(out_dtype)
+    if out_code is None:
+        raise ValueError(f"out_dtype must be float32 or bfloat16 (got {out_dtype})")
+    fresh = []
+    if out is None:
+        out = torch.empty((n, n_out), dtype=out_dtype, device=x.device)
+        fresh.append(out)
+    ho = _like_rows(out, "out", (n, n_out), out_dtype, device)
+    hr = None if residual is None else _like_rows(residual, "residual", (n, n_out), out_dtype, device)
+    at, size = None, 0
+    need = lib().gc_linear_workspace_bytes(n, n_out, n_in, code, int(bool(gated)))
+    if need > 0:
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+            fresh.append(workspace)
+        elif workspace.get_device() != device:
+            raise ValueError(f"workspace must be on {x.device} (got {workspace.device})")
+        at, size = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    _check(lib().gc_linear(hx, _floats(x_scale, "x_scale", n, device), hw, _floats(w_scale, "w_scale", w_rows, device),
+                           n, n_out, n_in, code, _floats(bias, "bias", w_rows, device), act, int(bool(gated)), hr, ho,
+                           out_code, at, size, _stream(stream)), "gc_linear")
+    _keep(stream, fresh)
+    return out
 
 
 lib()
