@@ -10,7 +10,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 struct LinearArgs {
@@ -23,109 +22,192 @@ struct LinearArgs {
   int64_t n_rows;
   int n_out, row_bytes;          // row_bytes: of n_in operands
   int act, gated, out_f32;
-  int out_whole, residual_whole; // 16 bytes of a row may be accessed at once
+  int whole;                     // groups of 8 outputs may be accessed as 16 bytes
   int parts;                     // of the inner dimension
-  int part_bytes;                // of a row in a part (the last one may be shorter)
-  float* partial;                // [parts][n_rows][n_out, or 2 n_out]
+  int part_bytes;                // of a row in a part, a multiple of kStepBytes (the last one may be shorter)
+  float* partial;                // sums of the parts: [parts][n_rows][partial_cols, or 2 partial_cols]
+  int64_t partial_part;          // floats of one part
+  int partial_cols;              // n_out, and up to a multiple of 8
 };
 
-// Activations, in float32.
-__device__ __forceinline__ float activation(float p, int act) {
-  if (act == GC_ACT_SILU) return p / (1.f + expf(-p));
-  if (act == GC_ACT_GELU) return 0.5f * p * (1.f + erff(p * 0.70710678118654752f));
-  // (1 + tanh u) / 2 = 1 / (1 + e^(-2u))
-  if (act == GC_ACT_GELU_TANH) return p / (1.f + expf(-1.5957691216057308f * (p + 0.044715f * p * p * p)));
-  return p;
+constexpr int kStepBytes = 128;   // of a row that a tile reads at a time
+
+// p * 1 / (1 + e^-u): u = p, or 2 sqrt(2 / pi) (p + 0.044715 p^3), since (1 + tanh v) / 2 = 1 / (1 + e^(-2 v)).
+__device__ __forceinline__ float times_logistic(float p, float u_log2e) {
+  return p * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u_log2e));
+}
+// p times the normal distribution function of p.  The tail beyond |p| is e^(-p^2 / 2) t P(t) / 2 with
+// t = 1 / (1 + 0.38 |p| / sqrt 2) and P fitted to e^(z^2) erfc(z) / t by least squares at Chebyshev nodes of t, weighted
+// towards the largest relative error (2e-8).
+__device__ __forceinline__ float gelu(float p) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(p), 0.26870057685088805f, 1.f));
+  float q = 0.059048961848020554f;
+  q = __builtin_fmaf(q, t, -0.2626957595348358f);
+  q = __builtin_fmaf(q, t, 0.36475491523742676f);
+  q = __builtin_fmaf(q, t, -0.16252949833869934f);
+  q = __builtin_fmaf(q, t, 0.23080290853977203f);
+  q = __builtin_fmaf(q, t, 0.13829964399337769f);
+  q = __builtin_fmaf(q, t, 0.20400194823741913f);
+  q = __builtin_fmaf(q, t, 0.21390503644943237f);
+  q = __builtin_fmaf(q, t, 0.2144118696451187f);
+  const float tail = 0.5f * __builtin_amdgcn_exp2f(p * p * -0.72134752044448170f) * (t * q);
+  return p * (p > 0.f ? 1.f - tail : tail);
+}
+template <int kCount>
+__device__ __forceinline__ void activate(float (&p)[kCount], int act) {
+  if (act == GC_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) p[i] = times_logistic(p[i], p[i] * 1.4426950408889634f);
+  } else if (act == GC_ACT_GELU_TANH) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+      p[i] = times_logistic(p[i], p[i] * __builtin_fmaf(p[i] * p[i], 0.10294323970f, 2.3022081985f));
+  } else if (act == GC_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) p[i] = gelu(p[i]);
+  }
 }
 
-// kCount consecutive outputs of one row, from column n (the last ones may lie past the end): the sums' epilogue.
-// gate: with gated products those of the value rows; otherwise unused.
-template <int kCount>
-__device__ __forceinline__ void load_floats(const float* p, int have, float fill, float (&v)[kCount]) {
+// Eight consecutive columns of the output, all inside it: what the epilogue has of them.
+struct Columns {
+  int n;
+  float scale[8], bias[8], value_scale[8], value_bias[8];
+  __device__ __forceinline__ static void load(const float* p, float fill, float (&v)[8]) {
 #pragma unroll
-  for (int i = 0; i < kCount; ++i) v[i] = p && i < have ? p[i] : fill;
-}
-template <int kCount>
-__device__ __forceinline__ void finish(const LinearArgs& p, int64_t m, int n, float (&a)[kCount], float (&b)[kCount]) {
-  const int have = p.n_out - n;
-  if (m >= p.n_rows || have <= 0) return;
-  const float xs = p.x_scale ? p.x_scale[m] : 1.f;
-  float s[kCount];
-  if (p.x_scale || p.w_scale) {
-    load_floats<kCount>(p.w_scale ? p.w_scale + n : nullptr, have, 1.f, s);
+    for (int i = 0; i < 8; ++i) v[i] = fill;
+    if (!p) return;
 #pragma unroll
-    for (int i = 0; i < kCount; ++i) a[i] = a[i] * xs * s[i];
+    for (int i = 0; i < 8; ++i) v[i] = p[i];
   }
-  if (p.bias) {
-    load_floats<kCount>(p.bias + n, have, 0.f, s);
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) a[i] += s[i];
-  }
-#pragma unroll
-  for (int i = 0; i < kCount; ++i) a[i] = activation(a[i], p.act);
-  if (p.gated) {
-    if (p.x_scale || p.w_scale) {
-      load_floats<kCount>(p.w_scale ? p.w_scale + p.n_out + n : nullptr, have, 1.f, s);
-#pragma unroll
-      for (int i = 0; i < kCount; ++i) b[i] = b[i] * xs * s[i];
+  template <bool kGated>
+  __device__ __forceinline__ void init(const LinearArgs& p, int first) {
+    n = first;
+    load(p.w_scale ? p.w_scale + n : nullptr, 1.f, scale);
+    load(p.bias ? p.bias + n : nullptr, 0.f, bias);
+    if (kGated) {
+      load(p.w_scale ? p.w_scale + p.n_out + n : nullptr, 1.f, value_scale);
+      load(p.bias ? p.bias + p.n_out + n : nullptr, 0.f, value_bias);
     }
-    if (p.bias) {
-      load_floats<kCount>(p.bias + p.n_out + n, have, 0.f, s);
-#pragma unroll
-      for (int i = 0; i < kCount; ++i) b[i] += s[i];
-    }
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) a[i] *= b[i];
   }
+};
+
+// The sums a (and b of the value rows) of eight columns of row m to the output, 16 bytes at a time.
+template <bool kGated>
+__device__ __forceinline__ void finish(const LinearArgs& p, const Columns& c, int64_t m, float (&a)[8], float (&b)[8]) {
   const int es = p.out_f32 ? 4 : 2;
-  if (p.residual) {
-    const char* r = p.residual + m * p.residual_row + (int64_t)n * es;
-    if (p.out_f32) {
+  float add[8];
 #pragma unroll
-      for (int i = 0; i < kCount; ++i)
-        if (i < have) a[i] += ((const float*)r)[i];
-    } else {
+  for (int i = 0; i < 8; ++i) add[i] = 0.f;
+  if (p.residual) {   // on its way during the arithmetic
+    const char* r = p.residual + m * p.residual_row + (int64_t)c.n * es;
+    if (p.out_f32) load_heads<8>((const float*)r, add);
+    else load_heads<8>((const uint16_t*)r, add);
+  }
+  if (p.x_scale || p.w_scale) {
+    const float xs = p.x_scale ? p.x_scale[m] : 1.f;
 #pragma unroll
-      for (int i = 0; i < kCount; ++i)
-        if (i < have) a[i] += load_one((const uint16_t*)r + i);
+    for (int i = 0; i < 8; ++i) a[i] = a[i] * xs * c.scale[i];
+    if (kGated) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = b[i] * xs * c.value_scale[i];
     }
   }
-  char* o = p.out + m * p.out_row + (int64_t)n * es;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] += c.bias[i];
+  activate<8>(a, p.act);
+  if (kGated) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] *= b[i] + c.value_bias[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] += add[i];
+  char* o = p.out + m * p.out_row + (int64_t)c.n * es;
+  if (p.out_f32) store_heads<8>((float*)o, a);
+  else store_heads<8>((uint16_t*)o, a);
+}
+
+// The same for one column.
+template <bool kGated>
+__device__ __forceinline__ void finish_one(const LinearArgs& p, int64_t m, int n, float sum, float value) {
+  float a[1] = {sum}, b = value;
+  if (p.x_scale || p.w_scale) {
+    const float xs = p.x_scale ? p.x_scale[m] : 1.f;
+    a[0] = a[0] * xs * (p.w_scale ? p.w_scale[n] : 1.f);
+    if (kGated) b = b * xs * (p.w_scale ? p.w_scale[p.n_out + n] : 1.f);
+  }
+  if (p.bias) a[0] += p.bias[n];
+  activate<1>(a, p.act);
+  if (kGated) a[0] *= b + (p.bias ? p.bias[p.n_out + n] : 0.f);
   if (p.out_f32) {
-#pragma unroll
-    for (int i = 0; i < kCount; ++i)
-      if (i < have) ((float*)o)[i] = a[i];
+    if (p.residual) a[0] += ((const float*)(p.residual + m * p.residual_row))[n];
+    ((float*)(p.out + m * p.out_row))[n] = a[0];
   } else {
-#pragma unroll
-    for (int i = 0; i < kCount; ++i)
-      if (i < have) store_one((uint16_t*)o + i, a[i]);
+    if (p.residual) a[0] += load_one((const uint16_t*)(p.residual + m * p.residual_row) + n);
+    store_one((uint16_t*)(p.out + m * p.out_row) + n, a[0]);
   }
 }
 
-// Operand types: what a pair of 16-byte chunks of a row, one in either half
-// of the wave's lanes, multiplies.  The order of the products inside is free:
-// both operands have the same.
-struct F32 {
-  static constexpr int kPairs = 1;   // of chunks that a product takes
+// Operand types.  A product takes kBlock rows of either operand; a fragment of
+// them is kChunks 16-byte chunks a lane, of row lane % kBlock and with the lanes'
+// groups side by side.  Which of a row's products a fragment holds where is
+// free: both operands have them alike.  Of an accumulator's four consecutive elements q the lane holds
+// weight rows kStride q + 4 (lane / kBlock) .. + 3 for row lane % kBlock of x.
+struct Blocks32 {
+  static constexpr int kBlock = 32, kQuads = 4, kStride = 8;
+  typedef f32x16 Acc;
+};
+struct Blocks16 {
+  static constexpr int kBlock = 16, kQuads = 1, kStride = 16;
+  typedef f32x4 Acc;
+};
+struct F32 : Blocks32 {
+  static constexpr int kChunks = 1, kProducts = 4;   // products of a pair of fragments
+  static constexpr bool kTotals = true;
   typedef f32x4 Frag;
-  __device__ __forceinline__ static f32x16 mma(const Frag& w, const Frag& x, f32x16 c) {
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[i], c, 0, 0, 0);
     return c;
   }
 };
-struct BF16 {
-  static constexpr int kPairs = 1;
+struct BF16 : Blocks16 {
+  static constexpr int kChunks = 1, kProducts = 1;
+  static constexpr bool kTotals = false;
   typedef bf16x8 Frag;
-  __device__ __forceinline__ static f32x16 mma(const Frag& w, const Frag& x, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x, c, 0, 0, 0);
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0);
   }
 };
-struct E4M3 {
-  static constexpr int kPairs = 2;
+// The 8-bit products add their terms to fewer bits than float32 has: over rows of 64 to 4096 they are 1.3e-5 off in the
+// 2-norm, 7e-5 with channels of 100 times the others' size.  A bfloat16 result is rounded by 1.7e-3, so it takes
+// them; for a float32 result the operands become bfloat16 first, which holds them exactly.
+struct E4M3Exact : Blocks32 {
+  static constexpr int kChunks = 1, kProducts = 2;
+  static constexpr bool kTotals = false;
+  typedef u32x4 Frag;
+  __device__ __forceinline__ static bf16x8 half(const Frag& f, int i) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    bf16x8 r;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + j], 1.f, false);
+      const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + j], 1.f, true);
+      r[4 * j] = lo[0], r[4 * j + 1] = lo[1], r[4 * j + 2] = hi[0], r[4 * j + 3] = hi[1];
+    }
+    return r;
+  }
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(half(w, i), half(x, i), c, 0, 0, 0);
+    return c;
+  }
+};
+struct E4M3 : Blocks32 {
+  static constexpr int kChunks = 2, kProducts = 1;
+  static constexpr bool kTotals = false;
   typedef i32x8 Frag;
-  __device__ __forceinline__ static f32x16 mma(const Frag& w, const Frag& x, f32x16 c) {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);   // (no scales: ones)
   }
 };
 

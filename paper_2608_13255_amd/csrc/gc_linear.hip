@@ -8,17 +8,37 @@
 namespace gc {
 namespace {
 
-template <class Op, bool kGated>
-void launch_tiles(const LinearArgs& p, hipStream_t stream) {
-  using C = Tiles<Op, 2, 2, 2, 2, kGated>;
-  const dim3 grid((unsigned)((p.n_out + C::kOut - 1) / C::kOut), (unsigned)((p.n_rows + C::kX - 1) / C::kX));
-  k_linear_tiles<Op, 2, 2, 2, 2, kGated><<<grid, C::kThreads, C::kStage, stream>>>(p);
+// Tiles of a launch, at most (times the parts of the inner dimension they fit an int).
+constexpr int64_t kMostTiles = 1 << 20;
+
+constexpr int kCus = 256;
+
+template <class C>
+void launch_tiles(LinearArgs p, hipStream_t stream) {
+  const int64_t tiles_w = (p.n_out + C::kOut - 1) / C::kOut, most = std::max<int64_t>(1, kMostTiles / tiles_w) * C::kX;
+  const int64_t n = p.n_rows, width = (p.gated ? 2 : 1) * (int64_t)p.partial_cols;
+  for (int64_t r = 0; r < n; r += most) {
+    p.n_rows = std::min(n - r, most);
+    const int64_t tiles_x = (p.n_rows + C::kX - 1) / C::kX;
+    const int64_t blocks = tiles_x * tiles_w * p.parts;
+    k_linear_tiles<C><<<(unsigned)blocks, C::kThreads, 0, stream>>>(p, (int)tiles_x, (int)tiles_w);
+    p.x += most * p.x_row;
+    if (p.x_scale) p.x_scale += most;
+    if (p.residual) p.residual += most * p.residual_row;
+    if (p.partial) p.partial += most * width;
+    p.out += most * p.out_row;
+  }
 }
 
 template <class Op>
 void launch_linear(const LinearArgs& p, hipStream_t stream) {
-  if (p.gated) launch_tiles<Op, true>(p, stream);
-  else launch_tiles<Op, false>(p, stream);
+  if (p.gated) launch_tiles<Tiles<Op, 2, 4, 128, 64, true>>(p, stream);
+  else launch_tiles<Tiles<Op, 2, 4, 128, 64, false>>(p, stream);
+}
+template <>
+void launch_linear<F32>(const LinearArgs& p, hipStream_t stream) {
+  if (p.gated) launch_tiles<Tiles<F32, 2, 4, 64, 64, true>>(p, stream);
+  else launch_tiles<Tiles<F32, 2, 4, 64, 64, false>>(p, stream);
 }
 
 constexpr int64_t kMostStride = (int64_t)1 << 40;
@@ -92,9 +112,11 @@ extern "C" int gc_linear(const gc_rows* x, const float* x_scale, const gc_rows* 
   p.out = (char*)out->data, p.out_row = out->stride * eo;
   p.n_rows = n_rows, p.n_out = n_out, p.row_bytes = (int)(n_in * es);
   p.act = act, p.gated = gated != 0, p.out_f32 = out_dtype == GC_F32;
-  p.out_whole = rows_aligned(*out, n_rows, 16, (int)eo), p.residual_whole = residual && rows_aligned(*residual, n_rows, 16, (int)eo);
+  p.whole = rows_aligned(*out, n_rows, 16, (int)eo) && (!residual || rows_aligned(*residual, n_rows, 16, (int)eo));
+  p.parts = 1, p.part_bytes = (p.row_bytes + kStepBytes - 1) / kStepBytes * kStepBytes;
   if (dtype == GC_F32) launch_linear<F32>(p, stream);
   else if (dtype == GC_BF16) launch_linear<BF16>(p, stream);
+  else if (p.out_f32) launch_linear<E4M3Exact>(p, stream);
   else launch_linear<E4M3>(p, stream);
   return after_launch(stream, who);
 }

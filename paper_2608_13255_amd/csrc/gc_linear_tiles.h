@@ -1,15 +1,14 @@
 // Matrix products in tiles: a block computes kX rows by kW rows of the weights.
 //
 // Both operands are rows with the inner dimension contiguous, so either tile is
-// read from memory to LDS 128 bytes of each row at a time, straight and
+// read from memory to LDS 128 bytes of each row at a time (a step), straight and
 // 16 bytes a lane, with chunk c of row r at place c ^ (r / 2 % 8): then
 // 16 rows' same chunk lie in 16 different places of the 256 bytes that the banks span.
+// Two steps are in LDS or on their way: when every wave has read a step, its place is filled with the second one after it.
 //
 // The weights are the first operand, so an accumulator's lane holds one row of
-// x and 16 weight rows.  Which weight row lies at which place of a 32-row
-// block is free: row 8 a + 4 h + b of the product is weight row 16 h + 4 a + b, so that
-// a lane's 16 outputs are consecutive.  Gated products take blocks of 32 gate and 32 value rows by
-// turns, so that a lane holds both.
+// x and groups of four consecutive weight rows.  Gated products take 32 gate and 32 value rows by
+// turns, so that a wave holds both.
 #pragma once
 
 #include "gc_linear.h"
@@ -18,124 +17,349 @@ namespace gc {
 
 typedef __attribute__((address_space(3))) void LdsVoid;
 
+// Until at most kLeft of the wave's loads from memory are outstanding, and none of its reads of LDS.
 template <int kLeft>
-__device__ __forceinline__ void wait_for_loads() {
+__device__ __forceinline__ void wait_all_but() {
   static_assert(kLeft < 64, "the counter has 6 bits");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt((kLeft & 15) | (7 << 4) | (15 << 8) | ((kLeft >> 4) << 14));
+  __builtin_amdgcn_s_waitcnt((kLeft & 15) | (7 << 4) | (0 << 8) | ((kLeft >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void block_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-constexpr int kStepBytes = 128;   // of a row, a step
+constexpr int kTotalSteps = 16;
+constexpr uint32_t kNowhere = 0x7ffffff0u;   // past any range
+// Blocks that share rows of x, or of the weights, and the steps between asking for a line and its load.
+constexpr int kAheadW = 4, kAheadX = 8, kAheadSteps = 2;
 
-__device__ __forceinline__ int tile_place(int row, int chunk) { return row * kStepBytes + ((chunk ^ (row >> 1)) & 7) * 16; }
-
-template <class Op, int kWavesX, int kWavesW, int kBlocksX, int kBlocksW, bool kGated>
+template <class Op_, int kWavesX_, int kWavesW_, int kRowsX, int kRowsW, bool kGated_>
 struct Tiles {
+  typedef Op_ Op;
+  static constexpr int kWavesX = kWavesX_, kWavesW = kWavesW_;
+  static constexpr bool kGated = kGated_, kTotals = Op::kTotals;
   static constexpr int kWaves = kWavesX * kWavesW, kThreads = kWaves * 64;
-  static constexpr int kX = kWavesX * kBlocksX * 32, kW = kWavesW * kBlocksW * 32;
+  static constexpr int kBlocksX = kRowsX / Op::kBlock, kBlocksW = kRowsW / Op::kBlock;   // of a wave
+  static constexpr int kX = kWavesX * kRowsX, kW = kWavesW * kRowsW;
+  static constexpr int kWaveX = kRowsX, kWaveW = kRowsW;
   static constexpr int kOut = kGated ? kW / 2 : kW;      // columns of the output
+  static constexpr int kBuffers = 2;
   static constexpr int kStage = (kX + kW) * kStepBytes;
-  static constexpr int kLoads = (kX + kW) / 8 / kWaves;  // a wave's, a step
+  static constexpr int kLoads = (kX + kW) / 8 / kWaves;      // a wave's, a step
+  static constexpr int kGroups = 64 / Op::kBlock;            // of lanes
+  static constexpr int kParts = 8 / kGroups / Op::kChunks;   // of a step: fragments that products take
+  static constexpr int kFrags = kBlocksX + kBlocksW;
+  // the epilogue's place of a wave: 16 rows of its columns
+  static constexpr int kWaveFloats = 16 * kRowsW;
+  static constexpr int kLds = kBuffers * kStage + kWaves * kWaveFloats * 4;
+  static constexpr int kBlocksPerCu = 163840 / kLds;
+  static_assert(kLds <= 163840 && (kRowsW == 64 || kRowsW == 32), "LDS of a compute unit, and what the epilogue's permutation covers");
   static_assert((kX + kW) / 8 % kWaves == 0 && kX / 8 % kWaves == 0 && kWaves % 4 == 0, "whole loads");
-  static_assert(!kGated || kBlocksW % 2 == 0, "gate and value in one wave");
+  static_assert(!kGated || kRowsW % 64 == 0, "gate and value in one wave");
 };
 
-template <class Op, int kWavesX, int kWavesW, int kBlocksX, int kBlocksW, bool kGated>
-__global__ __launch_bounds__(kWavesX* kWavesW * 64) void k_linear_tiles(const LinearArgs p) {
-  using C = Tiles<Op, kWavesX, kWavesW, kBlocksX, kBlocksW, kGated>;
-  extern __shared__ char lds[];
+// Tiles and parts of the inner dimension, as blocks take them: consecutive blocks go to the eight XCDs by turns, each
+// with an L2 of its own, so each XCD has a run of tiles, and walks it kGroup tiles of x high.
+struct TileAt {
+  int x, w, part;
+};
+__device__ __forceinline__ TileAt tile_at(int id, int tiles_x, int tiles_w, int parts) {
+  constexpr int kXcds = 8, kGroup = 8;
+  const int tiles = tiles_x * tiles_w, n = tiles * parts, q = n / kXcds, r = n % kXcds;
+  const int xcd = id % kXcds, all = xcd * q + (xcd < r ? xcd : r) + id / kXcds;
+  const int part = all / tiles, at = all - part * tiles;
+  const int group = at / (kGroup * tiles_w), first = group * kGroup;
+  const int high = tiles_x - first < kGroup ? tiles_x - first : kGroup;
+  const int in = at - group * kGroup * tiles_w;
+  return {first + in % high, in / high, part};
+}
+
+// The lane's number, where nothing computed from it before is kept in registers until here.
+__device__ __forceinline__ int lane_anew() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
+// The kernel's arguments, read again here: kept in scalar registers from the start they would not leave enough of them.
+__device__ __forceinline__ LinearArgs args_anew() {
+  typedef const __attribute__((address_space(4))) uint64_t* Words;
+  Words from = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(from));
+  constexpr int kWords = sizeof(LinearArgs) / 8;
+  static_assert(sizeof(LinearArgs) % 8 == 0, "whole words");
+  uint64_t words[kWords];
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) words[i] = from[i];
+  LinearArgs a;
+  __builtin_memcpy(&a, words, sizeof(a));
+  return a;
+}
+
+// Reads of steps' rows to LDS, one after the other.
+template <class C>
+struct StageLoader {
+  static constexpr int kLoadRows = 8 * C::kWaves, kLoadsX = C::kX / kLoadRows, kLoadsW = C::kW / kLoadRows;
+  const char *xb, *wb, *ab;
+  int range_x, range_w, range_a;   // bytes from the wave's first row to the first byte of the last one
+  int left;                        // bytes of a row from here to the part's end
+  int chunk16;
+  uint32_t at[kLoadsX + kLoadsW], ahead;
+
+  __device__ __forceinline__ void init(const TileAt& tile, int wave) {
+    const LinearArgs p = args_anew();
+    const int lane = lane_anew();
+    const int k_begin = tile.part * p.part_bytes;
+    const int k_end = p.row_bytes - k_begin < p.part_bytes ? p.row_bytes : k_begin + p.part_bytes;
+    const int64_t m0 = (int64_t)tile.x * C::kX;
+    const int n0 = tile.w * C::kOut;
+    const int rows_x = p.n_rows - m0 < C::kX ? (int)(p.n_rows - m0) : C::kX;
+    const int rows_w = p.n_out - n0 < C::kOut ? p.n_out - n0 : C::kOut;
+    xb = p.x + m0 * p.x_row + k_begin;
+    wb = p.w + (int64_t)n0 * p.w_row + k_begin;
+    const char* vb = wb + (C::kGated ? (int64_t)p.n_out * p.w_row : 0);
+    range_x = (int)((rows_x - 1) * p.x_row), range_w = (int)((rows_w - 1) * p.w_row);
+    left = k_end - k_begin;
+    // what this block asks for ahead
+    const bool of_w = wave >= C::kWaves / 2;
+    const int w4 = wave % (C::kWaves / 2);
+    constexpr int kHalf = C::kWaves / 2, kRowsX = C::kX / kAheadW / kHalf, kRowsW = C::kW / kAheadX / kHalf;
+    if (!of_w) {
+      ab = xb, range_a = range_x;
+      ahead = lane < kRowsX ? (uint32_t)((tile.w % kAheadW * kHalf + w4) * kRowsX + lane) * (uint32_t)p.x_row : kNowhere;
+    } else {
+      const bool value = C::kGated && w4 >= kHalf / 2;
+      ab = value ? vb : wb, range_a = range_w;
+      const int row = C::kGated ? (tile.x % kAheadX * (kHalf / 2) + w4 % (kHalf / 2)) * kRowsW + lane : (tile.x % kAheadX * kHalf + w4) * kRowsW + lane;
+      ahead = lane < kRowsW ? (uint32_t)row * (uint32_t)p.w_row : kNowhere;
+    }
+    // Load i takes the rows 8 (wave + i kWaves) + lane / 8, its places lane % 8.  Of the weights' places every other 32
+    // are values', so with eight waves a wave's loads are all of gates' rows or all of values', 32 apart.
+    static_assert(!C::kGated || C::kWaves == 8, "gates or values");
+    if (C::kGated && ((wave >> 2) & 1)) wb = vb;
+    chunk16 = ((lane ^ (lane >> 4) ^ (wave << 2)) & 7) * 16;
+#pragma unroll
+    for (int i = 0; i < kLoadsX; ++i) at[i] = (uint32_t)(i * kLoadRows + 8 * wave + (lane >> 3)) * (uint32_t)p.x_row + chunk16;
+#pragma unroll
+    for (int i = 0; i < kLoadsW; ++i)
+      at[kLoadsX + i] = (uint32_t)((C::kGated ? i * kLoadRows / 2 + 8 * (wave & 3) : i * kLoadRows + 8 * wave) + (lane >> 3)) * (uint32_t)p.w_row + chunk16;
+  }
+  // A step's loads.  Past the end nothing is read, and the places get zeros.
+  __device__ __forceinline__ void load(char* lds, int wave) {
+    const bool past = chunk16 >= left;
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)xb, 0, left > 0 ? range_x + left : 0, 0x00027000);
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)wb, 0, left > 0 ? range_w + left : 0, 0x00027000);
+#pragma unroll
+    for (int i = 0; i < kLoadsX; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (LdsVoid*)(lds + 8 * (wave + i * C::kWaves) * kStepBytes), 16, past ? kNowhere : at[i], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < kLoadsW; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (LdsVoid*)(lds + (C::kX + 8 * (wave + i * C::kWaves)) * kStepBytes), 16, past ? kNowhere : at[kLoadsX + i], 0, 0, 0);
+    xb += kStepBytes, wb += kStepBytes, left -= kStepBytes;
+  }
+  // Asks for the lines of the step kAheadSteps after the one to be loaded next, so that they are in the L2 by then.  Blocks that run at the same time on
+  // an XCD share rows: each asks for its part of them.  What arrives (4 bytes a line) is of no use.
+  __device__ __forceinline__ void ask(char* junk) {
+    const int far = left - kAheadSteps * kStepBytes;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(ab + kAheadSteps * kStepBytes), 0, far > 0 ? range_a + far : 0, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)junk, 4, ahead, 0, 0, 0);
+    ab += kStepBytes;
+  }
+};
+
+// A wave's fragments of one part of a step.
+template <class C>
+struct Fragments {
+  typename C::Op::Frag x[C::kBlocksX], w[C::kBlocksW];
+  // lane_at: places of the lane's chunks in the first block's rows
+  __device__ __forceinline__ void read(const char* xs, const char* ws, const int (&lane_at)[8 / C::kGroups], int part) {
+    constexpr int kChunks = C::Op::kChunks, kBytes = C::Op::kBlock * kStepBytes;
+#pragma unroll
+    for (int i = 0; i < C::kFrags; ++i) {
+      const char* from = i < C::kBlocksX ? xs + i * kBytes : ws + (i - C::kBlocksX) * kBytes;
+      u32x4 c[kChunks];
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) c[q] = *reinterpret_cast<const u32x4*>(from + lane_at[part * kChunks + q]);
+      if (i < C::kBlocksX) __builtin_memcpy(&x[i], c, sizeof(x[i]));
+      else __builtin_memcpy(&w[i - C::kBlocksX], c, sizeof(w[0]));
+    }
+  }
+};
+
+// The order of a part's instructions: a read of LDS or a load from memory between any two products.
+template <class C, int kDma>
+__device__ __forceinline__ void beside_products() {
+  constexpr int kProducts = C::kBlocksX * C::kBlocksW * C::Op::kProducts;
+  constexpr int kEach = kProducts / (2 * (C::kFrags + kDma)) > 1 ? kProducts / (2 * (C::kFrags + kDma)) : 1;
+#pragma unroll
+  for (int i = 0; i < C::kFrags; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, C::Op::kChunks, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < kDma; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+    __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kProducts, 0);
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <class C>
+__global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs args, int tiles_x, int tiles_w) {
+  __shared__ __align__(16) char lds[C::kLds];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t m0 = (int64_t)blockIdx.y * C::kX;
-  const int n0 = blockIdx.x * C::kOut;
+  const int wx = wave / C::kWavesW, ww = wave % C::kWavesW;
+  const int parts = args.parts;
+  float* mine = reinterpret_cast<float*>(lds + C::kBuffers * C::kStage) + wave * C::kWaveFloats;
+  char* junk = reinterpret_cast<char*>(mine);
 
-  // the rows that this lane's loads read, and their chunk
-  const int chunk = (lane ^ (lane >> 4) ^ (wave << 2)) & 7;   // rows of a load: 8 (wave + ..) + lane / 8
-  const int left_x = p.n_rows - m0 < C::kX ? (int)(p.n_rows - m0) : C::kX;
-  const int left_w = p.n_out - n0;
-  const int k_begin = 0, k_end = p.row_bytes;
-  uint32_t at[C::kLoads];
+  constexpr int kBlock = C::Op::kBlock;
+  int lane_at[8 / C::kGroups];
 #pragma unroll
-  for (int i = 0; i < C::kLoads; ++i) {
-    const int row = 8 * (wave + i * C::kWaves) + (lane >> 3);
-    if (8 * (wave + i * C::kWaves) < C::kX) {
-      at[i] = (uint32_t)row * (uint32_t)p.x_row + chunk * 16;
+  for (int s = 0; s < 8 / C::kGroups; ++s)
+    lane_at[s] = lane % kBlock * kStepBytes + (((C::kGroups * s + lane / kBlock) ^ (lane % kBlock >> 1)) & 7) * 16;
+  const int x_at = wx * C::kWaveX * kStepBytes, w_at = (C::kX + ww * C::kWaveW) * kStepBytes;
+
+  const TileAt tile = tile_at(blockIdx.x, tiles_x, tiles_w, parts);
+  StageLoader<C> in;
+  in.init(tile, wave);
+  const int steps = (in.left + kStepBytes - 1) / kStepBytes;
+  in.load(lds, wave);
+  in.load(lds + C::kStage, wave);
+  typedef typename C::Op::Acc Acc;
+  constexpr int kElements = 4 * C::Op::kQuads;
+  Acc acc[C::kBlocksX][C::kBlocksW];
+#pragma unroll
+  for (int i = 0; i < C::kBlocksX; ++i)
+#pragma unroll
+    for (int j = 0; j < C::kBlocksW; ++j)
+#pragma unroll
+      for (int e = 0; e < kElements; ++e) acc[i][j][e] = 0.f;
+  // float32: the sum of kTotalSteps steps is added to a total, so that roundings do not pile up over a long row
+  Acc total[C::kTotals ? C::kBlocksX : 1][C::kTotals ? C::kBlocksW : 1];
+  const auto add_to_total = [&] {
+#pragma unroll
+    for (int i = 0; i < (C::kTotals ? C::kBlocksX : 0); ++i)
+#pragma unroll
+      for (int j = 0; j < C::kBlocksW; ++j)
+#pragma unroll
+        for (int e = 0; e < kElements; ++e) total[i][j][e] += acc[i][j][e], acc[i][j][e] = 0.f;
+  };
+  if (C::kTotals) {
+#pragma unroll
+    for (int i = 0; i < C::kBlocksX; ++i)
+#pragma unroll
+      for (int j = 0; j < C::kBlocksW; ++j)
+#pragma unroll
+        for (int e = 0; e < kElements; ++e) total[C::kTotals ? i : 0][C::kTotals ? j : 0][e] = 0.f;
+  }
+
+  wait_all_but<C::kLoads>();
+  block_barrier();
+  Fragments<C> f[2];
+  char *now = lds, *next = lds + C::kStage;
+  f[0].read(now + x_at, now + w_at, lane_at, 0);
+  for (int k = 0; k < steps; ++k) {
+#pragma unroll
+    for (int s = 0; s < C::kParts; ++s) {
+      if (s + 1 < C::kParts) {
+        f[(s + 1) & 1].read(now + x_at, now + w_at, lane_at, s + 1);
+        if (s == 0) in.ask(junk);
+      } else {
+        // every wave has read this step whole, and the next one has arrived
+        wait_all_but<1>();
+        block_barrier();
+        f[(s + 1) & 1].read(next + x_at, next + w_at, lane_at, 0);
+        in.load(now, wave);
+      }
+#pragma unroll
+      for (int i = 0; i < C::kBlocksX; ++i)
+#pragma unroll
+        for (int j = 0; j < C::kBlocksW; ++j) acc[i][j] = C::Op::mma(f[s & 1].w[j], f[s & 1].x[i], acc[i][j]);
+      if (s == 0) beside_products<C, 1>();
+      else if (s + 1 < C::kParts) beside_products<C, 0>();
+      else beside_products<C, C::kLoads>();
+    }
+    asm volatile("" ::: "memory");   // the next step's first fragments are read here, not where they are used
+    char* t = now;
+    now = next, next = t;
+    if (C::kTotals && k % kTotalSteps == kTotalSteps - 1) add_to_total();
+  }
+  if (C::kTotals) {
+    add_to_total();
+#pragma unroll
+    for (int i = 0; i < C::kBlocksX; ++i)
+#pragma unroll
+      for (int j = 0; j < C::kBlocksW; ++j) acc[i][j] = total[C::kTotals ? i : 0][C::kTotals ? j : 0];
+  }
+  wait_all_but<0>();   // the loads past the end write to LDS as well, and the places asked for to the epilogue's
+
+  // Through LDS, 16 rows of the wave at a time: eight consecutive columns a lane.  16-byte chunk c of row r lies at place
+  // c ^ r (c ^ r / 2 of rows of 8 chunks).
+  const LinearArgs p = args_anew();
+  const int64_t m0 = (int64_t)tile.x * C::kX + wx * C::kWaveX;
+  constexpr int kCols = C::kOut / C::kWavesW, kLanes = kCols / 8, kRowsOnce = 64 / kLanes;
+  static_assert(64 % kLanes == 0, "whole rows");
+  const int n0 = tile.w * C::kOut + ww * kCols;
+  const auto place = [](int r, int c) { return r * C::kWaveW + (C::kWaveW == 64 ? c ^ r : c ^ (r >> 1)) * 4; };
+  const int el = lane_anew(), col = el % kLanes * 8, row = el / kLanes;
+  const bool fast = p.whole && n0 + kCols <= p.n_out;
+  Columns c;
+  if (fast) c.init<C::kGated>(p, n0 + col);
+  constexpr int kHalves = kBlock / 16;   // a block's rows 16 at a time
+#pragma unroll
+  for (int i = 0; i < C::kBlocksX * kHalves; ++i) {
+    if (kHalves == 1 || el % kBlock / 16 == i % kHalves) {
+#pragma unroll
+      for (int j = 0; j < C::kBlocksW; ++j)
+#pragma unroll
+        for (int q = 0; q < C::Op::kQuads; ++q) {
+          const Acc& c4 = acc[i / kHalves][j];
+          const f32x4 v = {c4[4 * q], c4[4 * q + 1], c4[4 * q + 2], c4[4 * q + 3]};
+          *reinterpret_cast<f32x4*>(mine + place(el % 16, (j * kBlock + q * C::Op::kStride) / 4 + el / kBlock)) = v;
+        }
+    }
+    __builtin_amdgcn_wave_barrier();   // (a wave's own LDS accesses are in order)
+    if (p.parts > 1 || fast) {
+#pragma unroll
+      for (int r = 0; r < 16; r += kRowsOnce) {
+        if (kRowsOnce > 16 && row >= 16) continue;
+        const int64_t m = m0 + i * 16 + r + row;
+        const int from = C::kGated ? col / 32 * 64 + col % 32 : col;
+        float a[8], b[8];
+        load_heads<4>(mine + place(r + row, from / 4), reinterpret_cast<float(&)[4]>(a[0]));
+        load_heads<4>(mine + place(r + row, from / 4 + 1), reinterpret_cast<float(&)[4]>(a[4]));
+        if (C::kGated) {
+          load_heads<4>(mine + place(r + row, from / 4 + 8), reinterpret_cast<float(&)[4]>(b[0]));
+          load_heads<4>(mine + place(r + row, from / 4 + 9), reinterpret_cast<float(&)[4]>(b[4]));
+        }
+        if (m >= p.n_rows) continue;
+        if (p.parts > 1) {
+          if (n0 + col < p.partial_cols) {
+            float* o = p.partial + tile.part * p.partial_part + m * p.partial_cols * (C::kGated ? 2 : 1) + n0 + col;
+            store_heads<8>(o, a);
+            if (C::kGated) store_heads<8>(o + p.partial_cols, b);
+          }
+        } else {
+          finish<C::kGated>(p, c, m, a, b);
+        }
+      }
     } else {
-      const int r = row - C::kX, block = r >> 5, in = ((r >> 2) & 1) * 16 + ((r >> 3) & 3) * 4 + (r & 3);
-      at[i] = (uint32_t)((kGated ? block >> 1 : block) * 32 + in) * (uint32_t)p.w_row + chunk * 16;
-    }
-  }
-  const int rows_w = left_w < C::kOut ? left_w : C::kOut;
-
-  f32x16 acc[kBlocksX][kBlocksW];
-#pragma unroll
-  for (int i = 0; i < kBlocksX; ++i)
-#pragma unroll
-    for (int j = 0; j < kBlocksW; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-
-  const int wx = wave / kWavesW, ww = wave % kWavesW;
-  for (int k = k_begin; k < k_end; k += kStepBytes) {
-    const int left = k_end - k;
-    const bool past = chunk * 16 >= left;
-    const char* xb = p.x + m0 * p.x_row + k;
-    const char* wb = p.w + (int64_t)n0 * p.w_row + k;
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)xb, 0, (int)((left_x - 1) * p.x_row) + left, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)wb, 0, (int)((rows_w - 1) * p.w_row) + left, 0x00027000);
-    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(wb + (int64_t)p.n_out * p.w_row), 0, (int)((rows_w - 1) * p.w_row) + left, 0x00027000);
-#pragma unroll
-    for (int i = 0; i < C::kLoads; ++i) {
-      const int first = 8 * (wave + i * C::kWaves);
-      const bool of_x = first < C::kX;
-      const bool value = kGated && !of_x && (((first - C::kX) >> 5) & 1);
-      LdsVoid* to = (LdsVoid*)(lds + first * kStepBytes);
-      const uint32_t from = past ? 0x7ffffff0u : at[i];
-      if (of_x) __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, to, 16, from, 0, 0, 0);
-      else if (value) __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, to, 16, from, 0, 0, 0);
-      else __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, to, 16, from, 0, 0, 0);
-    }
-    wait_for_loads<0>();
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 4 / Op::kPairs; ++s) {
-      typename Op::Frag x[kBlocksX], w[kBlocksW];
-#pragma unroll
-      for (int i = 0; i < kBlocksX; ++i) {
-        u32x4 c[Op::kPairs];
-#pragma unroll
-        for (int q = 0; q < Op::kPairs; ++q)
-          c[q] = *reinterpret_cast<const u32x4*>(lds + tile_place((wx * kBlocksX + i) * 32 + (lane & 31), 2 * (s * Op::kPairs + q) + (lane >> 5)));
-        __builtin_memcpy(&x[i], c, sizeof(x[i]));
+#pragma unroll 1
+      for (int at = el; at < 16 * kCols; at += 64) {
+        const int r = at / kCols, cc = at % kCols, from = C::kGated ? cc / 32 * 64 + cc % 32 : cc;
+        const int64_t m = m0 + i * 16 + r;
+        const float a = mine[place(r, from / 4) + from % 4], b = C::kGated ? mine[place(r, from / 4 + 8) + from % 4] : 0.f;
+        if (m < p.n_rows && n0 + cc < p.n_out) finish_one<C::kGated>(p, m, n0 + cc, a, b);
       }
-#pragma unroll
-      for (int j = 0; j < kBlocksW; ++j) {
-        u32x4 c[Op::kPairs];
-#pragma unroll
-        for (int q = 0; q < Op::kPairs; ++q)
-          c[q] = *reinterpret_cast<const u32x4*>(lds + tile_place(C::kX + (ww * kBlocksW + j) * 32 + (lane & 31), 2 * (s * Op::kPairs + q) + (lane >> 5)));
-        __builtin_memcpy(&w[j], c, sizeof(w[j]));
-      }
-#pragma unroll
-      for (int i = 0; i < kBlocksX; ++i)
-#pragma unroll
-        for (int j = 0; j < kBlocksW; ++j) acc[i][j] = Op::mma(w[j], x[i], acc[i][j]);
     }
-    __syncthreads();
+    __builtin_amdgcn_wave_barrier();
   }
-
-#pragma unroll
-  for (int i = 0; i < kBlocksX; ++i)
-#pragma unroll
-    for (int j = 0; j < kBlocksW; j += kGated ? 2 : 1) {
-      const int64_t m = m0 + (wx * kBlocksX + i) * 32 + (lane & 31);
-      const int n = n0 + (ww * kBlocksW + j) * (kGated ? 16 : 32) + (lane >> 5) * 16;
-      float a[16], b[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) a[e] = acc[i][j][e], b[e] = kGated ? acc[i][j + (kGated ? 1 : 0)][e] : 0.f;
-      finish<16>(p, m, n, a, b);
-    }
 }
 
 }  // namespace gc
