@@ -2,43 +2,97 @@
 //
 //   p = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,  out = act(p) (* p of the value rows) + residual
 #include <algorithm>
+#include <cmath>
 
-#include "gc_linear_tiles.h"
+#include "gc_linear_plan.h"
 
 namespace gc {
 namespace {
 
-// Tiles of a launch, at most (times the parts of the inner dimension they fit an int).
-constexpr int64_t kMostTiles = 1 << 20;
+// What a launch of tiles takes, in microseconds, from timings: a step with one tile on a compute unit, with two, and the
+// rest of a tile.
+struct TileCost {
+  int kind, x, w;
+  double one, two, rest;     // two = 0: a unit holds one
+};
+constexpr TileCost kCosts[] = {
+    {kLinearTiles64, 64, 128, 0.42, 0.75, 1.5}, {kLinearTiles128, 128, 128, 0.45, 1.06, 2.5}, {kLinearTiles256, 256, 256, 1.35, 0, 8}};
+constexpr TileCost kCostsF32[] = {
+    {kLinearTiles64, 64, 128, 1.2, 2.05, 1.5}, {kLinearTiles128, 128, 128, 2.05, 4.0, 2.5}, {kLinearTiles256, 128, 256, 3.75, 0, 4}};
 
-constexpr int kCus = 256;
+// Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 14 us; in tiles with
+// parts 16); a wave's share of a row where there are few weight rows is cut by more waves, then by parts (16 x 1024 gated x
+// 2736 13 us whole, 9 in four).  Else the tiles, and the parts of the inner dimension, that take least: 4096^3 bfloat16 183, 137 and
+// 104 us with tiles of 64, 128 and 256, 1024^3 10.6, 11.3 and 26, 128 x 1024 x 4096 28, 29 and 74 whole, 12.6 with 64 in eight parts.
+LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated) {
+  const int steps = (row_bytes + kStepBytes - 1) / kStepBytes;
+  const auto in_parts = [&](int kind, int parts, int waves) {
+    const int each = (steps + parts - 1) / parts;
+    return LinearPlan{kind, (steps + each - 1) / each, each * kStepBytes, waves};
+  };
+  const double w_rows = gated ? 2.0 * n_out : n_out;
+  if (n_rows <= kLinearFewRows) {
+    const int blocks = (n_out + 15) / 16;
+    const int parts = std::min({8, kCus / blocks, row_bytes / 1280});
+    return in_parts(kLinearFew, std::max(1, parts), blocks < 2 * kCus ? 16 : 4);
+  }
+  LinearPlan best = {};
+  double least = 0;
+  for (const TileCost& c : dtype == GC_F32 ? kCostsF32 : kCosts) {
+    const double tiles = std::ceil((double)n_rows / c.x) * std::ceil(w_rows / c.w);
+    for (const int parts : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (parts > 1 && (steps < 2 * parts || tiles * parts > 4 * kCus)) break;
+      const LinearPlan plan = in_parts(c.kind, parts, 0);
+      const double blocks = tiles * plan.parts, each = plan.part_bytes / kStepBytes, at_once = c.two > 0 ? 2 * kCus : kCus;
+      const double rounds = std::floor(blocks / at_once), over = blocks - rounds * at_once;
+      const double one = c.rest + each * c.one, two = c.two > 0 ? c.rest + each * c.two : one;
+      double t = rounds * two + (over > kCus ? two : over > 0 ? one : 0);
+      // the parts' sums out and back, and their launch
+      if (plan.parts > 1) t += 3.5 + 8e-6 / 4 * plan.parts * (double)n_rows * w_rows;
+      if (least > 0 && t >= least) continue;
+      least = t, best = plan;
+      if (c.kind == kLinearTiles128 && blocks <= kCus) best.kind = kLinearTiles128Deep;
+    }
+  }
+  return best;
+}
 
-template <class C>
-void launch_tiles(LinearArgs p, hipStream_t stream) {
-  const int64_t tiles_w = (p.n_out + C::kOut - 1) / C::kOut, most = std::max<int64_t>(1, kMostTiles / tiles_w) * C::kX;
-  const int64_t n = p.n_rows, width = (p.gated ? 2 : 1) * (int64_t)p.partial_cols;
-  for (int64_t r = 0; r < n; r += most) {
-    p.n_rows = std::min(n - r, most);
-    const int64_t tiles_x = (p.n_rows + C::kX - 1) / C::kX;
-    const int64_t blocks = tiles_x * tiles_w * p.parts;
-    k_linear_tiles<C><<<(unsigned)blocks, C::kThreads, 0, stream>>>(p, (int)tiles_x, (int)tiles_w);
-    p.x += most * p.x_row;
-    if (p.x_scale) p.x_scale += most;
-    if (p.residual) p.residual += most * p.residual_row;
-    if (p.partial) p.partial += most * width;
-    p.out += most * p.out_row;
+// Sums of the parts, and the epilogue: eight columns a thread.
+template <bool kGated>
+__global__ __launch_bounds__(256) void k_linear_join(const LinearArgs p, int64_t groups) {
+  const int row_groups = p.partial_cols / 8;
+  for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g < groups; g += (int64_t)gridDim.x * 256) {
+    const int64_t m = g / row_groups;
+    const int n = (int)(g - m * row_groups) * 8;
+    const float* from = p.partial + m * p.partial_cols * (kGated ? 2 : 1) + n;
+    float a[8], b[8];
+    load_heads<8>(from, a);
+    if (kGated) load_heads<8>(from + p.partial_cols, b);
+    for (int part = 1; part < p.parts; ++part) {
+      float add[8];
+      load_heads<8>(from + part * p.partial_part, add);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] += add[i];
+      if (kGated) {
+        load_heads<8>(from + part * p.partial_part + p.partial_cols, add);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] += add[i];
+      }
+    }
+    if (p.whole && n + 8 <= p.n_out) {
+      Columns c;
+      c.init<kGated>(p, n);
+      finish<kGated>(p, c, m, a, b);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n + i < p.n_out) finish_one<kGated>(p, m, n + i, a[i], kGated ? b[i] : 0.f);
+    }
   }
 }
 
-template <class Op>
-void launch_linear(const LinearArgs& p, hipStream_t stream) {
-  if (p.gated) launch_tiles<Tiles<Op, 2, 4, 128, 64, true>>(p, stream);
-  else launch_tiles<Tiles<Op, 2, 4, 128, 64, false>>(p, stream);
-}
-template <>
-void launch_linear<F32>(const LinearArgs& p, hipStream_t stream) {
-  if (p.gated) launch_tiles<Tiles<F32, 2, 4, 64, 64, true>>(p, stream);
-  else launch_tiles<Tiles<F32, 2, 4, 64, 64, false>>(p, stream);
+int64_t workspace_bytes(const LinearPlan& plan, int64_t n_rows, int n_out, int gated) {
+  return plan.parts > 1 ? plan.parts * n_rows * ((n_out + 7) / 8 * 8) * (gated ? 2 : 1) * (int64_t)sizeof(float) : 0;
 }
 
 constexpr int64_t kMostStride = (int64_t)1 << 40;
@@ -61,8 +115,7 @@ using namespace gc;
 extern "C" int64_t gc_linear_workspace_bytes(int64_t n_rows, int n_out, int n_in, int dtype, int gated) {
   clear_error();
   if (check_sizes(n_rows, n_out, n_in, dtype, "gc_linear_workspace_bytes")) return -1;
-  (void)gated;
-  return 0;
+  return workspace_bytes(choose(n_rows, n_out, n_in * row_type_bytes(dtype), dtype, gated), n_rows, n_out, gated);
 }
 
 extern "C" int gc_linear(const gc_rows* x, const float* x_scale, const gc_rows* w, const float* w_scale, int64_t n_rows,
@@ -83,7 +136,8 @@ extern "C" int gc_linear(const gc_rows* x, const float* x_scale, const gc_rows* 
     return rc;
   if ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale) | reinterpret_cast<uintptr_t>(bias)) & 3)
     return fail(GC_ERR_ALIGN, "%s: x_scale, w_scale or bias misaligned", who);
-  const int64_t need = gc_linear_workspace_bytes(n_rows, n_out, n_in, dtype, gated);
+  const LinearPlan plan = choose(n_rows, n_out, n_in * row_type_bytes(dtype), dtype, gated);
+  const int64_t need = workspace_bytes(plan, n_rows, n_out, gated);
   if (need > 0 && !workspace) return fail(GC_ERR_ARG, "%s: workspace is null", who);
   if (ws_bytes < (size_t)need)
     return fail(GC_ERR_CAPACITY, "%s: workspace of %zu bytes is below the %lld required", who, ws_bytes, (long long)need);
@@ -113,10 +167,17 @@ extern "C" int gc_linear(const gc_rows* x, const float* x_scale, const gc_rows* 
   p.n_rows = n_rows, p.n_out = n_out, p.row_bytes = (int)(n_in * es);
   p.act = act, p.gated = gated != 0, p.out_f32 = out_dtype == GC_F32;
   p.whole = rows_aligned(*out, n_rows, 16, (int)eo) && (!residual || rows_aligned(*residual, n_rows, 16, (int)eo));
-  p.parts = 1, p.part_bytes = (p.row_bytes + kStepBytes - 1) / kStepBytes * kStepBytes;
-  if (dtype == GC_F32) launch_linear<F32>(p, stream);
-  else if (dtype == GC_BF16) launch_linear<BF16>(p, stream);
-  else if (p.out_f32) launch_linear<E4M3Exact>(p, stream);
-  else launch_linear<E4M3>(p, stream);
+  p.parts = plan.parts, p.part_bytes = plan.part_bytes;
+  p.partial = reinterpret_cast<float*>(workspace);
+  p.partial_cols = (n_out + 7) / 8 * 8, p.partial_part = n_rows * p.partial_cols * (gated ? 2 : 1);
+  if (dtype == GC_F32) launch_linear_f32(p, plan, stream);
+  else if (dtype == GC_BF16) launch_linear_bf16(p, plan, stream);
+  else launch_linear_e4m3(p, plan, stream);
+  if (plan.parts > 1) {
+    const int64_t groups = n_rows * (p.partial_cols / 8);
+    const unsigned blocks = (unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16);
+    if (gated) k_linear_join<true><<<blocks, 256, 0, stream>>>(p, groups);
+    else k_linear_join<false><<<blocks, 256, 0, stream>>>(p, groups);
+  }
   return after_launch(stream, who);
 }

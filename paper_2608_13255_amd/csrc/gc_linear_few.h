@@ -1,0 +1,103 @@
+// Matrix products of few rows: every weight is read once, from memory to registers.
+//
+// A wave takes 16 weight rows (the first operand) 64 bytes of each at a time,
+// and the waves of a block the same rows' other bytes by turns; their sums
+// meet in LDS.  x, read as often as there are blocks, comes from the caches.
+#pragma once
+
+#include "gc_linear.h"
+
+namespace gc {
+
+// Operands of 16 rows: a 16-byte chunk a lane, row lane % 16, chunk lane / 16 of four.
+struct FewF32 {
+  __device__ __forceinline__ static f32x4 mma(const u32x4& w, const u32x4& x, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i]), __uint_as_float(x[i]), c, 0, 0, 0);
+    return c;
+  }
+};
+struct FewBF16 {
+  __device__ __forceinline__ static f32x4 mma(const u32x4& w, const u32x4& x, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+  }
+};
+struct FewE4M3 {   // as bfloat16, which holds them exactly: there is time for it
+  __device__ __forceinline__ static f32x4 mma(const u32x4& w, const u32x4& x, f32x4 c) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(E4M3Exact::half(w, i), E4M3Exact::half(x, i), c, 0, 0, 0);
+    return c;
+  }
+};
+
+constexpr int kFewStep = 64;     // bytes of a row that a wave takes at a time
+constexpr uint32_t kFewNowhere = 0x7ffffff0u;   // past any range
+
+constexpr int kFewUnroll = 8;    // steps that are read before they are used
+
+// 16 rows of x, 16 weight rows (gated: gates and as many values) and kWaves waves a block.
+template <class Op, int kWaves, bool kGated>
+__global__ __launch_bounds__(kWaves * 64) void k_linear_few(const LinearArgs p) {
+  constexpr int kBlocks = kGated ? 2 : 1;
+  __shared__ f32x4 sums[kWaves][kBlocks][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int k_begin = blockIdx.y * p.part_bytes;
+  const int k_end = p.row_bytes - k_begin < p.part_bytes ? p.row_bytes : k_begin + p.part_bytes;
+  const int rows_x = (int)p.n_rows, rows_w = p.n_out - n0 < 16 ? p.n_out - n0 : 16;
+  const int chunk16 = lane / 16 * 16;
+  const uint32_t x_at = (uint32_t)(lane % 16) * (uint32_t)p.x_row + chunk16, w_at = (uint32_t)(lane % 16) * (uint32_t)p.w_row + chunk16;
+  const char* wb = p.w + (int64_t)n0 * p.w_row;
+  const char* vb = wb + (int64_t)p.n_out * p.w_row;
+  const int range_x = (int)((rows_x - 1) * p.x_row), range_w = (int)((rows_w - 1) * p.w_row);
+
+  f32x4 acc[kBlocks];
+#pragma unroll
+  for (int j = 0; j < kBlocks; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k = k_begin + wave * kFewStep * kFewUnroll; k < k_end; k += kWaves * kFewStep * kFewUnroll) {
+    u32x4 w[kFewUnroll][kBlocks], x[kFewUnroll];
+#pragma unroll
+    for (int u = 0; u < kFewUnroll; ++u) {
+      const int at = k + u * kFewStep, left = k_end - at;
+      // past the end of a row, and past the last row, zeros arrive
+      const bool past = chunk16 >= left;
+      const uint32_t from_w = past ? kFewNowhere : w_at, from_x = past ? kFewNowhere : x_at;
+      const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)(wb + at), 0, left > 0 ? range_w + left : 0, 0x00027000);
+      const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(vb + at), 0, left > 0 ? range_w + left : 0, 0x00027000);
+      const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(p.x + at), 0, left > 0 ? range_x + left : 0, 0x00027000);
+      w[u][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, from_w, 0, 2));
+      if (kGated) w[u][kBlocks - 1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, from_w, 0, 2));
+      x[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, from_x, 0, 0));
+    }
+    __builtin_amdgcn_sched_barrier(0);   // all reads before any use
+#pragma unroll
+    for (int u = 0; u < kFewUnroll; ++u)
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) acc[j] = Op::mma(w[u][j], x[u], acc[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < kBlocks; ++j) sums[wave][j][lane] = acc[j];
+  __syncthreads();
+
+  // one output a thread: row m of x and weight row n are lane n / 4 * 16 + m of a block's sums, element n % 4
+  const int n = threadIdx.x % 16, m = threadIdx.x / 16;
+  if (m >= rows_x || n >= rows_w) return;
+  const int from = n / 4 * 16 + m;
+  float a = 0.f, b = 0.f;
+#pragma unroll
+  for (int v = 0; v < kWaves; ++v) {
+    a += sums[v][0][from][n % 4];
+    if (kGated) b += sums[v][kBlocks - 1][from][n % 4];
+  }
+  if (p.parts > 1) {
+    float* o = p.partial + blockIdx.y * p.partial_part + (int64_t)m * p.partial_cols * (kGated ? 2 : 1) + n0 + n;
+    o[0] = a;
+    if (kGated) o[p.partial_cols] = b;
+  } else {
+    finish_one<kGated>(p, m, n0 + n, a, b);
+  }
+}
+
+}  // namespace gc

@@ -4,7 +4,7 @@
 // read from memory to LDS 128 bytes of each row at a time (a step), straight and
 // 16 bytes a lane, with chunk c of row r at place c ^ (r / 2 % 8): then
 // 16 rows' same chunk lie in 16 different places of the 256 bytes that the banks span.
-// Two steps are in LDS or on their way: when every wave has read a step, its place is filled with the second one after it.
+// kBuffers steps are in LDS or on their way: when every wave has read a step, its place is filled again.
 //
 // The weights are the first operand, so an accumulator's lane holds one row of
 // x and groups of four consecutive weight rows.  Gated products take 32 gate and 32 value rows by
@@ -36,7 +36,7 @@ constexpr uint32_t kNowhere = 0x7ffffff0u;   // past any range
 // Blocks that share rows of x, or of the weights, and the steps between asking for a line and its load.
 constexpr int kAheadW = 4, kAheadX = 8, kAheadSteps = 2;
 
-template <class Op_, int kWavesX_, int kWavesW_, int kRowsX, int kRowsW, bool kGated_>
+template <class Op_, int kWavesX_, int kWavesW_, int kRowsX, int kRowsW, int kBuffers_, bool kGated_>
 struct Tiles {
   typedef Op_ Op;
   static constexpr int kWavesX = kWavesX_, kWavesW = kWavesW_;
@@ -46,16 +46,16 @@ struct Tiles {
   static constexpr int kX = kWavesX * kRowsX, kW = kWavesW * kRowsW;
   static constexpr int kWaveX = kRowsX, kWaveW = kRowsW;
   static constexpr int kOut = kGated ? kW / 2 : kW;      // columns of the output
-  static constexpr int kBuffers = 2;
+  static constexpr int kBuffers = kBuffers_;
   static constexpr int kStage = (kX + kW) * kStepBytes;
   static constexpr int kLoads = (kX + kW) / 8 / kWaves;      // a wave's, a step
   static constexpr int kGroups = 64 / Op::kBlock;            // of lanes
   static constexpr int kParts = 8 / kGroups / Op::kChunks;   // of a step: fragments that products take
   static constexpr int kFrags = kBlocksX + kBlocksW;
-  // the epilogue's place of a wave: 16 rows of its columns
+  // the epilogue's place of a wave: 16 rows of its columns, where the steps lay
   static constexpr int kWaveFloats = 16 * kRowsW;
-  static constexpr int kLds = kBuffers * kStage + kWaves * kWaveFloats * 4;
-  static constexpr int kBlocksPerCu = 163840 / kLds;
+  static constexpr int kLds = kBuffers * kStage + kWaves * 256;
+  static_assert(kBuffers * kStage >= kWaves * kWaveFloats * 4, "room for the epilogue");
   static_assert(kLds <= 163840 && (kRowsW == 64 || kRowsW == 32), "LDS of a compute unit, and what the epilogue's permutation covers");
   static_assert((kX + kW) / 8 % kWaves == 0 && kX / 8 % kWaves == 0 && kWaves % 4 == 0, "whole loads");
   static_assert(!kGated || kRowsW % 64 == 0, "gate and value in one wave");
@@ -106,6 +106,7 @@ struct StageLoader {
   const char *xb, *wb, *ab;
   int range_x, range_w, range_a;   // bytes from the wave's first row to the first byte of the last one
   int left;                        // bytes of a row from here to the part's end
+  int64_t values;                  // bytes from the gates' rows to the values'
   int chunk16;
   uint32_t at[kLoadsX + kLoadsW], ahead;
 
@@ -137,15 +138,17 @@ struct StageLoader {
       ahead = lane < kRowsW ? (uint32_t)row * (uint32_t)p.w_row : kNowhere;
     }
     // Load i takes the rows 8 (wave + i kWaves) + lane / 8, its places lane % 8.  Of the weights' places every other 32
-    // are values', so with eight waves a wave's loads are all of gates' rows or all of values', 32 apart.
-    static_assert(!C::kGated || C::kWaves == 8, "gates or values");
-    if (C::kGated && ((wave >> 2) & 1)) wb = vb;
+    // are values': with eight waves a wave's loads are all of gates' rows or all of values', 32 apart, with four they
+    // alternate.
+    static_assert(!C::kGated || C::kWaves == 8 || C::kWaves == 4, "gates or values");
+    values = C::kGated ? (int64_t)p.n_out * p.w_row : 0;
+    if (C::kGated && C::kWaves == 8 && ((wave >> 2) & 1)) wb = vb;
     chunk16 = ((lane ^ (lane >> 4) ^ (wave << 2)) & 7) * 16;
 #pragma unroll
     for (int i = 0; i < kLoadsX; ++i) at[i] = (uint32_t)(i * kLoadRows + 8 * wave + (lane >> 3)) * (uint32_t)p.x_row + chunk16;
 #pragma unroll
     for (int i = 0; i < kLoadsW; ++i)
-      at[kLoadsX + i] = (uint32_t)((C::kGated ? i * kLoadRows / 2 + 8 * (wave & 3) : i * kLoadRows + 8 * wave) + (lane >> 3)) * (uint32_t)p.w_row + chunk16;
+      at[kLoadsX + i] = (uint32_t)((!C::kGated ? i * kLoadRows + 8 * wave : C::kWaves == 8 ? i * 32 + 8 * (wave & 3) : i / 2 * 32 + 8 * wave) + (lane >> 3)) * (uint32_t)p.w_row + chunk16;
   }
   // A step's loads.  Past the end nothing is read, and the places get zeros.
   __device__ __forceinline__ void load(char* lds, int wave) {
@@ -155,9 +158,14 @@ struct StageLoader {
 #pragma unroll
     for (int i = 0; i < kLoadsX; ++i)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (LdsVoid*)(lds + 8 * (wave + i * C::kWaves) * kStepBytes), 16, past ? kNowhere : at[i], 0, 0, 0);
+    const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(wb + values), 0, left > 0 ? range_w + left : 0, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < kLoadsW; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (LdsVoid*)(lds + (C::kX + 8 * (wave + i * C::kWaves)) * kStepBytes), 16, past ? kNowhere : at[kLoadsX + i], 0, 0, 0);
+    for (int i = 0; i < kLoadsW; ++i) {
+      LdsVoid* to = (LdsVoid*)(lds + (C::kX + 8 * (wave + i * C::kWaves)) * kStepBytes);
+      const uint32_t from = past ? kNowhere : at[kLoadsX + i];
+      if (C::kGated && C::kWaves == 4 && i % 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, to, 16, from, 0, 0, 0);
+      else __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, to, 16, from, 0, 0, 0);
+    }
     xb += kStepBytes, wb += kStepBytes, left -= kStepBytes;
   }
   // Asks for the lines of the step kAheadSteps after the one to be loaded next, so that they are in the L2 by then.  Blocks that run at the same time on
@@ -215,8 +223,7 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wx = wave / C::kWavesW, ww = wave % C::kWavesW;
   const int parts = args.parts;
-  float* mine = reinterpret_cast<float*>(lds + C::kBuffers * C::kStage) + wave * C::kWaveFloats;
-  char* junk = reinterpret_cast<char*>(mine);
+  char* junk = lds + C::kBuffers * C::kStage + wave * 256;
 
   constexpr int kBlock = C::Op::kBlock;
   int lane_at[8 / C::kGroups];
@@ -229,8 +236,8 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
   StageLoader<C> in;
   in.init(tile, wave);
   const int steps = (in.left + kStepBytes - 1) / kStepBytes;
-  in.load(lds, wave);
-  in.load(lds + C::kStage, wave);
+#pragma unroll
+  for (int s = 0; s < C::kBuffers; ++s) in.load(lds + s * C::kStage, wave);
   typedef typename C::Op::Acc Acc;
   constexpr int kElements = 4 * C::Op::kQuads;
   Acc acc[C::kBlocksX][C::kBlocksW];
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
         for (int e = 0; e < kElements; ++e) total[C::kTotals ? i : 0][C::kTotals ? j : 0][e] = 0.f;
   }
 
-  wait_all_but<C::kLoads>();
+  wait_all_but<(C::kBuffers - 1) * C::kLoads>();
   block_barrier();
   Fragments<C> f[2];
   char *now = lds, *next = lds + C::kStage;
@@ -271,8 +278,9 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
         f[(s + 1) & 1].read(now + x_at, now + w_at, lane_at, s + 1);
         if (s == 0) in.ask(junk);
       } else {
-        // every wave has read this step whole, and the next one has arrived
-        wait_all_but<1>();
+        // every wave has read this step whole, and the next one has arrived: at most the loads of the steps after that and
+        // what was asked for in this one are on their way
+        wait_all_but<(C::kBuffers - 2) * C::kLoads + 1>();
         block_barrier();
         f[(s + 1) & 1].read(next + x_at, next + w_at, lane_at, 0);
         in.load(now, wave);
@@ -286,8 +294,8 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
       else beside_products<C, C::kLoads>();
     }
     asm volatile("" ::: "memory");   // the next step's first fragments are read here, not where they are used
-    char* t = now;
-    now = next, next = t;
+    now = next;
+    next = next == lds + (C::kBuffers - 1) * C::kStage ? lds : next + C::kStage;
     if (C::kTotals && k % kTotalSteps == kTotalSteps - 1) add_to_total();
   }
   if (C::kTotals) {
@@ -297,8 +305,10 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
 #pragma unroll
       for (int j = 0; j < C::kBlocksW; ++j) acc[i][j] = total[C::kTotals ? i : 0][C::kTotals ? j : 0];
   }
-  wait_all_but<0>();   // the loads past the end write to LDS as well, and the places asked for to the epilogue's
+  wait_all_but<0>();   // the loads past the end write to LDS as well
+  block_barrier();
 
+  float* mine = reinterpret_cast<float*>(lds) + wave * C::kWaveFloats;
   // Through LDS, 16 rows of the wave at a time: eight consecutive columns a lane.  16-byte chunk c of row r lies at place
   // c ^ r (c ^ r / 2 of rows of 8 chunks).
   const LinearArgs p = args_anew();
