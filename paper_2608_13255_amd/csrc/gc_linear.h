@@ -91,20 +91,26 @@ struct Columns {
   }
 };
 
+// What the epilogue reads of a row: asked for before it is needed, and before the rows in front of it are stored, since the
+// output may be the residual.
+struct RowAhead {
+  u32x4 add[2];
+  float scale;
+  __device__ __forceinline__ void load(const LinearArgs& p, int64_t m, int n) {
+    if (p.residual) {
+      const char* r = p.residual + m * p.residual_row + (int64_t)n * (p.out_f32 ? 4 : 2);
+      add[0] = *reinterpret_cast<const u32x4*>(r);
+      if (p.out_f32) add[1] = *reinterpret_cast<const u32x4*>(r + 16);
+    }
+    if (p.x_scale) scale = p.x_scale[m];
+  }
+};
+
 // The sums a (and b of the value rows) of eight columns of row m to the output, 16 bytes at a time.
 template <bool kGated>
-__device__ __forceinline__ void finish(const LinearArgs& p, const Columns& c, int64_t m, float (&a)[8], float (&b)[8]) {
-  const int es = p.out_f32 ? 4 : 2;
-  float add[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) add[i] = 0.f;
-  if (p.residual) {   // on its way during the arithmetic
-    const char* r = p.residual + m * p.residual_row + (int64_t)c.n * es;
-    if (p.out_f32) load_heads<8>((const float*)r, add);
-    else load_heads<8>((const uint16_t*)r, add);
-  }
+__device__ __forceinline__ void finish(const LinearArgs& p, const Columns& c, int64_t m, const RowAhead& row, float (&a)[8], float (&b)[8]) {
   if (p.x_scale || p.w_scale) {
-    const float xs = p.x_scale ? p.x_scale[m] : 1.f;
+    const float xs = p.x_scale ? row.scale : 1.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = a[i] * xs * c.scale[i];
     if (kGated) {
@@ -119,32 +125,61 @@ __device__ __forceinline__ void finish(const LinearArgs& p, const Columns& c, in
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] *= b[i] + c.value_bias[i];
   }
+  char* o = p.out + m * p.out_row + (int64_t)c.n * (p.out_f32 ? 4 : 2);
+  if (p.out_f32) {
+    if (p.residual) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a[i] += add[i];
-  char* o = p.out + m * p.out_row + (int64_t)c.n * es;
-  if (p.out_f32) store_heads<8>((float*)o, a);
-  else store_heads<8>((uint16_t*)o, a);
+      for (int i = 0; i < 8; ++i) a[i] += __uint_as_float(row.add[i / 4][i % 4]);
+    }
+    store_heads<8>((float*)o, a);
+  } else {
+    if (p.residual) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] += HeadVec<uint16_t, 8>::at(row.add[0], i);
+    }
+    store_heads<8>((uint16_t*)o, a);
+  }
 }
 
 // The same for one column.
+struct Column {
+  int n;
+  float scale, bias, value_scale, value_bias;
+  template <bool kGated>
+  __device__ __forceinline__ void init(const LinearArgs& p, int at) {
+    n = at;
+    scale = p.w_scale ? p.w_scale[n] : 1.f;
+    bias = p.bias ? p.bias[n] : 0.f;
+    if (kGated) {
+      value_scale = p.w_scale ? p.w_scale[p.n_out + n] : 1.f;
+      value_bias = p.bias ? p.bias[p.n_out + n] : 0.f;
+    }
+  }
+};
+struct OneAhead {
+  float add, scale;
+  __device__ __forceinline__ void load(const LinearArgs& p, int64_t m, int n) {
+    add = 0.f, scale = 1.f;
+    if (p.residual) {
+      const char* r = p.residual + m * p.residual_row;
+      add = p.out_f32 ? ((const float*)r)[n] : load_one((const uint16_t*)r + n);
+    }
+    if (p.x_scale) scale = p.x_scale[m];
+  }
+};
 template <bool kGated>
-__device__ __forceinline__ void finish_one(const LinearArgs& p, int64_t m, int n, float sum, float value) {
+__device__ __forceinline__ void finish_one(const LinearArgs& p, const Column& c, int64_t m, const OneAhead& row, float sum, float value) {
   float a[1] = {sum}, b = value;
   if (p.x_scale || p.w_scale) {
-    const float xs = p.x_scale ? p.x_scale[m] : 1.f;
-    a[0] = a[0] * xs * (p.w_scale ? p.w_scale[n] : 1.f);
-    if (kGated) b = b * xs * (p.w_scale ? p.w_scale[p.n_out + n] : 1.f);
+    a[0] = a[0] * row.scale * c.scale;
+    if (kGated) b = b * row.scale * c.value_scale;
   }
-  if (p.bias) a[0] += p.bias[n];
+  a[0] += c.bias;
   activate<1>(a, p.act);
-  if (kGated) a[0] *= b + (p.bias ? p.bias[p.n_out + n] : 0.f);
-  if (p.out_f32) {
-    if (p.residual) a[0] += ((const float*)(p.residual + m * p.residual_row))[n];
-    ((float*)(p.out + m * p.out_row))[n] = a[0];
-  } else {
-    if (p.residual) a[0] += load_one((const uint16_t*)(p.residual + m * p.residual_row) + n);
-    store_one((uint16_t*)(p.out + m * p.out_row) + n, a[0]);
-  }
+  if (kGated) a[0] *= b + c.value_bias;
+  if (p.residual) a[0] += row.add;
+  if (p.out_f32) ((float*)(p.out + m * p.out_row))[c.n] = a[0];
+  else store_one((uint16_t*)(p.out + m * p.out_row) + c.n, a[0]);
 }
 
 // Operand types.  A product takes kBlock rows of either operand; a fragment of
@@ -164,17 +199,15 @@ struct F32 : Blocks32 {
   static constexpr int kChunks = 1, kProducts = 4;   // products of a pair of fragments
   static constexpr bool kTotals = true;
   typedef f32x4 Frag;
-  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[i], c, 0, 0, 0);
-    return c;
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c, int i) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[i], c, 0, 0, 0);
   }
 };
 struct BF16 : Blocks16 {
   static constexpr int kChunks = 1, kProducts = 1;
   static constexpr bool kTotals = false;
   typedef bf16x8 Frag;
-  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c, int) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0);
   }
 };
@@ -196,17 +229,15 @@ struct E4M3Exact : Blocks32 {
     }
     return r;
   }
-  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(half(w, i), half(x, i), c, 0, 0, 0);
-    return c;
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c, int i) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(half(w, i), half(x, i), c, 0, 0, 0);
   }
 };
 struct E4M3 : Blocks32 {
   static constexpr int kChunks = 2, kProducts = 1;
   static constexpr bool kTotals = false;
   typedef i32x8 Frag;
-  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c) {
+  __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c, int) {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);   // (no scales: ones)
   }
 };

@@ -3,6 +3,7 @@
 //   p = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,  out = act(p) (* p of the value rows) + residual
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 
 #include "gc_linear_plan.h"
 
@@ -18,7 +19,15 @@ struct TileCost {
 constexpr TileCost kCosts[] = {
     {kLinearTiles64, 64, 128, 0.42, 0.75, 1.5}, {kLinearTiles128, 128, 128, 0.45, 1.06, 2.5}, {kLinearTiles256, 256, 256, 1.35, 0, 8}};
 constexpr TileCost kCostsF32[] = {
+    {kLinearTiles64x64, 64, 64, 0.7, 1.1, 1.5},
     {kLinearTiles64, 64, 128, 1.2, 2.05, 1.5}, {kLinearTiles128, 128, 128, 2.05, 4.0, 2.5}, {kLinearTiles256, 128, 256, 3.75, 0, 4}};
+
+struct CostList {
+  const TileCost *first, *last;
+  explicit CostList(int dtype) : first(dtype == GC_F32 ? std::begin(kCostsF32) : std::begin(kCosts)), last(dtype == GC_F32 ? std::end(kCostsF32) : std::end(kCosts)) {}
+  const TileCost* begin() const { return first; }
+  const TileCost* end() const { return last; }
+};
 
 // Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 14 us; in tiles with
 // parts 16); a wave's share of a row where there are few weight rows is cut by more waves, then by parts (16 x 1024 gated x
@@ -38,7 +47,8 @@ LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated
   }
   LinearPlan best = {};
   double least = 0;
-  for (const TileCost& c : dtype == GC_F32 ? kCostsF32 : kCosts) {
+  for (const TileCost& c : CostList(dtype)) {
+    if (gated && c.kind == kLinearTiles64x64) continue;
     const double tiles = std::ceil((double)n_rows / c.x) * std::ceil(w_rows / c.w);
     for (const int parts : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (parts > 1 && (steps < 2 * parts || tiles * parts > 4 * kCus)) break;
@@ -81,12 +91,20 @@ __global__ __launch_bounds__(256) void k_linear_join(const LinearArgs p, int64_t
     }
     if (p.whole && n + 8 <= p.n_out) {
       Columns c;
+      RowAhead row;
       c.init<kGated>(p, n);
-      finish<kGated>(p, c, m, a, b);
+      row.load(p, m, n);
+      finish<kGated>(p, c, m, row, a, b);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (n + i < p.n_out) finish_one<kGated>(p, m, n + i, a[i], kGated ? b[i] : 0.f);
+        if (n + i < p.n_out) {
+          Column c;
+          OneAhead row;
+          c.init<kGated>(p, n + i);
+          row.load(p, m, n + i);
+          finish_one<kGated>(p, c, m, row, a[i], kGated ? b[i] : 0.f);
+        }
     }
   }
 }

@@ -77,12 +77,16 @@ __global__ __launch_bounds__(kWaves * 64) void k_linear_few(const LinearArgs p) 
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j) acc[j] = Op::mma(w[u][j], x[u], acc[j]);
   }
+  // one output a thread: row m of x and weight row n
+  const int n = threadIdx.x % 16, m = threadIdx.x / 16;
+  Column c;
+  OneAhead row;
+  if (m < rows_x && n < rows_w && p.parts == 1) c.init<kGated>(p, n0 + n), row.load(p, m, n0 + n);
 #pragma unroll
   for (int j = 0; j < kBlocks; ++j) sums[wave][j][lane] = acc[j];
   __syncthreads();
 
-  // one output a thread: row m of x and weight row n are lane n / 4 * 16 + m of a block's sums, element n % 4
-  const int n = threadIdx.x % 16, m = threadIdx.x / 16;
+  // they are lane n / 4 * 16 + m of a block's sums, element n % 4
   if (m >= rows_x || n >= rows_w) return;
   const int from = n / 4 * 16 + m;
   float a = 0.f, b = 0.f;
@@ -96,7 +100,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_linear_few(const LinearArgs p) 
     o[0] = a;
     if (kGated) o[p.partial_cols] = b;
   } else {
-    finish_one<kGated>(p, m, n0 + n, a, b);
+    finish_one<kGated>(p, c, m, row, a, b);
   }
 }
 

@@ -55,6 +55,7 @@ struct Tiles {
   // the epilogue's place of a wave: 16 rows of its columns, where the steps lay
   static constexpr int kWaveFloats = 16 * kRowsW;
   static constexpr int kLds = kBuffers * kStage + kWaves * 256;
+  static constexpr int kAtOnce = 163840 / kLds > 2 ? 2 : 163840 / kLds;   // blocks on a compute unit
   static_assert(kBuffers * kStage >= kWaves * kWaveFloats * 4, "room for the epilogue");
   static_assert(kLds <= 163840 && (kRowsW == 64 || kRowsW == 32), "LDS of a compute unit, and what the epilogue's permutation covers");
   static_assert((kX + kW) / 8 % kWaves == 0 && kX / 8 % kWaves == 0 && kWaves % 4 == 0, "whole loads");
@@ -217,7 +218,7 @@ __device__ __forceinline__ void beside_products() {
 }
 
 template <class C>
-__global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs args, int tiles_x, int tiles_w) {
+__global__ __launch_bounds__(C::kThreads, C::kAtOnce * C::kWaves / 4) void k_linear_tiles(const LinearArgs args, int tiles_x, int tiles_w) {
   __shared__ __align__(16) char lds[C::kLds];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -286,9 +287,11 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
         in.load(now, wave);
       }
 #pragma unroll
-      for (int i = 0; i < C::kBlocksX; ++i)
+      for (int e = 0; e < C::Op::kProducts; ++e)   // (the next product is on another sum)
 #pragma unroll
-        for (int j = 0; j < C::kBlocksW; ++j) acc[i][j] = C::Op::mma(f[s & 1].w[j], f[s & 1].x[i], acc[i][j]);
+        for (int i = 0; i < C::kBlocksX; ++i)
+#pragma unroll
+          for (int j = 0; j < C::kBlocksW; ++j) acc[i][j] = C::Op::mma(f[s & 1].w[j], f[s & 1].x[i], acc[i][j], e);
       if (s == 0) beside_products<C, 1>();
       else if (s + 1 < C::kParts) beside_products<C, 0>();
       else beside_products<C, C::kLoads>();
@@ -318,10 +321,25 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
   const int n0 = tile.w * C::kOut + ww * kCols;
   const auto place = [](int r, int c) { return r * C::kWaveW + (C::kWaveW == 64 ? c ^ r : c ^ (r >> 1)) * 4; };
   const int el = lane_anew(), col = el % kLanes * 8, row = el / kLanes;
-  const bool fast = p.whole && n0 + kCols <= p.n_out;
+  const bool whole = p.parts > 1 || (p.whole && n0 + kCols <= p.n_out);
+  constexpr int kHalves = kBlock / 16;                              // a block's rows 16 at a time
+  constexpr int kTimes = kRowsOnce < 16 ? 16 / kRowsOnce : 1;       // eight columns a lane
+  constexpr int kOneCol = kCols < 64 ? kCols : 64, kOneRows = 64 / kOneCol, kOneTimes = 4;   // one column a lane
+  static_assert(kCols <= 64, "a lane's column");
+  const auto row_at = [&](int i, int r) {
+    const int64_t m = m0 + i * 16 + r;
+    return m < p.n_rows ? m : p.n_rows - 1;
+  };
   Columns c;
-  if (fast) c.init<C::kGated>(p, n0 + col);
-  constexpr int kHalves = kBlock / 16;   // a block's rows 16 at a time
+  RowAhead ahead[kTimes];
+  if (whole && p.parts == 1) {
+    c.init<C::kGated>(p, n0 + col);
+#pragma unroll
+    for (int r = 0; r < kTimes; ++r) ahead[r].load(p, row_at(0, r * kRowsOnce + row), c.n);
+  }
+  const int one = el % kOneCol;
+  Column c1;
+  if (!whole) c1.init<C::kGated>(p, n0 + one < p.n_out ? n0 + one : p.n_out - 1);
 #pragma unroll
   for (int i = 0; i < C::kBlocksX * kHalves; ++i) {
     if (kHalves == 1 || el % kBlock / 16 == i % kHalves) {
@@ -335,18 +353,25 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
         }
     }
     __builtin_amdgcn_wave_barrier();   // (a wave's own LDS accesses are in order)
-    if (p.parts > 1 || fast) {
+    if (whole) {
+      RowAhead now_row[kTimes];
 #pragma unroll
-      for (int r = 0; r < 16; r += kRowsOnce) {
-        if (kRowsOnce > 16 && row >= 16) continue;
-        const int64_t m = m0 + i * 16 + r + row;
+      for (int r = 0; r < kTimes; ++r) {
+        now_row[r] = ahead[r];
+        if (p.parts == 1 && i + 1 < C::kBlocksX * kHalves) ahead[r].load(p, row_at(i + 1, r * kRowsOnce + row), c.n);
+      }
+#pragma unroll
+      for (int r = 0; r < kTimes; ++r) {
+        const int at = r * kRowsOnce + row;
+        if (kRowsOnce > 16 && at >= 16) continue;
+        const int64_t m = m0 + i * 16 + at;
         const int from = C::kGated ? col / 32 * 64 + col % 32 : col;
         float a[8], b[8];
-        load_heads<4>(mine + place(r + row, from / 4), reinterpret_cast<float(&)[4]>(a[0]));
-        load_heads<4>(mine + place(r + row, from / 4 + 1), reinterpret_cast<float(&)[4]>(a[4]));
+        load_heads<4>(mine + place(at, from / 4), reinterpret_cast<float(&)[4]>(a[0]));
+        load_heads<4>(mine + place(at, from / 4 + 1), reinterpret_cast<float(&)[4]>(a[4]));
         if (C::kGated) {
-          load_heads<4>(mine + place(r + row, from / 4 + 8), reinterpret_cast<float(&)[4]>(b[0]));
-          load_heads<4>(mine + place(r + row, from / 4 + 9), reinterpret_cast<float(&)[4]>(b[4]));
+          load_heads<4>(mine + place(at, from / 4 + 8), reinterpret_cast<float(&)[4]>(b[0]));
+          load_heads<4>(mine + place(at, from / 4 + 9), reinterpret_cast<float(&)[4]>(b[4]));
         }
         if (m >= p.n_rows) continue;
         if (p.parts > 1) {
@@ -356,16 +381,23 @@ __global__ __launch_bounds__(C::kThreads) void k_linear_tiles(const LinearArgs a
             if (C::kGated) store_heads<8>(o + p.partial_cols, b);
           }
         } else {
-          finish<C::kGated>(p, c, m, a, b);
+          finish<C::kGated>(p, c, m, now_row[r], a, b);
         }
       }
     } else {
+      const int from = C::kGated ? one / 32 * 64 + one % 32 : one;
 #pragma unroll 1
-      for (int at = el; at < 16 * kCols; at += 64) {
-        const int r = at / kCols, cc = at % kCols, from = C::kGated ? cc / 32 * 64 + cc % 32 : cc;
-        const int64_t m = m0 + i * 16 + r;
-        const float a = mine[place(r, from / 4) + from % 4], b = C::kGated ? mine[place(r, from / 4 + 8) + from % 4] : 0.f;
-        if (m < p.n_rows && n0 + cc < p.n_out) finish_one<C::kGated>(p, m, n0 + cc, a, b);
+      for (int r0 = el / kOneCol; r0 < 16; r0 += kOneRows * kOneTimes) {
+        OneAhead some[kOneTimes];
+#pragma unroll
+        for (int u = 0; u < kOneTimes; ++u) some[u].load(p, row_at(i, r0 + u * kOneRows), c1.n);
+#pragma unroll
+        for (int u = 0; u < kOneTimes; ++u) {
+          const int r = r0 + u * kOneRows;
+          const int64_t m = m0 + i * 16 + r;
+          const float a = mine[place(r, from / 4) + from % 4], b = C::kGated ? mine[place(r, from / 4 + 8) + from % 4] : 0.f;
+          if (m < p.n_rows && n0 + one < p.n_out) finish_one<C::kGated>(p, c1, m, some[u], a, b);
+        }
       }
     }
     __builtin_amdgcn_wave_barrier();
