@@ -1280,6 +1280,15 @@ def _rows(t: torch.Tensor, name: str) -> _Rows:
     return _Rows(t.data_ptr(), strides[0] if n > 1 else c)
 
 
+def _device_of(x: torch.Tensor, stream) -> int:
+    """The device of a call's tensors, which must be the stream's."""
+    device = x.get_device()
+    at = stream.device_index if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_device()
+    if device != at:
+        raise ValueError(f"tensors are on cuda:{device}, the stream is on cuda:{at}")
+    return device
+
+
 def _like_rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: int) -> _Rows:
     if t.dtype != dtype or t.shape != shape or t.get_device() != device:
         raise ValueError(f"{name} must be {dtype} {list(shape)} on cuda:{device} (got {t.dtype} {list(t.shape)} on "
@@ -1309,7 +1318,7 @@ def gc_add_rms_norm(x: torch.Tensor, residual: torch.Tensor = None, gain: torch.
     if code is None:
         raise ValueError(f"rows must be float32 or bfloat16 (got {x.dtype})")
     n, width = shape = x.shape
-    device = x.get_device()
+    device = _device_of(x, stream)
     if out_dtype is None:
         out_dtype = x.dtype if out is None else out.dtype
     out_code = _ROW_CODES.get(out_dtype)
@@ -1347,7 +1356,7 @@ def gc_quantize_rows(x: torch.Tensor, out: torch.Tensor = None, out_scale: torch
     if code is None:
         raise ValueError(f"rows must be float32 or bfloat16 (got {x.dtype})")
     n, width = shape = x.shape
-    device = x.get_device()
+    device = _device_of(x, stream)
     fresh = []
     if out is None:
         out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
@@ -1386,7 +1395,7 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
         raise ValueError(f"x must be float32, bfloat16 or {torch.float8_e4m3fn} (got {x.dtype})")
     n, n_in = x.shape
     w_rows = w.shape[0]
-    device = x.get_device()
+    device = _device_of(x, stream)
     if w.dtype != x.dtype or w.shape[1] != n_in or w.get_device() != device:
         raise ValueError(f"w must be {x.dtype} [n_out, {n_in}] on {x.device} (got {w.dtype} {list(w.shape)} on {w.device})")
     n_out = w_rows

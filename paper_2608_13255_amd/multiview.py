@@ -1,5 +1,5 @@
-"""Attention of a multi-view denoiser over a slice of the views (Sec. 3.2,
-batch-sliced anchor forward).
+"""Attention, and whole blocks, of a multi-view denoiser over a slice of the
+views (Sec. 3.2, batch-sliced anchor forward).
 
 A cached step runs the denoiser on the anchor views only, and every token
 keeps the structural index and the rotary slot it has among all views.  Only
@@ -18,12 +18,12 @@ from __future__ import annotations
 import math
 from collections import OrderedDict
 from dataclasses import dataclass, field
-from typing import List, Optional, Sequence, Set, Tuple
+from typing import Dict, List, Optional, Sequence, Set, Tuple
 
 import torch
 
-from . import (GC_MAX_VIEWS, GC_ROPE_HALF, AttentionPlan, gc_attention, gc_attention_plan, gc_qk_norm_rope,
-               gc_rope_table)
+from . import (GC_ACT_SILU, GC_MAX_VIEWS, GC_ROPE_HALF, AttentionPlan, gc_add_rms_norm, gc_attention, gc_attention_plan,
+               gc_linear, gc_qk_norm_rope, gc_quantize_rows, gc_rope_table)
 
 
 @dataclass
@@ -52,23 +52,14 @@ class TokenSlice:
         return {**self.__dict__, "known_streams": set()}
 
 
-class MultiViewAttention:
-    """softmax(q k) v of each asset's foreground tokens, with per-head RMS
-    norms of queries and keys and rotary positions, between a fused input
-    projection and an output projection.  The forward pass only: a call that
-    torch would record for a gradient is refused.  One layer may be called
-    under several streams and from several threads at the same time."""
+class _SlicedAttention:
+    """What follows from the position maps and the views at hand, and
+    attention between its projections."""
 
     MOST_SLICES = GC_MAX_VIEWS + 1   # a rotation's distinct sets, and all views
 
-    def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int,
-                 dtype: torch.dtype = torch.bfloat16, sections: Optional[Sequence[int]] = None, base: float = 10000.0,
-                 generator: Optional[torch.Generator] = None):
-        """pos: device float32 [B, N, H, W, 3] position maps (NaN: background).
-        sections: columns of the rotation for the view, row and column axes
-        (default: the whole head, a quarter of it for the view).  The weights
-        are drawn from the generator; load others into w_qkv [width, (heads +
-        2 kv_heads) dim], w_out [heads dim, width], q_gain and k_gain [dim]."""
+    def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int, dtype: torch.dtype,
+                 sections: Optional[Sequence[int]], base: float):
         self.B, self.N, self.H, self.W = pos.shape[:4]
         self.width, self.heads, self.kv_heads, self.dim, self.dtype = width, heads, kv_heads, dim, dtype
         if sections is None:
@@ -78,9 +69,6 @@ class MultiViewAttention:
         dev = pos.device
         self.foreground = torch.isfinite(pos).all(-1)                     # [B, N, H, W]
         self.table = gc_rope_table(max(self.N, self.H, self.W), self.sections, base, device=dev)
-        rand = lambda *shape: torch.randn(shape, generator=generator, device=dev)
-        self.w_qkv = (rand(width, (heads + 2 * kv_heads) * dim) / math.sqrt(width)).to(dtype)
-        self.w_out = (rand(heads * dim, width) / math.sqrt(heads * dim)).to(dtype)
         self.q_gain = torch.ones(dim, dtype=torch.float32, device=dev)
         self.k_gain = torch.ones(dim, dtype=torch.float32, device=dev)
         self._slices: OrderedDict[Tuple[int, ...], TokenSlice] = OrderedDict()   # the one used last at the end
@@ -108,24 +96,124 @@ class MultiViewAttention:
             self._slices.popitem(last=False)
         return got
 
-    def __call__(self, x: torch.Tensor, views: Sequence[int]) -> torch.Tensor:
-        """x [B, len(views), H, W, width] of the layer's type -> the layer's
-        output on foreground tokens, zeros on the background."""
+    def _tokens(self, x: torch.Tensor, views: Sequence[int], weights: Sequence[Optional[torch.Tensor]]):
+        """(slice, its tokens of x), after the checks of a call."""
         shape = (self.B, len(views), self.H, self.W, self.width)
         if x.shape != shape or x.dtype != self.dtype or x.device != self.foreground.device:
             raise ValueError(f"x must be {self.dtype} {list(shape)} on {self.foreground.device} (got {x.dtype} "
                              f"{list(x.shape)} on {x.device})")
-        if torch.is_grad_enabled() and any(t.requires_grad for t in (x, self.w_qkv, self.w_out, self.q_gain, self.k_gain)):
+        if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, *weights)):
             raise ValueError("the layer has no gradient: call it under torch.no_grad(), or on tensors that require none")
         s = self.slice(views)
         s.used_here()
+        return s, x.reshape(-1, self.width)[s.index]
+
+    def _attend(self, qkv: torch.Tensor, s: TokenSlice) -> torch.Tensor:
+        """Attention [tokens, heads, dim] of the fused projection's rows, whose queries and keys are normed in place."""
         H, Hk, D = self.heads, self.kv_heads, self.dim
-        tokens = x.reshape(-1, self.width)[s.index]
-        qkv = (tokens @ self.w_qkv).view(-1, H + 2 * Hk, D)
-        q, k, v = qkv.split([H, Hk, Hk], dim=1)
+        q, k, v = qkv.view(-1, H + 2 * Hk, D).split([H, Hk, Hk], dim=1)
         gc_qk_norm_rope(q, k, self.q_gain, self.k_gain, s.positions, self.table, sections=self.sections,
                         layout=GC_ROPE_HALF, q_out=q, k_out=k)            # where the projection left them
-        out, _ = gc_attention(q, k, v, s.plan)
-        y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)          # (zeros_like keeps a permuted x's order)
-        y.view(-1, self.width)[s.index] = out.view(-1, H * D) @ self.w_out
-        return y
+        return gc_attention(q, k, v, s.plan)[0]
+
+    def _spread(self, y: torch.Tensor, x: torch.Tensor, s: TokenSlice) -> torch.Tensor:
+        """Tokens in x's shape, zeros on the background."""
+        out = torch.zeros(x.shape, dtype=x.dtype, device=x.device)        # (zeros_like keeps a permuted x's order)
+        out.view(-1, self.width)[s.index] = y
+        return out
+
+
+class MultiViewAttention(_SlicedAttention):
+    """softmax(q k) v of each asset's foreground tokens, with per-head RMS
+    norms of queries and keys and rotary positions, between a fused input
+    projection and an output projection.  The forward pass only: a call that
+    torch would record for a gradient is refused.  One layer may be called
+    under several streams and from several threads at the same time."""
+
+    def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int,
+                 dtype: torch.dtype = torch.bfloat16, sections: Optional[Sequence[int]] = None, base: float = 10000.0,
+                 generator: Optional[torch.Generator] = None):
+        """pos: device float32 [B, N, H, W, 3] position maps (NaN: background).
+        sections: columns of the rotation for the view, row and column axes
+        (default: the whole head, a quarter of it for the view).  The weights
+        are drawn from the generator; load others into w_qkv [width, (heads +
+        2 kv_heads) dim], w_out [heads dim, width], q_gain and k_gain [dim]."""
+        super().__init__(pos, width, heads, kv_heads, dim, dtype, sections, base)
+        rand = lambda *shape: torch.randn(shape, generator=generator, device=pos.device)
+        self.w_qkv = (rand(width, (heads + 2 * kv_heads) * dim) / math.sqrt(width)).to(dtype)
+        self.w_out = (rand(heads * dim, width) / math.sqrt(heads * dim)).to(dtype)
+
+    def __call__(self, x: torch.Tensor, views: Sequence[int]) -> torch.Tensor:
+        """x [B, len(views), H, W, width] of the layer's type -> the layer's
+        output on foreground tokens, zeros on the background."""
+        s, tokens = self._tokens(x, views, (self.w_qkv, self.w_out, self.q_gain, self.k_gain))
+        out = self._attend(tokens @ self.w_qkv, s)
+        return self._spread(out.view(-1, self.heads * self.dim) @ self.w_out, x, s)
+
+
+class MultiViewBlock(_SlicedAttention):
+    """A whole block on each asset's foreground tokens x:
+
+      h = x + attention(norm(x)),  y = h + down(act(in(norm(h))))
+
+    with RMS norms, the attention of MultiViewAttention and a feed-forward
+    part, gated (act(gate) * value) or not.  With lay_out_in_8_bits() the
+    products' operands are 8-bit rows with a scale each.  The forward pass only: a call that
+    torch would record for a gradient is refused.  One block may be called under several streams and from several
+    threads at the same time."""
+
+    def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int, hidden: int,
+                 act: int = GC_ACT_SILU, gated: bool = True, dtype: torch.dtype = torch.bfloat16,
+                 sections: Optional[Sequence[int]] = None, base: float = 10000.0, eps: float = 1e-6,
+                 generator: Optional[torch.Generator] = None):
+        """pos, sections, base: as MultiViewAttention's.  The weights, rows of
+        outputs, are drawn from the generator; load others into w_qkv [(heads +
+        2 kv_heads) dim, width], w_out [width, heads dim], w_in [hidden, or 2
+        hidden: gates and values, width], w_down [width, hidden], the biases
+        b_qkv, b_out, b_in, b_down (float32, None: none) and the gains
+        attention_gain, feed_gain [width], q_gain, k_gain [dim] (float32)."""
+        super().__init__(pos, width, heads, kv_heads, dim, dtype, sections, base)
+        self.hidden, self.act, self.gated, self.eps = hidden, act, gated, eps
+        dev = pos.device
+        rand = lambda n, m: (torch.randn((n, m), generator=generator, device=dev) / math.sqrt(m)).to(dtype)
+        self.w_qkv = rand((heads + 2 * kv_heads) * dim, width)
+        self.w_out = rand(width, heads * dim)
+        self.w_in = rand(2 * hidden if gated else hidden, width)
+        self.w_down = rand(width, hidden)
+        self.b_qkv = self.b_out = self.b_in = self.b_down = None
+        self.attention_gain = torch.ones(width, dtype=torch.float32, device=dev)
+        self.feed_gain = torch.ones(width, dtype=torch.float32, device=dev)
+        self.eight_bits: Optional[Dict[str, Tuple[torch.Tensor, torch.Tensor]]] = None
+
+    def lay_out_in_8_bits(self) -> None:
+        """The products' weights as they are now in 8 bits with a scale a row:
+        calls from here on use those, whatever is loaded into w_... later
+        (call again after that).  width, heads * dim and hidden are multiples of 16."""
+        for n in (self.width, self.heads * self.dim, self.hidden):
+            if n % 16:
+                raise ValueError(f"8-bit products need a width, heads * dim and hidden of whole 16 (got {n})")
+        self.eight_bits = {name: gc_quantize_rows(getattr(self, name)) for name in ("w_qkv", "w_out", "w_in", "w_down")}
+        torch.cuda.current_stream(self.foreground.device).synchronize()   # any stream may read them from here on
+
+    def _product(self, name: str, x: torch.Tensor, scale: Optional[torch.Tensor] = None, **more) -> torch.Tensor:
+        """x (of the layer's type, or 8-bit rows with their scales) times a weight."""
+        bias = getattr(self, "b" + name[1:])
+        if self.eight_bits is None:
+            return gc_linear(x, getattr(self, name), bias, out_dtype=self.dtype, **more)
+        if scale is None:
+            x, scale = gc_quantize_rows(x)
+        w, w_scale = self.eight_bits[name]
+        return gc_linear(x, w, bias, x_scale=scale, w_scale=w_scale, out_dtype=self.dtype, **more)
+
+    def __call__(self, x: torch.Tensor, views: Sequence[int]) -> torch.Tensor:
+        """x [B, len(views), H, W, width] of the layer's type -> the block's
+        output on foreground tokens, zeros on the background."""
+        s, tokens = self._tokens(x, views, (self.w_qkv, self.w_out, self.w_in, self.w_down, self.b_qkv, self.b_out, self.b_in,
+                                            self.b_down, self.q_gain, self.k_gain, self.attention_gain, self.feed_gain))
+        normed = torch.float8_e4m3fn if self.eight_bits is not None else self.dtype
+        n, scale, _ = gc_add_rms_norm(tokens, gain=self.attention_gain, eps=self.eps, out_dtype=normed)
+        out = self._attend(self._product("w_qkv", n, scale), s)
+        out = self._product("w_out", out.view(-1, self.heads * self.dim))
+        n, scale, h = gc_add_rms_norm(out, residual=tokens, gain=self.feed_gain, eps=self.eps, out_dtype=normed, total=out)
+        m = self._product("w_in", n, scale, act=self.act, gated=self.gated)
+        return self._spread(self._product("w_down", m, residual=h, out=h), x, s)
