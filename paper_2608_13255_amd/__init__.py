@@ -210,6 +210,7 @@ def _current_raw_stream() -> int:
 
 # what torch's own generated code calls for the same purpose
 _RAW_STREAM = getattr(torch._C, "_cuda_getCurrentRawStream", None) if hasattr(torch._C, "_cuda_getDevice") else None
+_GET_DEVICE = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _stream(stream) -> Optional[int]:
@@ -1280,13 +1281,19 @@ def _rows(t: torch.Tensor, name: str) -> _Rows:
     return _Rows(t.data_ptr(), strides[0] if n > 1 else c)
 
 
-def _device_of(x: torch.Tensor, stream) -> int:
-    """The device of a call's tensors, which must be the stream's."""
+def _device_of(x: torch.Tensor, stream) -> Tuple[int, int]:
+    """(device of a call's tensors, handle of its stream), which must be on
+    that device."""
     device = x.get_device()
-    at = stream.device_index if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_device()
+    if stream is None and _RAW_STREAM is not None:
+        at = _GET_DEVICE()
+        handle = _RAW_STREAM(at)
+    else:
+        at = stream.device_index if isinstance(stream, torch.cuda.Stream) else torch.cuda.current_device()
+        handle = _stream(stream)
     if device != at:
         raise ValueError(f"tensors are on cuda:{device}, the stream is on cuda:{at}")
-    return device
+    return device, handle
 
 
 def _like_rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: int) -> _Rows:
@@ -1318,32 +1325,38 @@ def gc_add_rms_norm(x: torch.Tensor, residual: torch.Tensor = None, gain: torch.
     if code is None:
         raise ValueError(f"rows must be float32 or bfloat16 (got {x.dtype})")
     n, width = shape = x.shape
-    device = _device_of(x, stream)
+    device, handle = _device_of(x, stream)
     if out_dtype is None:
         out_dtype = x.dtype if out is None else out.dtype
     out_code = _ROW_CODES.get(out_dtype)
     if out_code is None:
         raise ValueError(f"out_dtype must be {x.dtype} or {torch.float8_e4m3fn} (got {out_dtype})")
-    gain_at = _floats(gain, "gain", width, device)
     fresh = []
     hr = ht = None
     if residual is not None:
         hr = _like_rows(residual, "residual", shape, x.dtype, device)
         if total is None:
             total = torch.empty_like(x, memory_format=_CONTIGUOUS)
+            ht = _Rows(total.data_ptr(), width)
             fresh.append(total)
-    if total is not None:
+    if total is not None and ht is None:
         ht = _like_rows(total, "total", shape, x.dtype, device)
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype, device=x.device)
+        out = torch.empty_like(x, dtype=out_dtype, memory_format=_CONTIGUOUS)
+        ho = _Rows(out.data_ptr(), width)
         fresh.append(out)
-    ho = _like_rows(out, "out", shape, out_dtype, device)
+    else:
+        ho = _like_rows(out, "out", shape, out_dtype, device)
     if out_code == GC_E4M3 and out_scale is None:
         out_scale = torch.empty((n,), dtype=torch.float32, device=x.device)
+        scale_at = out_scale.data_ptr()
         fresh.append(out_scale)
-    _check(lib().gc_add_rms_norm(hx, hr, n, width, code, gain_at, eps, ht, ho, out_code,
-                                 _floats(out_scale, "out_scale", n, device), _stream(stream)), "gc_add_rms_norm")
-    _keep(stream, fresh)
+    else:
+        scale_at = _floats(out_scale, "out_scale", n, device)
+    _check(lib().gc_add_rms_norm(hx, hr, n, width, code, None if gain is None else _floats(gain, "gain", width, device), eps, ht, ho, out_code,
+                                 scale_at, handle), "gc_add_rms_norm")
+    if stream is not None:
+        _keep(stream, fresh)
     return out, out_scale, x if total is None else total
 
 
@@ -1356,17 +1369,23 @@ def gc_quantize_rows(x: torch.Tensor, out: torch.Tensor = None, out_scale: torch
     if code is None:
         raise ValueError(f"rows must be float32 or bfloat16 (got {x.dtype})")
     n, width = shape = x.shape
-    device = _device_of(x, stream)
+    device, handle = _device_of(x, stream)
     fresh = []
     if out is None:
-        out = torch.empty(shape, dtype=torch.float8_e4m3fn, device=x.device)
+        out = torch.empty_like(x, dtype=torch.float8_e4m3fn, memory_format=_CONTIGUOUS)
+        ho = _Rows(out.data_ptr(), width)
         fresh.append(out)
+    else:
+        ho = _like_rows(out, "out", shape, torch.float8_e4m3fn, device)
     if out_scale is None:
         out_scale = torch.empty((n,), dtype=torch.float32, device=x.device)
+        scale_at = out_scale.data_ptr()
         fresh.append(out_scale)
-    _check(lib().gc_quantize_rows(hx, n, width, code, _like_rows(out, "out", shape, torch.float8_e4m3fn, device),
-                                  _floats(out_scale, "out_scale", n, device), _stream(stream)), "gc_quantize_rows")
-    _keep(stream, fresh)
+    else:
+        scale_at = _floats(out_scale, "out_scale", n, device)
+    _check(lib().gc_quantize_rows(hx, n, width, code, ho, scale_at, handle), "gc_quantize_rows")
+    if stream is not None:
+        _keep(stream, fresh)
     return out, out_scale
 
 
@@ -1395,10 +1414,10 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
         raise ValueError(f"x must be float32, bfloat16 or {torch.float8_e4m3fn} (got {x.dtype})")
     n, n_in = x.shape
     w_rows = w.shape[0]
-    device = _device_of(x, stream)
+    device, handle = _device_of(x, stream)
     if w.dtype != x.dtype or w.shape[1] != n_in or w.get_device() != device:
         raise ValueError(f"w must be {x.dtype} [n_out, {n_in}] on {x.device} (got {w.dtype} {list(w.shape)} on {w.device})")
-    n_out = w_rows
+    n_out, gated = w_rows, int(bool(gated))
     if gated:
         if w_rows % 2:
             raise ValueError(f"gated products need an even number of rows of w (got {w_rows})")
@@ -1411,12 +1430,14 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
         raise ValueError(f"out_dtype must be float32 or bfloat16 (got {out_dtype})")
     fresh = []
     if out is None:
-        out = torch.empty((n, n_out), dtype=out_dtype, device=x.device)
+        out = x.new_empty((n, n_out), dtype=out_dtype)
+        ho = _Rows(out.data_ptr(), n_out)
         fresh.append(out)
-    ho = _like_rows(out, "out", (n, n_out), out_dtype, device)
+    else:
+        ho = _like_rows(out, "out", (n, n_out), out_dtype, device)
     hr = None if residual is None else _like_rows(residual, "residual", (n, n_out), out_dtype, device)
     at, size = None, 0
-    need = lib().gc_linear_workspace_bytes(n, n_out, n_in, code, int(bool(gated)))
+    need = lib().gc_linear_workspace_bytes(n, n_out, n_in, code, gated)
     if need > 0:
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
@@ -1424,10 +1445,12 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
         elif workspace.get_device() != device:
             raise ValueError(f"workspace must be on {x.device} (got {workspace.device})")
         at, size = _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
-    _check(lib().gc_linear(hx, _floats(x_scale, "x_scale", n, device), hw, _floats(w_scale, "w_scale", w_rows, device),
-                           n, n_out, n_in, code, _floats(bias, "bias", w_rows, device), act, int(bool(gated)), hr, ho,
-                           out_code, at, size, _stream(stream)), "gc_linear")
-    _keep(stream, fresh)
+    _check(lib().gc_linear(hx, None if x_scale is None else _floats(x_scale, "x_scale", n, device), hw,
+                           None if w_scale is None else _floats(w_scale, "w_scale", w_rows, device), n, n_out, n_in, code,
+                           None if bias is None else _floats(bias, "bias", w_rows, device), act, gated, hr, ho, out_code,
+                           at, size, handle), "gc_linear")
+    if stream is not None:
+        _keep(stream, fresh)
     return out
 
 

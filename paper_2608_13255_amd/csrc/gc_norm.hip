@@ -46,34 +46,63 @@ __device__ __forceinline__ uint32_t max_wave(uint32_t x) {
   return x;
 }
 
-// Groups of V values that one access reads.
-template <class T, int V>
-__device__ __forceinline__ void load_group(const T* p, float (&x)[V]) {
-  if constexpr (V == 1) x[0] = load_one(p);
-  else load_heads<V>(p, x);
-}
-template <class T, int V>
-__device__ __forceinline__ void store_group(T* p, const float (&x)[V]) {
-  if constexpr (V == 1) store_one(p, x[0]);
-  else store_heads<V>(p, x);
-}
-template <int V>
-__device__ __forceinline__ void store_eight(uint8_t* p, const float (&x)[V]) {
-  if constexpr (V == 1) {
-    *p = (uint8_t)pack_e4m3(x[0], 0.f, 0.f, 0.f);
-  } else {
-    typedef uint32_t uv __attribute__((ext_vector_type(V / 4)));
-    uv v;
+// Groups of V values, 16 bytes in memory.  Where kWhole is not set they may begin anywhere and the last one may lie
+// partly past the row's end (`have` values are in it): the hardware takes 16 bytes at any address.
+template <class T, int V, bool kWhole, bool kOnce>
+__device__ __forceinline__ void load_group(const T* p, int have, float (&x)[V]) {
+  using Vec = typename HeadVec<T, V>::type;
+  if (kWhole) {
+    const Vec v = load_vec<kOnce, Vec>(p);
 #pragma unroll
-    for (int i = 0; i < V; i += 4) v[i / 4] = pack_e4m3(x[i], x[i + 1], x[i + 2], x[i + 3]);
-    *reinterpret_cast<uv*>(p) = v;
+    for (int i = 0; i < V; ++i) x[i] = HeadVec<T, V>::at(v, i);
+  } else if (have >= V) {
+    Vec v;
+    __builtin_memcpy(&v, p, sizeof(v));
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = HeadVec<T, V>::at(v, i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = load_one(p + (i < have ? i : 0));
+#pragma unroll
+    for (int i = 1; i < V; ++i) x[i] = i < have ? x[i] : 0.f;
+  }
+}
+template <class T, int V, bool kWhole, bool kOnce>
+__device__ __forceinline__ void store_group(T* p, int have, const float (&x)[V]) {
+  if (kWhole) {
+    store_heads<V, kOnce>(p, x);
+  } else if (have >= V) {
+    T v[V];
+    store_heads<V>(v, x);
+    __builtin_memcpy(p, v, sizeof(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < have) store_one(p + i, x[i]);
+  }
+}
+template <int V, bool kWhole, bool kOnce>
+__device__ __forceinline__ void store_eight(uint8_t* p, int have, const float (&x)[V]) {
+  typedef uint32_t uv __attribute__((ext_vector_type(V / 4)));
+  uv v;
+#pragma unroll
+  for (int i = 0; i < V; i += 4) v[i / 4] = pack_e4m3(x[i], x[i + 1], x[i + 2], x[i + 3]);
+  if (kWhole) {
+    store_vec<kOnce, uv>(p, v);
+  } else if (have >= V) {
+    __builtin_memcpy(p, &v, sizeof(v));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < have) p[i] = (uint8_t)(v[i / 4] >> (8 * (i % 4)));
   }
 }
 
 // kLanes threads a row, kGroups groups of V values a thread.  A block is 256
-// threads (four rows of a wave each, or one), or 1024.
-template <class T, int V, int kGroups, int kLanes>
+// threads (four rows of a wave each, or one), or a row's 512 or 1024.
+template <class T, int kGroups, int kLanes, bool kWhole, bool kOnce>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const NormArgs p) {
+  constexpr int V = 16 / sizeof(T);
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
   constexpr int kWaves = kLanes / 64;
   __shared__ uint32_t shared[2 * kWaves];
@@ -87,7 +116,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
     const int at = (u * kLanes + i) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j) h[u][j] = 0.f;
-    if (at < p.width) load_group<T, V>(x + at, h[u]);
+    if (at < p.width) load_group<T, V, kWhole, kOnce>(x + at, p.width - at, h[u]);
   }
   if (p.residual) {
     const T* r = (const T*)p.residual + row * p.residual_row;
@@ -96,7 +125,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
       const int at = (u * kLanes + i) * V;
       if (at < p.width) {
         float a[V];
-        load_group<T, V>(r + at, a);
+        load_group<T, V, kWhole, kOnce>(r + at, p.width - at, a);
 #pragma unroll
         for (int j = 0; j < V; ++j) h[u][j] += a[j];
       }
@@ -107,7 +136,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
       const int at = (u * kLanes + i) * V;
-      if (at < p.width) store_group<T, V>(t + at, h[u]);
+      if (at < p.width) store_group<T, V, kWhole, kOnce>(t + at, p.width - at, h[u]);
     }
   }
   if (p.norm) {
@@ -134,7 +163,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
         for (int j = 0; j < V; ++j) g[j] = 1.f;
         if (p.gain) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) g[j] = p.gain[at + j];
+          for (int j = 0; j < V; ++j) g[j] = kWhole || at + j < p.width ? p.gain[at + j] : 0.f;
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) h[u][j] = h[u][j] * r * g[j];
@@ -146,7 +175,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
       const int at = (u * kLanes + i) * V;
-      if (at < p.width) store_group<T, V>(o + at, h[u]);
+      if (at < p.width) store_group<T, V, kWhole, kOnce>(o + at, p.width - at, h[u]);
     }
     return;
   }
@@ -176,14 +205,14 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
         const float q = h[u][j] * inv;
         h[u][j] = __builtin_fmaf(__builtin_fmaf(-q, scale, h[u][j]), inv, q);
       }
-      store_eight<V>(o + at, h[u]);
+      store_eight<V, kWhole, kOnce>(o + at, p.width - at, h[u]);
     }
   }
 }
 
 constexpr int64_t kMostBlocks = 1 << 22;
 
-template <class T, int V, int kGroups, int kLanes>
+template <class T, int kGroups, int kLanes, bool kWhole, bool kOnce>
 void launch(NormArgs p, hipStream_t stream) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
   constexpr int64_t kRowsMost = kMostBlocks * kRows;
@@ -191,7 +220,7 @@ void launch(NormArgs p, hipStream_t stream) {
   const int64_t es = sizeof(T);
   for (int64_t r = 0; r < n; r += kRowsMost) {
     p.n_rows = n - r < kRowsMost ? n - r : kRowsMost;
-    k_norm<T, V, kGroups, kLanes><<<(unsigned)((p.n_rows + kRows - 1) / kRows), kLanes < 256 ? 256 : kLanes, 0, stream>>>(p);
+    k_norm<T, kGroups, kLanes, kWhole, kOnce><<<(unsigned)((p.n_rows + kRows - 1) / kRows), kLanes < 256 ? 256 : kLanes, 0, stream>>>(p);
     p.x = (const char*)p.x + kRowsMost * p.x_row * es;
     if (p.residual) p.residual = (const char*)p.residual + kRowsMost * p.residual_row * es;
     if (p.total) p.total = (char*)p.total + kRowsMost * p.total_row * es;
@@ -200,24 +229,38 @@ void launch(NormArgs p, hipStream_t stream) {
   }
 }
 
-// A row in one wave up to 16 values a lane, then in a block of 256, then of 1024.
-template <class T, int V>
-void launch_v(const NormArgs& p, hipStream_t stream) {
+// Bytes read and written from which they go past the caches (a copy of them does not stay there anyway): 16384 x 4096 float32
+// to 8 bits, 336 MB, 56 us against 60; 10403 x 4096 bfloat16, 128 MB, 23 against 22.
+constexpr int64_t kOnceBytes = 192 << 20;
+
+// A row in one wave up to two groups a lane, rows that are not of whole groups up to eight (5741 x 1283 float32 24 us, 27 in
+// blocks); else in a block (196608 x 2048 bfloat16 with its sum 468 us, 497 in waves; 16384 x 4096
+// float32 to 8 bits 53 us in blocks of 512, 56 of 256 and 66 of 1024).
+template <class T, bool kWhole, bool kOnce>
+void launch_groups(const NormArgs& p, hipStream_t stream) {
+  constexpr int V = 16 / sizeof(T);
   const int groups = (p.width + V - 1) / V;
-  if (groups <= 64) launch<T, V, 1, 64>(p, stream);
-  else if (groups <= 128) launch<T, V, 2, 64>(p, stream);
-  else if (groups <= 256) launch<T, V, 1, 256>(p, stream);
-  else if (groups <= 512) launch<T, V, 2, 256>(p, stream);
-  else if (groups <= 1024) launch<T, V, 4, 256>(p, stream);
-  else if (groups <= 2048) launch<T, V, 8, 256>(p, stream);
-  else if (groups <= 4096) launch<T, V, 4, 1024>(p, stream);
-  else launch<T, V, (V == 1 ? 32 : 32768 / V / 1024), 1024>(p, stream);
+  if (groups <= 64) return launch<T, 1, 64, kWhole, kOnce>(p, stream);
+  if (groups <= 128) return launch<T, 2, 64, kWhole, kOnce>(p, stream);
+  if constexpr (!kWhole) {
+    if (groups <= 256) return launch<T, 4, 64, kWhole, kOnce>(p, stream);
+    if (groups <= 512) return launch<T, 8, 64, kWhole, kOnce>(p, stream);
+  } else {
+    if (groups <= 256) return launch<T, 1, 256, kWhole, kOnce>(p, stream);
+    if (groups <= 512) return launch<T, 2, 256, kWhole, kOnce>(p, stream);
+  }
+  if (groups <= 1024) return launch<T, 2, 512, kWhole, kOnce>(p, stream);
+  if (groups <= 2048) return launch<T, 4, 512, kWhole, kOnce>(p, stream);
+  if (groups <= 4096) return launch<T, 4, 1024, kWhole, kOnce>(p, stream);
+  launch<T, 8, 1024, kWhole, kOnce>(p, stream);
 }
 
 template <class T>
-void launch_norm(const NormArgs& p, bool wide, hipStream_t stream) {
-  if (wide) launch_v<T, 16 / sizeof(T)>(p, stream);
-  else launch_v<T, 1>(p, stream);
+void launch_norm(const NormArgs& p, bool whole, hipStream_t stream) {
+  const int64_t bytes = (int64_t)sizeof(T) * (1 + (p.residual != nullptr) + (p.total != nullptr)) + (p.eight ? 1 : sizeof(T));
+  if (whole && p.n_rows * p.width >= kOnceBytes / bytes) launch_groups<T, true, true>(p, stream);
+  else if (whole) launch_groups<T, true, false>(p, stream);
+  else launch_groups<T, false, false>(p, stream);
 }
 
 int check_width(int64_t n_rows, int width, int dtype, const char* who) {
@@ -241,10 +284,10 @@ int check_eight(const gc_rows* out, const float* out_scale, int64_t n_rows, int 
 void run_norm(const NormArgs& p, int dtype, hipStream_t stream) {
   const int es = dtype_bytes(dtype), V = 16 / es;
   const auto fits = [&](const void* data, int64_t stride, int bytes, int e) { return !data || rows_aligned({(void*)data, stride}, p.n_rows, bytes, e); };
-  const bool wide = p.width % V == 0 && fits(p.x, p.x_row, 16, es) && fits(p.residual, p.residual_row, 16, es) &&
+  const bool whole = p.width % V == 0 && fits(p.x, p.x_row, 16, es) && fits(p.residual, p.residual_row, 16, es) &&
                     fits(p.total, p.total_row, 16, es) && fits(p.out, p.out_row, p.eight ? V : 16, p.eight ? 1 : es);
-  if (dtype == GC_F32) launch_norm<float>(p, wide, stream);
-  else launch_norm<uint16_t>(p, wide, stream);
+  if (dtype == GC_F32) launch_norm<float>(p, whole, stream);
+  else launch_norm<uint16_t>(p, whole, stream);
 }
 
 }  // namespace
