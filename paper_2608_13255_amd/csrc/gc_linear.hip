@@ -3,7 +3,6 @@
 //   p = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,  out = act(p) (* p of the value rows) + residual
 #include <algorithm>
 #include <cmath>
-#include <iterator>
 
 #include "gc_linear_plan.h"
 
@@ -17,22 +16,29 @@ struct TileCost {
   double one, two, rest;     // two = 0: a unit holds one
 };
 constexpr TileCost kCosts[] = {
-    {kLinearTiles64, 64, 128, 0.42, 0.75, 1.5}, {kLinearTiles128, 128, 128, 0.45, 1.06, 2.5}, {kLinearTiles256, 256, 256, 1.35, 0, 8}};
+    {kLinearTiles64, 64, 128, 0.42, 0.75, 1.5}, {kLinearTiles128, 128, 128, 0.45, 1.15, 2.5},
+    {kLinearTiles192, 192, 256, 1.25, 0, 9},    {kLinearTiles256, 256, 256, 1.6, 0, 10}};
+// (8 bits: the epilogue's registers of two tiles of 128 on a unit do not all fit)
+constexpr TileCost kCostsE4M3[] = {
+    {kLinearTiles64, 64, 128, 0.42, 0.8, 1.5}, {kLinearTiles128, 128, 128, 0.45, 2.0, 2.5},
+    {kLinearTiles192, 192, 256, 1.35, 0, 9},   {kLinearTiles256, 256, 256, 1.7, 0, 10}};
 constexpr TileCost kCostsF32[] = {
     {kLinearTiles64x64, 64, 64, 0.7, 1.1, 1.5},
     {kLinearTiles64, 64, 128, 1.2, 2.05, 1.5}, {kLinearTiles128, 128, 128, 2.05, 4.0, 2.5}, {kLinearTiles256, 128, 256, 3.75, 0, 4}};
 
 struct CostList {
   const TileCost *first, *last;
-  explicit CostList(int dtype) : first(dtype == GC_F32 ? std::begin(kCostsF32) : std::begin(kCosts)), last(dtype == GC_F32 ? std::end(kCostsF32) : std::end(kCosts)) {}
+  template <int kCount>
+  explicit CostList(const TileCost (&c)[kCount]) : first(c), last(c + kCount) {}
   const TileCost* begin() const { return first; }
   const TileCost* end() const { return last; }
 };
+CostList costs_of(int dtype) { return dtype == GC_F32 ? CostList(kCostsF32) : dtype == GC_BF16 ? CostList(kCosts) : CostList(kCostsE4M3); }
 
-// Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 14 us; in tiles with
+// Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 13 us; in tiles with
 // parts 16); a wave's share of a row where there are few weight rows is cut by more waves, then by parts (16 x 1024 gated x
 // 2736 13 us whole, 9 in four).  Else the tiles, and the parts of the inner dimension, that take least: 4096^3 bfloat16 183, 137 and
-// 104 us with tiles of 64, 128 and 256, 1024^3 10.6, 11.3 and 26, 128 x 1024 x 4096 28, 29 and 74 whole, 12.6 with 64 in eight parts.
+// 104 us with tiles of 64, 128 and 256, 10403 x 1024 x 2736 81 with 256 and 69 with 192, 1024^3 10.6, 11.3 and 26, 128 x 1024 x 4096 28, 29 and 74 whole, 12.6 with 64 in eight parts.
 LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated) {
   const int steps = (row_bytes + kStepBytes - 1) / kStepBytes;
   const auto in_parts = [&](int kind, int parts, int waves) {
@@ -43,11 +49,11 @@ LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated
   if (n_rows <= kLinearFewRows) {
     const int blocks = (n_out + 15) / 16;
     const int parts = std::min({8, kCus / blocks, row_bytes / 1280});
-    return in_parts(kLinearFew, std::max(1, parts), blocks < 2 * kCus ? 16 : 4);
+    return in_parts(kLinearFew, std::max(1, parts), blocks < 5 * kCus / 4 ? 16 : 4);
   }
   LinearPlan best = {};
   double least = 0;
-  for (const TileCost& c : CostList(dtype)) {
+  for (const TileCost& c : costs_of(dtype)) {
     if (gated && c.kind == kLinearTiles64x64) continue;
     const double tiles = std::ceil((double)n_rows / c.x) * std::ceil(w_rows / c.w);
     for (const int parts : {1, 2, 3, 4, 6, 8, 12, 16}) {

@@ -1,15 +1,18 @@
 // Matrix products of few rows: every weight is read once, from memory to registers.
 //
-// A wave takes 16 weight rows (the first operand) 64 bytes of each at a time,
-// and the waves of a block the same rows' other bytes by turns; their sums
+// A wave takes 16 weight rows (the first operand) 128 bytes of each at a time,
+// 32 a lane in two loads, so that the first brings whole lines and the second finds them; eight loads are on their way
+// before any is used.  The waves of a block take the same rows' other bytes by turns; their sums
 // meet in LDS.  x, read as often as there are blocks, comes from the caches.
+// 1 x 6144 x 4096 bfloat16: 12.9 us (3.9 TB/s), 13.8 with 64 bytes of each row a load and past the caches.
+//
 #pragma once
 
 #include "gc_linear.h"
 
 namespace gc {
 
-// Operands of 16 rows: a 16-byte chunk a lane, row lane % 16, chunk lane / 16 of four.
+// Operands of 16 rows: a 16-byte chunk a lane, row lane % 16.
 struct FewF32 {
   __device__ __forceinline__ static f32x4 mma(const u32x4& w, const u32x4& x, f32x4 c) {
 #pragma unroll
@@ -31,10 +34,10 @@ struct FewE4M3 {   // as bfloat16, which holds them exactly: there is time for i
   }
 };
 
-constexpr int kFewStep = 64;     // bytes of a row that a wave takes at a time
+constexpr int kFewStep = 128;    // bytes of a row that a wave takes at a time
 constexpr uint32_t kFewNowhere = 0x7ffffff0u;   // past any range
 
-constexpr int kFewUnroll = 8;    // steps that are read before they are used
+constexpr int kFewUnroll = 4;    // steps that are read before they are used
 
 // 16 rows of x, 16 weight rows (gated: gates and as many values) and kWaves waves a block.
 template <class Op, int kWaves, bool kGated>
@@ -47,8 +50,8 @@ __global__ __launch_bounds__(kWaves * 64) void k_linear_few(const LinearArgs p) 
   const int k_begin = blockIdx.y * p.part_bytes;
   const int k_end = p.row_bytes - k_begin < p.part_bytes ? p.row_bytes : k_begin + p.part_bytes;
   const int rows_x = (int)p.n_rows, rows_w = p.n_out - n0 < 16 ? p.n_out - n0 : 16;
-  const int chunk16 = lane / 16 * 16;
-  const uint32_t x_at = (uint32_t)(lane % 16) * (uint32_t)p.x_row + chunk16, w_at = (uint32_t)(lane % 16) * (uint32_t)p.w_row + chunk16;
+  const int first = lane / 16 * 32;     // byte of the lane's first chunk of a step
+  const uint32_t x_at = (uint32_t)(lane % 16) * (uint32_t)p.x_row + first, w_at = (uint32_t)(lane % 16) * (uint32_t)p.w_row + first;
   const char* wb = p.w + (int64_t)n0 * p.w_row;
   const char* vb = wb + (int64_t)p.n_out * p.w_row;
   const int range_x = (int)((rows_x - 1) * p.x_row), range_w = (int)((rows_w - 1) * p.w_row);
@@ -57,23 +60,23 @@ __global__ __launch_bounds__(kWaves * 64) void k_linear_few(const LinearArgs p) 
 #pragma unroll
   for (int j = 0; j < kBlocks; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int k = k_begin + wave * kFewStep * kFewUnroll; k < k_end; k += kWaves * kFewStep * kFewUnroll) {
-    u32x4 w[kFewUnroll][kBlocks], x[kFewUnroll];
+    u32x4 w[2 * kFewUnroll][kBlocks], x[2 * kFewUnroll];
 #pragma unroll
-    for (int u = 0; u < kFewUnroll; ++u) {
-      const int at = k + u * kFewStep, left = k_end - at;
+    for (int u = 0; u < 2 * kFewUnroll; ++u) {
+      const int at = k + u / 2 * kFewStep, left = k_end - at;
       // past the end of a row, and past the last row, zeros arrive
-      const bool past = chunk16 >= left;
-      const uint32_t from_w = past ? kFewNowhere : w_at, from_x = past ? kFewNowhere : x_at;
+      const bool past = first + u % 2 * 16 >= left;
+      const uint32_t from_w = past ? kFewNowhere : w_at + u % 2 * 16, from_x = past ? kFewNowhere : x_at + u % 2 * 16;
       const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)(wb + at), 0, left > 0 ? range_w + left : 0, 0x00027000);
       const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(vb + at), 0, left > 0 ? range_w + left : 0, 0x00027000);
       const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(p.x + at), 0, left > 0 ? range_x + left : 0, 0x00027000);
-      w[u][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, from_w, 0, 2));
-      if (kGated) w[u][kBlocks - 1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, from_w, 0, 2));
+      w[u][0] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, from_w, 0, 0));
+      if (kGated) w[u][kBlocks - 1] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rv, from_w, 0, 0));
       x[u] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, from_x, 0, 0));
     }
     __builtin_amdgcn_sched_barrier(0);   // all reads before any use
 #pragma unroll
-    for (int u = 0; u < kFewUnroll; ++u)
+    for (int u = 0; u < 2 * kFewUnroll; ++u)
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j) acc[j] = Op::mma(w[u][j], x[u], acc[j]);
   }

@@ -48,6 +48,9 @@ void launch_kind(const LinearArgs& p, const LinearPlan& plan, hipStream_t stream
     case kLinearTiles64: launch_tiles<Tiles<Op, 2, 2, 32, 64, 3, kGated>>(p, stream); break;
     case kLinearTiles128: launch_tiles<Tiles<Op, 4, 2, 32, 64, 2, kGated>>(p, stream); break;
     case kLinearTiles128Deep: launch_tiles<Tiles<Op, 4, 2, 32, 64, 4, kGated>>(p, stream); break;
+    case kLinearTiles192:
+      if constexpr (!Op::kTotals) launch_tiles<Tiles<Op, 2, 4, 96, 64, 2, kGated>>(p, stream);
+      break;
     default: launch_tiles<Tiles<Op, 2, 4, kLargeX, 64, 2, kGated>>(p, stream); break;
   }
 }

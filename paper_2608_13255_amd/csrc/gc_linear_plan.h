@@ -11,6 +11,7 @@ enum LinearKind : int {
   kLinearTiles64,   // 64 rows x 128 weight rows a block
   kLinearTiles128,  // 128 x 128, two of them on a compute unit
   kLinearTiles128Deep,  // one, with more steps on their way
+  kLinearTiles192,  // 192 x 256 (bfloat16 and 8 bits)
   kLinearTiles256,  // 256 x 256 (float32: 128 x 256)
   kLinearKinds
 };
