@@ -106,8 +106,8 @@ struct RowAhead {
   }
 };
 
-// The sums a (and b of the value rows) of eight columns of row m to the output, 16 bytes at a time.
-template <bool kGated>
+// The sums a (and b of the value rows) of eight columns of row m to the output, 16 bytes at a time.  kOnce: past the caches.
+template <bool kGated, bool kOnce = false>
 __device__ __forceinline__ void finish(const LinearArgs& p, const Columns& c, int64_t m, const RowAhead& row, float (&a)[8], float (&b)[8]) {
   if (p.x_scale || p.w_scale) {
     const float xs = p.x_scale ? row.scale : 1.f;
@@ -131,13 +131,13 @@ __device__ __forceinline__ void finish(const LinearArgs& p, const Columns& c, in
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] += __uint_as_float(row.add[i / 4][i % 4]);
     }
-    store_heads<8>((float*)o, a);
+    store_heads<8, kOnce>((float*)o, a);
   } else {
     if (p.residual) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) a[i] += HeadVec<uint16_t, 8>::at(row.add[0], i);
     }
-    store_heads<8>((uint16_t*)o, a);
+    store_heads<8, kOnce>((uint16_t*)o, a);
   }
 }
 

@@ -33,8 +33,8 @@ __device__ __forceinline__ void block_barrier() {
 
 constexpr int kTotalSteps = 16;
 constexpr uint32_t kNowhere = 0x7ffffff0u;   // past any range
-// Blocks that share rows of x, or of the weights, and the steps between asking for a line and its load.
-constexpr int kAheadW = 4, kAheadX = 8, kAheadSteps = 2;
+// Blocks that share rows of x, or of the weights, and the steps between a line asked for and the one to be loaded next.
+constexpr int kAheadW = 4, kAheadX = 8, kAheadSteps = 0;
 
 template <class Op_, int kWavesX_, int kWavesW_, int kRowsX, int kRowsW, int kBuffers_, bool kGated_>
 struct Tiles {
@@ -52,11 +52,17 @@ struct Tiles {
   static constexpr int kGroups = 64 / Op::kBlock;            // of lanes
   static constexpr int kParts = 8 / kGroups / Op::kChunks;   // of a step: fragments that products take
   static constexpr int kFrags = kBlocksX + kBlocksW;
-  // the epilogue's place of a wave: 16 rows of its columns, where the steps lay
-  static constexpr int kWaveFloats = 16 * kRowsW;
   static constexpr int kLds = kBuffers * kStage + kWaves * 256;
+  // the epilogue's place of a wave, where the steps lay: its sums, or a half or third of their rows
+  static constexpr int kPlace = kBuffers * kStage / kWaves;
+  static constexpr bool fits(int passes) { return kRowsX % (32 * passes) == 0 && kRowsX / passes * kRowsW * 4 <= kPlace; }
+  static constexpr int kPasses = fits(1) ? 1 : fits(2) ? 2 : 3, kPassRows = kRowsX / kPasses;
+  static constexpr int kWaveFloats = kPassRows * kRowsW;
+  // A round of large tiles writes what all L2s hold, at once: past the caches (24576 x 16384 x 1024 bfloat16 763 us, 817 through
+  // them).
+  static constexpr bool kOnce = kX * kW >= 192 * 256;
   static constexpr int kAtOnce = 163840 / kLds > 2 ? 2 : 163840 / kLds;   // blocks on a compute unit
-  static_assert(kBuffers * kStage >= kWaves * kWaveFloats * 4, "room for the epilogue");
+  static_assert(fits(kPasses), "room for the epilogue");
   static_assert(kLds <= 163840 && (kRowsW == 64 || kRowsW == 32), "LDS of a compute unit, and what the epilogue's permutation covers");
   static_assert((kX + kW) / 8 % kWaves == 0 && kX / 8 % kWaves == 0 && kWaves % 4 == 0, "whole loads");
   static_assert(!kGated || kRowsW % 64 == 0, "gate and value in one wave");
@@ -169,11 +175,12 @@ struct StageLoader {
     }
     xb += kStepBytes, wb += kStepBytes, left -= kStepBytes;
   }
-  // Asks for the lines of the step kAheadSteps after the one to be loaded next, so that they are in the L2 by then.  Blocks that run at the same time on
-  // an XCD share rows: each asks for its part of them.  What arrives (4 bytes a line) is of no use.
+  // Asks for the lines of the step kAheadSteps after the one to be loaded next, so that they are in the L2 by then (`left` is that
+  // one's).  Blocks that run at the same time on an XCD share rows: each asks for its part of them.  What arrives (4 bytes a
+  // line) is of no use.
   __device__ __forceinline__ void ask(char* junk) {
     const int far = left - kAheadSteps * kStepBytes;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(ab + kAheadSteps * kStepBytes), 0, far > 0 ? range_a + far : 0, 0x00027000);
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)(ab + (C::kBuffers + kAheadSteps) * kStepBytes), 0, far > 0 ? range_a + far : 0, 0x00027000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LdsVoid*)junk, 4, ahead, 0, 0, 0);
     ab += kStepBytes;
   }
@@ -198,9 +205,11 @@ struct Fragments {
   }
 };
 
-// The order of a part's instructions: a read of LDS or a load from memory between any two products.
+// The order of a part's instructions: a read of LDS or a load from memory between any two products.  (8-bit products run
+// four times as long as one is issued, and the compiler's own order is 2 % better.)
 template <class C, int kDma>
 __device__ __forceinline__ void beside_products() {
+  if (C::Op::kChunks == 2) return;
   constexpr int kProducts = C::kBlocksX * C::kBlocksW * C::Op::kProducts;
   constexpr int kEach = kProducts / (2 * (C::kFrags + kDma)) > 1 ? kProducts / (2 * (C::kFrags + kDma)) : 1;
 #pragma unroll
@@ -312,91 +321,85 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce * C::kWaves / 4) void k_lin
   block_barrier();
 
   float* mine = reinterpret_cast<float*>(lds) + wave * C::kWaveFloats;
-  // Through LDS, 16 rows of the wave at a time: eight consecutive columns a lane.  16-byte chunk c of row r lies at place
-  // c ^ r (c ^ r / 2 of rows of 8 chunks).
+  // Through LDS, so that few lanes hold whole lines of the output: eight consecutive columns a lane.  16-byte chunk c of row
+  // r lies at place c ^ r % 16 (c ^ r / 2 % 8 of rows of 8 chunks).
   const LinearArgs p = args_anew();
   const int64_t m0 = (int64_t)tile.x * C::kX + wx * C::kWaveX;
-  constexpr int kCols = C::kOut / C::kWavesW, kLanes = kCols / 8, kRowsOnce = 64 / kLanes;
-  static_assert(64 % kLanes == 0, "whole rows");
+  constexpr int kCols = C::kOut / C::kWavesW, kLanes = kCols / 8, kRowsOnce = 64 / kLanes, kTimes = 2;
+  constexpr int kOneRows = 64 / kCols, kOneTimes = 4;
+  static_assert(64 % kLanes == 0 && kCols <= 64 && C::kPassRows % (kTimes * kRowsOnce) == 0 && C::kPassRows % (kOneTimes * kOneRows) == 0, "whole rows");
   const int n0 = tile.w * C::kOut + ww * kCols;
-  const auto place = [](int r, int c) { return r * C::kWaveW + (C::kWaveW == 64 ? c ^ r : c ^ (r >> 1)) * 4; };
-  const int el = lane_anew(), col = el % kLanes * 8, row = el / kLanes;
+  const auto place = [](int r, int c) { return r * C::kWaveW + (C::kWaveW == 64 ? c ^ (r & 15) : c ^ ((r >> 1) & 7)) * 4; };
+  const int el = lane_anew(), col = el % kLanes * 8, row = el / kLanes, one = el % kCols;
   const bool whole = p.parts > 1 || (p.whole && n0 + kCols <= p.n_out);
-  constexpr int kHalves = kBlock / 16;                              // a block's rows 16 at a time
-  constexpr int kTimes = kRowsOnce < 16 ? 16 / kRowsOnce : 1;       // eight columns a lane
-  constexpr int kOneCol = kCols < 64 ? kCols : 64, kOneRows = 64 / kOneCol, kOneTimes = 4;   // one column a lane
-  static_assert(kCols <= 64, "a lane's column");
-  const auto row_at = [&](int i, int r) {
-    const int64_t m = m0 + i * 16 + r;
-    return m < p.n_rows ? m : p.n_rows - 1;
-  };
+  const auto row_in = [&](int64_t m) { return m < p.n_rows ? m : p.n_rows - 1; };
   Columns c;
-  RowAhead ahead[kTimes];
-  if (whole && p.parts == 1) {
-    c.init<C::kGated>(p, n0 + col);
-#pragma unroll
-    for (int r = 0; r < kTimes; ++r) ahead[r].load(p, row_at(0, r * kRowsOnce + row), c.n);
-  }
-  const int one = el % kOneCol;
   Column c1;
+  if (whole && p.parts == 1) c.init<C::kGated>(p, n0 + col);
   if (!whole) c1.init<C::kGated>(p, n0 + one < p.n_out ? n0 + one : p.n_out - 1);
 #pragma unroll
-  for (int i = 0; i < C::kBlocksX * kHalves; ++i) {
-    if (kHalves == 1 || el % kBlock / 16 == i % kHalves) {
+  for (int pass = 0; pass < C::kPasses; ++pass) {
+    constexpr int kPassBlocks = C::kBlocksX / C::kPasses;
+#pragma unroll
+    for (int i = 0; i < kPassBlocks; ++i)
 #pragma unroll
       for (int j = 0; j < C::kBlocksW; ++j)
 #pragma unroll
         for (int q = 0; q < C::Op::kQuads; ++q) {
-          const Acc& c4 = acc[i / kHalves][j];
+          const Acc& c4 = acc[pass * kPassBlocks + i][j];
           const f32x4 v = {c4[4 * q], c4[4 * q + 1], c4[4 * q + 2], c4[4 * q + 3]};
-          *reinterpret_cast<f32x4*>(mine + place(el % 16, (j * kBlock + q * C::Op::kStride) / 4 + el / kBlock)) = v;
+          *reinterpret_cast<f32x4*>(mine + place(i * kBlock + el % kBlock, (j * kBlock + q * C::Op::kStride) / 4 + el / kBlock)) = v;
         }
-    }
     __builtin_amdgcn_wave_barrier();   // (a wave's own LDS accesses are in order)
+    const int64_t m1 = m0 + pass * C::kPassRows;
     if (whole) {
-      RowAhead now_row[kTimes];
+      RowAhead ahead[kTimes];
 #pragma unroll
-      for (int r = 0; r < kTimes; ++r) {
-        now_row[r] = ahead[r];
-        if (p.parts == 1 && i + 1 < C::kBlocksX * kHalves) ahead[r].load(p, row_at(i + 1, r * kRowsOnce + row), c.n);
-      }
+      for (int t = 0; t < kTimes; ++t)
+        if (p.parts == 1) ahead[t].load(p, row_in(m1 + t * kRowsOnce + row), c.n);
+#pragma unroll 1
+      for (int r = row; r < C::kPassRows; r += kTimes * kRowsOnce) {
+        RowAhead now_row[kTimes];
 #pragma unroll
-      for (int r = 0; r < kTimes; ++r) {
-        const int at = r * kRowsOnce + row;
-        if (kRowsOnce > 16 && at >= 16) continue;
-        const int64_t m = m0 + i * 16 + at;
-        const int from = C::kGated ? col / 32 * 64 + col % 32 : col;
-        float a[8], b[8];
-        load_heads<4>(mine + place(at, from / 4), reinterpret_cast<float(&)[4]>(a[0]));
-        load_heads<4>(mine + place(at, from / 4 + 1), reinterpret_cast<float(&)[4]>(a[4]));
-        if (C::kGated) {
-          load_heads<4>(mine + place(at, from / 4 + 8), reinterpret_cast<float(&)[4]>(b[0]));
-          load_heads<4>(mine + place(at, from / 4 + 9), reinterpret_cast<float(&)[4]>(b[4]));
+        for (int t = 0; t < kTimes; ++t) {
+          now_row[t] = ahead[t];
+          if (p.parts == 1) ahead[t].load(p, row_in(m1 + r + (kTimes + t) * kRowsOnce), c.n);   // (past the last one: not used)
         }
-        if (m >= p.n_rows) continue;
-        if (p.parts > 1) {
-          if (n0 + col < p.partial_cols) {
-            float* o = p.partial + tile.part * p.partial_part + m * p.partial_cols * (C::kGated ? 2 : 1) + n0 + col;
-            store_heads<8>(o, a);
-            if (C::kGated) store_heads<8>(o + p.partial_cols, b);
+#pragma unroll
+        for (int t = 0; t < kTimes; ++t) {
+          const int at = r + t * kRowsOnce, from = C::kGated ? col / 32 * 64 + col % 32 : col;
+          const int64_t m = m1 + at;
+          float a[8], b[8];
+          load_heads<4>(mine + place(at, from / 4), reinterpret_cast<float(&)[4]>(a[0]));
+          load_heads<4>(mine + place(at, from / 4 + 1), reinterpret_cast<float(&)[4]>(a[4]));
+          if (C::kGated) {
+            load_heads<4>(mine + place(at, from / 4 + 8), reinterpret_cast<float(&)[4]>(b[0]));
+            load_heads<4>(mine + place(at, from / 4 + 9), reinterpret_cast<float(&)[4]>(b[4]));
           }
-        } else {
-          finish<C::kGated>(p, c, m, now_row[r], a, b);
+          if (m >= p.n_rows) continue;
+          if (p.parts > 1) {
+            if (n0 + col < p.partial_cols) {
+              float* o = p.partial + tile.part * p.partial_part + m * p.partial_cols * (C::kGated ? 2 : 1) + n0 + col;
+              store_heads<8>(o, a);
+              if (C::kGated) store_heads<8>(o + p.partial_cols, b);
+            }
+          } else {
+            finish<C::kGated, C::kOnce>(p, c, m, now_row[t], a, b);
+          }
         }
       }
     } else {
       const int from = C::kGated ? one / 32 * 64 + one % 32 : one;
 #pragma unroll 1
-      for (int r0 = el / kOneCol; r0 < 16; r0 += kOneRows * kOneTimes) {
+      for (int r0 = el / kCols; r0 < C::kPassRows; r0 += kOneRows * kOneTimes) {
         OneAhead some[kOneTimes];
 #pragma unroll
-        for (int u = 0; u < kOneTimes; ++u) some[u].load(p, row_at(i, r0 + u * kOneRows), c1.n);
+        for (int u = 0; u < kOneTimes; ++u) some[u].load(p, row_in(m1 + r0 + u * kOneRows), c1.n);
 #pragma unroll
         for (int u = 0; u < kOneTimes; ++u) {
           const int r = r0 + u * kOneRows;
-          const int64_t m = m0 + i * 16 + r;
           const float a = mine[place(r, from / 4) + from % 4], b = C::kGated ? mine[place(r, from / 4 + 8) + from % 4] : 0.f;
-          if (m < p.n_rows && n0 + one < p.n_out) finish_one<C::kGated>(p, c1, m, some[u], a, b);
+          if (m1 + r < p.n_rows && n0 + one < p.n_out) finish_one<C::kGated>(p, c1, m1 + r, some[u], a, b);
         }
       }
     }
