@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
   }
 }
 
-constexpr int64_t kMostBlocks = 1 << 22;
+constexpr int64_t kMostBlocks = 1 << 21;   // (of 1024 threads: below 2^32 in all)
 
 template <class T, int kGroups, int kLanes, bool kWhole, bool kOnce>
 void launch(NormArgs p, hipStream_t stream) {

@@ -119,10 +119,12 @@ def test_epilogues(gc, kind, out, M, N, K, act, gated, bias, residual):
     run(gc, kind, out, M, N, K, act, gated, bias, residual)
 
 
-# every variant, by what the rule on sizes takes there: one and two tiles of 128 on a compute unit, 256, 64, 64 x 64; parts
+# every variant, by what the rule on sizes takes there: tiles of 64 (and 64 x 64) and 128, one and two on a compute unit, 192, 256;
+# one part, a few and sixteen
 @pytest.mark.parametrize("kind,out", PAIRS)
-@pytest.mark.parametrize("M,N,K", [(300, 520, 96), (1000, 1040, 128), (1100, 4100, 112), (2300, 1030, 400),
-                                   (4100, 4090, 272), (130, 136, 6000 // 16 * 16), (20, 24, 16384), (70, 2000, 4096)])
+@pytest.mark.parametrize("M,N,K", [(300, 520, 96), (513, 1000, 1040), (1030, 2050, 304), (1100, 4100, 112), (2300, 1030, 400),
+                                   (2900, 4000, 2048), (4000, 4090, 1024), (130, 136, 6000 // 16 * 16), (20, 24, 16384),
+                                   (70, 2000, 4096)])
 @pytest.mark.parametrize("gated", [False, True])
 def test_variants(gc, kind, out, M, N, K, gated):
     g = torch.Generator(device=DEV)

@@ -192,7 +192,7 @@ def test_offsets_past_32_bits(gc):
 
 def test_more_rows_than_a_launch_has(gc):
     """Rows past one launch's blocks go out in the next one."""
-    n = (1 << 24) + 5
+    n = (1 << 23) + 5
     x = torch.randint(-3, 4, (n, 1), device=DEV, dtype=torch.int8).to(torch.bfloat16)
     q, scale = gc.gc_quantize_rows(x)
     some = x.float() != 0
