@@ -835,6 +835,8 @@ int gc_quantize_rows(const gc_rows* x, int64_t n_rows, int width, int dtype, con
  *             consequence.  Calls in flight at the same time need workspaces of their own.  May be NULL where that is 0.
  * out and workspace may otherwise share no byte with an input or each other (columns of one buffer are apart).
  * The result does not depend on the order in which blocks run, but which products are added first depends on the sizes.
+ * The sum is multiplied by x_scale first.  With GC_E4M3 operands and a GC_BF16 result the sum over more than 16 rows' products is that of
+ * the 8-bit matrix units, which is off by about 2^-16 of itself (a GC_F32 result's is float32's).
  * gc_linear_workspace_bytes: -1 for sizes that gc_linear refuses.
  */
 int64_t gc_linear_workspace_bytes(int64_t n_rows, int n_out, int n_in, int dtype, int gated);

@@ -1,6 +1,17 @@
 // Matrix products with what follows them.
 //
 //   p = x_scale_i w_scale_j sum_k x_ik w_jk + bias_j,  out = act(p) (* p of the value rows) + residual
+//
+// A call cannot do without 2 n_rows n_in operations a weight row, and reading x and w and writing out once: few rows are bound by
+// the weights' bytes, everything else by the matrix units.  Measured, us, with the time of the bound at a large
+// product's 1570 (bfloat16), 2720 (8 bits) and 153 TFLOP/s (float32), or a large read's 7.0 TB/s:
+//   1 x 6144 x 4096 bfloat16                                  11.9   7.2
+//   16 x 8192 x 4096 in 8 bits                                11.0   4.8
+//   1024 x 1283 x 1024 float32, bias, GELU, residual          44.5  17.6
+//   10403 x 2736 gated x 1024 bfloat16                         132    74
+//   10403 x 1024 x 2736 bfloat16, bias, residual                68    37
+//   24576 x 16384 x 4096 bfloat16, bias, GELU                 2490  2101
+//   24576 x 8192 gated x 4096 in 8 bits                       1345  1213
 #include <algorithm>
 #include <cmath>
 
@@ -73,7 +84,8 @@ LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated
   return best;
 }
 
-// Sums of the parts, and the epilogue: eight columns a thread.
+// Sums of the parts in their order, and the epilogue: eight columns a thread.  Memory-bound, and small beside what cutting a
+// long inner dimension saves (128 x 1024 x 4096 bfloat16 12.6 us in eight parts, 28 whole).
 template <bool kGated>
 __global__ __launch_bounds__(256) void k_linear_join(const LinearArgs p, int64_t groups) {
   const int row_groups = p.partial_cols / 8;

@@ -9,6 +9,15 @@
 // The weights are the first operand, so an accumulator's lane holds one row of
 // x and groups of four consecutive weight rows.  Gated products take 32 gate and 32 value rows by
 // turns, so that a wave holds both.
+//
+// What bounds it: power and the steps' arrival.  8192^3 bfloat16: 759 us (1450 TFLOP/s), matrix units busy 75 % of the time at
+// 1.78 GHz; without the loads of the steps 671, without the epilogue 719.  The library takes 673.  What counted there:
+//   products of 16 x 16 instead of 32 x 32 (791 and 845), with less power; eight waves (828 with four of 128 x 128)
+//   a step's loads all at once after the barrier that frees their place (789 spread over the step)
+//   lines asked for half a step before their loads, by one of the blocks that share them (852 without)
+//   128 bytes of a row a load: with 64 bytes and four steps on their way the L2 gets twice the requests (866)
+// Blocks that stay and take tiles by turns were slower (24576 x 16384 x 4096 2590, 2497): all units then
+// write at the same time, and wait for it.
 #pragma once
 
 #include "gc_linear.h"
@@ -58,8 +67,8 @@ struct Tiles {
   static constexpr bool fits(int passes) { return kRowsX % (32 * passes) == 0 && kRowsX / passes * kRowsW * 4 <= kPlace; }
   static constexpr int kPasses = fits(1) ? 1 : fits(2) ? 2 : 3, kPassRows = kRowsX / kPasses;
   static constexpr int kWaveFloats = kPassRows * kRowsW;
-  // A round of large tiles writes what all L2s hold, at once: past the caches (24576 x 16384 x 1024 bfloat16 763 us, 817 through
-  // them).
+  // A round of large tiles writes what all L2s hold, at once: past the caches (24576 x 16384 x 1024 bfloat16 763 us, 817
+  // through them).
   static constexpr bool kOnce = kX * kW >= 192 * 256;
   static constexpr int kAtOnce = 163840 / kLds > 2 ? 2 : 163840 / kLds;   // blocks on a compute unit
   static_assert(fits(kPasses), "room for the epilogue");

@@ -5,7 +5,13 @@
 //
 // Each value is read once and written once (twice with the sum), for about
 // 6 operations: memory-bound.  A row lies in the registers of one wave or one
-// block, so neither the mean nor the largest magnitude reads it again.
+// block, so neither the mean nor the largest magnitude reads it again.  Measured, us, with
+// the time of the bytes at a large copy's 6.5 TB/s:
+//   196608 x 2048 bfloat16 with its sum, to 8 bits     470  434
+//   16384 x 4096 float32 to 8 bits                      53   52
+//   10403 x 4096 bfloat16 to 8 bits                     22   20
+//   5741 x 1283 float32 with its sum                    24   18   (rows that begin anywhere)
+//   1 x 4096 bfloat16                                  2.7        (a call from Python 8.1)
 #include <cmath>
 
 #include "gc_rows.h"
