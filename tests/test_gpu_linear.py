@@ -367,3 +367,70 @@ def test_refusals_on_the_device(gc):
         gc.gc_linear(x, w, act=9)
     with pytest.raises(gc.GeoCacheError, match="overlaps x"):
         gc.gc_linear(x, w, out=x[:, :6])
+
+
+@pytest.mark.parametrize("M", [7, 150])
+def test_x_and_output_in_one_buffer(gc, M):
+    """The output beside x in the rows of one buffer."""
+    K, N = 192, 72
+    g = torch.Generator(device=DEV)
+    g.manual_seed(13)
+    x, w, _, _, x64, w64 = operands("bf16", M, N, K, g)
+    buffer = torch.zeros((M, K + N), dtype=torch.bfloat16, device=DEV)
+    buffer[:, :K] = x
+    gc.gc_linear(buffer[:, :K], w, out=buffer[:, K:])
+    check(buffer[:, K:], *expected(x64, w64, None, "none", False, None, False))
+    assert torch.equal(buffer[:, :K], x)
+    with pytest.raises(gc.GeoCacheError, match="overlaps x"):
+        gc.gc_linear(buffer[:, :K], w, out=buffer[:, K - 8:-8])
+
+
+@pytest.mark.parametrize("kind,out", PAIRS)
+@pytest.mark.parametrize("M", [3, 90, 600])
+def test_weight_rows_that_repeat(gc, kind, out, M):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(14)
+    x, w, xs, ws, x64, w64 = operands(kind, M, 1, 272, g)
+    got = gc.gc_linear(x, w.expand(150, -1), x_scale=xs, w_scale=None if ws is None else ws.expand(150).contiguous(),
+                       out_dtype=TYPES[out])
+    check(got, *expected(x64, w64.expand(150, -1), None, "none", False, None, kind == "e4m3" and out == "bf16"))
+    assert bool((got == got[:, :1]).all())
+
+
+@pytest.mark.parametrize("kind,M", [("bf16", 3), ("bf16", 40), ("f32", 2), ("f32", 40), ("e4m3", 20)])
+def test_the_longest_rows(gc, kind, M):
+    K, N, out = 1 << 20, 20, "f32"
+    g = torch.Generator(device=DEV)
+    g.manual_seed(15)
+    x, w, xs, ws, x64, w64 = operands(kind, M, N, K, g)
+    got = gc.gc_linear(x, w, x_scale=xs, w_scale=ws, out_dtype=TYPES[out])
+    want = x64 @ w64.t()
+    # (K u S would say nothing here: the products' signs are random, and the error is within 64 sqrt(K) u of their root)
+    root = (x64.square() @ w64.square().t()).sqrt()
+    assert float(((got.double() - want).abs() / root).max()) < 64 * math.sqrt(K) * U
+
+
+def test_the_widest_output(gc):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(16)
+    for M in (2, 33):
+        x, w, _, _, x64, w64 = operands("bf16", M, 300001, 16, g)
+        got = gc.gc_linear(x, w, act=1)
+        check(got, *expected(x64, w64, None, "silu", False, None, False))
+
+
+def test_more_rows_than_a_launch_has_tiles(gc):
+    """Rows past one launch's tiles go out in the next one."""
+    M, N, K = (1 << 26) + 100003, 8, 4
+    x = torch.randint(-4, 5, (M, K), device=DEV, dtype=torch.int8).float()
+    w = torch.randint(-4, 5, (N, K), device=DEV, dtype=torch.int8).float()
+    r = torch.randint(-4, 5, (M, 1), device=DEV, dtype=torch.int8).float().expand(-1, N).contiguous()
+    got = gc.gc_linear(x, w, residual=r, out=r)
+    first = r is got
+    for i in (0, (1 << 26) - 70, M - 1000):
+        n = min(1000, M - i)
+        part = got[i:i + n] - x[i:i + n] @ w.t()
+        assert bool((part == part[:, :1]).all()) and bool((part.abs() <= 4).all())   # whole numbers: exact
+    assert first
+    del x, r, got
+    torch.cuda.empty_cache()

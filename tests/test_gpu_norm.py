@@ -105,7 +105,7 @@ def test_no_rows(gc):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("width,pad", [(64, 16), (100, 7), (2048, 32), (1283, 2)])
+@pytest.mark.parametrize("width,pad", [(64, 16), (100, 7), (2048, 32), (1283, 2), (4000, 3), (9001, 5), (20000, 6), (32768, 2)])
 def test_strides(gc, dtype, width, pad):
     """Columns of wider buffers, aligned and not; what lies around the outputs stays."""
     x, r = rows(50, width, dtype, 6, pad), rows(50, width, dtype, 7, pad)
