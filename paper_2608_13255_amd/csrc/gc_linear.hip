@@ -48,7 +48,7 @@ CostList costs_of(int dtype) { return dtype == GC_F32 ? CostList(kCostsF32) : dt
 
 // Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 13 us; in tiles with
 // parts 16); a wave's share of a row where there are few weight rows is cut by more waves, then by parts (16 x 1024 gated x
-// 2736 13 us whole, 9 in four).  Else the tiles, and the parts of the inner dimension, that take least: 4096^3 bfloat16 183, 137 and
+// 2736 13 us whole, 9 in four; 1 x 16384 x 4096 in 8 bits 13.1, 14.3 and 16.6 with 8, 4 and 16 waves a block).  Else the tiles, and the parts of the inner dimension, that take least: 4096^3 bfloat16 183, 137 and
 // 104 us with tiles of 64, 128 and 256, 10403 x 1024 x 2736 81 with 256 and 69 with 192, 1024^3 10.6, 11.3 and 26, 128 x 1024 x 4096 28, 29 and 74 whole, 12.6 with 64 in eight parts.
 LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated) {
   const int steps = (row_bytes + kStepBytes - 1) / kStepBytes;
@@ -60,7 +60,7 @@ LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated
   if (n_rows <= kLinearFewRows) {
     const int blocks = (n_out + 15) / 16;
     const int parts = std::min({8, kCus / blocks, row_bytes / 1280});
-    return in_parts(kLinearFew, std::max(1, parts), blocks < 5 * kCus / 4 ? 16 : 4);
+    return in_parts(kLinearFew, std::max(1, parts), blocks <= kCus ? 16 : 8);
   }
   LinearPlan best = {};
   double least = 0;

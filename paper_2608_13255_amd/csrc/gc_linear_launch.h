@@ -31,7 +31,7 @@ void launch_tiles(LinearArgs p, hipStream_t stream) {
 template <class Few, bool kGated>
 void launch_few(const LinearArgs& p, const LinearPlan& plan, hipStream_t stream) {
   const dim3 grid((unsigned)((p.n_out + 15) / 16), (unsigned)p.parts);
-  if (plan.waves == 4) k_linear_few<Few, 4, kGated><<<grid, 256, 0, stream>>>(p);
+  if (plan.waves == 8) k_linear_few<Few, 8, kGated><<<grid, 512, 0, stream>>>(p);
   else k_linear_few<Few, 16, kGated><<<grid, 1024, 0, stream>>>(p);
 }
 
