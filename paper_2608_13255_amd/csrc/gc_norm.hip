@@ -41,14 +41,17 @@ __device__ __forceinline__ float reciprocal_root_of(float m) {
   return 1.f / __builtin_sqrtf(m);
 }
 
-__device__ __forceinline__ float sum_wave(float x) {
+// The sum, and the largest, over the lanes of a row (of a wave, if it has more), in every one of them.
+template <int kLanes>
+__device__ __forceinline__ float sum_lanes(float x) {
 #pragma unroll
-  for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i);
+  for (int i = 1; i < (kLanes < 64 ? kLanes : 64); i *= 2) x += __shfl_xor(x, i);
   return x;
 }
-__device__ __forceinline__ uint32_t max_wave(uint32_t x) {
+template <int kLanes>
+__device__ __forceinline__ uint32_t max_lanes(uint32_t x) {
 #pragma unroll
-  for (int i = 1; i < 64; i *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, i));
+  for (int i = 1; i < (kLanes < 64 ? kLanes : 64); i *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, i));
   return x;
 }
 
@@ -105,12 +108,12 @@ __device__ __forceinline__ void store_eight(uint8_t* p, int have, const float (&
 }
 
 // kLanes threads a row, kGroups groups of V values a thread.  A block is 256
-// threads (four rows of a wave each, or one), or a row's 512 or 1024.
+// threads (a row, or several in a wave or part of one each), or a row's 512 or 1024.
 template <class T, int kGroups, int kLanes, bool kWhole, bool kOnce>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const NormArgs p) {
   constexpr int V = 16 / sizeof(T);
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
-  constexpr int kWaves = kLanes / 64;
+  constexpr int kWaves = kLanes < 64 ? 1 : kLanes / 64;
   __shared__ uint32_t shared[2 * kWaves];
   const int i = threadIdx.x % kLanes, wave = i / 64;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
     for (int u = 0; u < kGroups; ++u)
 #pragma unroll
       for (int j = 0; j < V; ++j) q = __builtin_fmaf(h[u][j], h[u][j], q);
-    q = sum_wave(q);
+    q = sum_lanes<kLanes>(q);
     if constexpr (kWaves > 1) {
       if (i % 64 == 0) shared[wave] = __float_as_uint(q);
       __syncthreads();
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
   for (int u = 0; u < kGroups; ++u)
 #pragma unroll
     for (int j = 0; j < V; ++j) top = max(top, __float_as_uint(h[u][j]) & 0x7fffffffu);
-  top = max_wave(top);
+  top = max_lanes<kLanes>(top);
   if constexpr (kWaves > 1) {
     if (i % 64 == 0) shared[kWaves + wave] = top;
     __syncthreads();
@@ -239,13 +242,17 @@ void launch(NormArgs p, hipStream_t stream) {
 // to 8 bits, 336 MB, 56 us against 60; 10403 x 4096 bfloat16, 128 MB, 23 against 22.
 constexpr int64_t kOnceBytes = 192 << 20;
 
-// A row in one wave up to two groups a lane, rows that are not of whole groups up to eight (5741 x 1283 float32 24 us, 27 in
-// blocks); else in a block (196608 x 2048 bfloat16 with its sum 468 us, 497 in waves; 16384 x 4096
+// Narrow rows in parts of a wave (70920 x 16 bfloat16 9 us, 18 in waves), a
+// row in one wave up to two groups a lane, rows that are not of whole groups
+// up to eight (5741 x 1283 float32 24 us, 27 in blocks); else in a block
+// (196608 x 2048 bfloat16 with its sum 468 us, 497 in waves; 16384 x 4096
 // float32 to 8 bits 53 us in blocks of 512, 56 of 256 and 66 of 1024).
 template <class T, bool kWhole, bool kOnce>
 void launch_groups(const NormArgs& p, hipStream_t stream) {
   constexpr int V = 16 / sizeof(T);
   const int groups = (p.width + V - 1) / V;
+  if (groups <= 8) return launch<T, 1, 8, kWhole, kOnce>(p, stream);
+  if (groups <= 32) return launch<T, 1, 32, kWhole, kOnce>(p, stream);
   if (groups <= 64) return launch<T, 1, 64, kWhole, kOnce>(p, stream);
   if (groups <= 128) return launch<T, 2, 64, kWhole, kOnce>(p, stream);
   if constexpr (!kWhole) {
