@@ -195,12 +195,12 @@ struct Blocks16 {
   static constexpr int kBlock = 16, kQuads = 1, kStride = 16;
   typedef f32x4 Acc;
 };
-struct F32 : Blocks32 {
+struct F32 : Blocks16 {
   static constexpr int kChunks = 1, kProducts = 4;   // products of a pair of fragments
   static constexpr bool kTotals = true;
   typedef f32x4 Frag;
   __device__ __forceinline__ static Acc mma(const Frag& w, const Frag& x, Acc c, int i) {
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(w[i], x[i], c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(w[i], x[i], c, 0, 0, 0);
   }
 };
 struct BF16 : Blocks16 {

@@ -42,8 +42,8 @@ template <class Few, class Op, int kLargeX, bool kGated>
 void launch_kind(const LinearArgs& p, const LinearPlan& plan, hipStream_t stream) {
   switch (plan.kind) {
     case kLinearFew: launch_few<Few, kGated>(p, plan, stream); break;
-    case kLinearTiles64x64:
-      if constexpr (Op::kTotals && !kGated) launch_tiles<Tiles<Op, 2, 2, 32, 32, 3, false>>(p, stream);
+    case kLinearTiles32x64:
+      if constexpr (Op::kTotals && !kGated) launch_tiles<Tiles<Op, 2, 2, 16, 32, 3, false>>(p, stream);
       break;
     case kLinearTiles64: launch_tiles<Tiles<Op, 2, 2, 32, 64, 3, kGated>>(p, stream); break;
     case kLinearTiles128: launch_tiles<Tiles<Op, 4, 2, 32, 64, 2, kGated>>(p, stream); break;

@@ -7,7 +7,7 @@ namespace gc {
 
 enum LinearKind : int {
   kLinearFew,       // at most 16 rows: each weight to the registers of one wave
-  kLinearTiles64x64,  // 64 rows x 64 weight rows a block (float32, not gated)
+  kLinearTiles32x64,  // 32 rows x 64 weight rows a block (float32, not gated)
   kLinearTiles64,   // 64 rows x 128 weight rows a block
   kLinearTiles128,  // 128 x 128, two of them on a compute unit
   kLinearTiles128Deep,  // one, with more steps on their way

@@ -12,7 +12,7 @@
 //
 // What bounds it: power and the steps' arrival.  8192^3 bfloat16: 759 us (1450 TFLOP/s), matrix units busy 75 % of the time at
 // 1.78 GHz; without the loads of the steps 671, without the epilogue 719.  The library takes 673.  What counted there:
-//   products of 16 x 16 instead of 32 x 32 (791 and 845), with less power; eight waves (828 with four of 128 x 128)
+//   products of 16 x 16 instead of 32 x 32 (791 and 845; float32, 2048^3: 128 and 135), with less power; eight waves (828 with four of 128 x 128)
 //   a step's loads all at once after the barrier that frees their place (789 spread over the step)
 //   lines asked for half a step before their loads, by one of the blocks that share them (852 without)
 //   128 bytes of a row a load: with 64 bytes and four steps on their way the L2 gets twice the requests (866)
@@ -64,13 +64,13 @@ struct Tiles {
   static constexpr int kLds = kBuffers * kStage + kWaves * 256;
   // the epilogue's place of a wave, where the steps lay: its sums, or a half or third of their rows
   static constexpr int kPlace = kBuffers * kStage / kWaves;
-  static constexpr bool fits(int passes) { return kRowsX % (32 * passes) == 0 && kRowsX / passes * kRowsW * 4 <= kPlace; }
+  static constexpr bool fits(int passes) { return kRowsX % ((kRowsX < 32 ? 16 : 32) * passes) == 0 && kRowsX / passes * kRowsW * 4 <= kPlace; }
   static constexpr int kPasses = fits(1) ? 1 : fits(2) ? 2 : 3, kPassRows = kRowsX / kPasses;
   static constexpr int kWaveFloats = kPassRows * kRowsW;
   // A round of large tiles writes what all L2s hold, at once: past the caches (24576 x 16384 x 1024 bfloat16 763 us, 817
   // through them).
   static constexpr bool kOnce = kX * kW >= 192 * 256;
-  static constexpr int kAtOnce = 163840 / kLds > 2 ? 2 : 163840 / kLds;   // blocks on a compute unit
+  static constexpr int kAtOnce = 163840 / kLds;   // blocks on a compute unit
   static_assert(fits(kPasses), "room for the epilogue");
   static_assert(kLds <= 163840 && (kRowsW == 64 || kRowsW == 32), "LDS of a compute unit, and what the epilogue's permutation covers");
   static_assert((kX + kW) / 8 % kWaves == 0 && kX / 8 % kWaves == 0 && kWaves % 4 == 0, "whole loads");
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce * C::kWaves / 4) void k_lin
   // r lies at place c ^ r % 16 (c ^ r / 2 % 8 of rows of 8 chunks).
   const LinearArgs p = args_anew();
   const int64_t m0 = (int64_t)tile.x * C::kX + wx * C::kWaveX;
-  constexpr int kCols = C::kOut / C::kWavesW, kLanes = kCols / 8, kRowsOnce = 64 / kLanes, kTimes = 2;
+  constexpr int kCols = C::kOut / C::kWavesW, kLanes = kCols / 8, kRowsOnce = 64 / kLanes, kTimes = C::kPassRows < 2 * kRowsOnce ? 1 : 2;
   constexpr int kOneRows = 64 / kCols, kOneTimes = 4;
   static_assert(64 % kLanes == 0 && kCols <= 64 && C::kPassRows % (kTimes * kRowsOnce) == 0 && C::kPassRows % (kOneTimes * kOneRows) == 0, "whole rows");
   const int n0 = tile.w * C::kOut + ww * kCols;

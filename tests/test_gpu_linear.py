@@ -119,7 +119,7 @@ def test_epilogues(gc, kind, out, M, N, K, act, gated, bias, residual):
     run(gc, kind, out, M, N, K, act, gated, bias, residual)
 
 
-# every variant, by what the rule on sizes takes there: tiles of 64 (and 64 x 64) and 128, one and two on a compute unit, 192, 256;
+# every variant, by what the rule on sizes takes there: tiles of 64 (and 32 x 64) and 128, one and two on a compute unit, 192, 256;
 # one part, a few and sixteen
 @pytest.mark.parametrize("kind,out", PAIRS)
 @pytest.mark.parametrize("M,N,K", [(300, 520, 96), (513, 1000, 1040), (1030, 2050, 304), (1100, 4100, 112), (2300, 1030, 400),
