@@ -1263,6 +1263,7 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
 
 # codes by torch type
 _ROW_CODES = {torch.float32: GC_F32, torch.bfloat16: GC_BF16, torch.float8_e4m3fn: GC_E4M3}
+_INT_MAX = 2 ** 31 - 1
 
 
 def _rows(t: torch.Tensor, name: str) -> _Rows:
@@ -1278,6 +1279,8 @@ def _rows(t: torch.Tensor, name: str) -> _Rows:
     n, c = t.shape
     if strides[1] != 1 and c > 1:
         raise ValueError(f"{name} must have contiguous columns")
+    if n > _INT_MAX or c > _INT_MAX:      # (ctypes would pass what is left of them in 32 bits)
+        raise ValueError(f"{name} has a size above 2^31 - 1 (got {tuple(t.shape)})")
     return _Rows(t.data_ptr(), strides[0] if n > 1 else c)
 
 
@@ -1391,6 +1394,8 @@ def gc_quantize_rows(x: torch.Tensor, out: torch.Tensor = None, out_scale: torch
 
 def gc_linear_workspace_bytes(n_rows: int, n_out: int, n_in: int, dtype: torch.dtype, gated: bool = False) -> int:
     """Bytes of device memory that gc_linear needs beside its arguments."""
+    if max(n_rows, n_out, n_in) > _INT_MAX or min(n_rows, n_out, n_in) < 0:
+        raise ValueError(f"sizes must be in [0, 2^31 - 1] (got {n_rows}, {n_out}, {n_in})")
     need = lib().gc_linear_workspace_bytes(n_rows, n_out, n_in, _ROW_CODES.get(dtype, -1), int(bool(gated)))
     if need < 0:
         _check(-2, "gc_linear_workspace_bytes")

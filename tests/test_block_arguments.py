@@ -182,3 +182,6 @@ def test_binding_refusals(gc):
         gc.gc_linear_workspace_bytes(4, 6, 33, torch.bfloat16)
     with pytest.raises(gc.GeoCacheError):
         gc.gc_linear_workspace_bytes(4, 6, 32, torch.float16)
+    for sizes in ((4, 2 ** 32 + 6, 32), (4, 6, 2 ** 32 + 32), (2 ** 31, 6, 32), (4, -1, 32)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            gc.gc_linear_workspace_bytes(*sizes, torch.bfloat16)

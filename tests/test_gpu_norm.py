@@ -241,3 +241,12 @@ def test_refusals_on_the_device(gc):
         gc.gc_add_rms_norm(x, out=torch.zeros((1, 32), device=DEV).expand(4, -1))
     with pytest.raises(gc.GeoCacheError, match="out_scale"):
         gc.gc_add_rms_norm(x, out_scale=torch.zeros(4, device=DEV))
+
+
+def test_sizes_past_32_bits_are_refused(gc):
+    x = torch.ones((1, 16), device=DEV)
+    for call in (gc.gc_add_rms_norm, gc.gc_quantize_rows):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call(x.expand(2 ** 32 + 3, 16))
+    with pytest.raises(ValueError, match="2\\^31"):
+        gc.gc_linear(x, x.expand(2 ** 32 + 3, 16))
