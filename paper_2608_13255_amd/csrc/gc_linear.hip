@@ -6,7 +6,7 @@
 // the weights' bytes, everything else by the matrix units.  Measured, us, with the time of the bound at a large
 // product's 1570 (bfloat16), 2720 (8 bits) and 153 TFLOP/s (float32), or a large read's 7.0 TB/s:
 //   1 x 6144 x 4096 bfloat16                                  11.9   7.2
-//   16 x 8192 x 4096 in 8 bits                                11.0   4.8
+//   16 x 8192 x 4096 in 8 bits                                 9.2   4.8
 //   1024 x 1283 x 1024 float32, bias, GELU, residual          33.6  17.6
 //   10403 x 2736 gated x 1024 bfloat16                         132    74
 //   10403 x 1024 x 2736 bfloat16, bias, residual                68    37
@@ -47,21 +47,27 @@ struct CostList {
 };
 CostList costs_of(int dtype) { return dtype == GC_F32 ? CostList(kCostsF32) : dtype == GC_BF16 ? CostList(kCosts) : CostList(kCostsE4M3); }
 
-// Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 13 us; in tiles with
+// Variant and parts.  At most 16 rows: each weight is read once by one wave (1 x 6144 x 4096 bfloat16 12 us; in tiles with
 // parts 16); a wave's share of a row where there are few weight rows is cut by more waves, then by parts (16 x 1024 gated x
-// 2736 13 us whole, 9 in four; 1 x 16384 x 4096 in 8 bits 13.1, 14.3 and 16.6 with 8, 4 and 16 waves a block).  Else the tiles, and the parts of the inner dimension, that take least: 4096^3 bfloat16 183, 137 and
-// 104 us with tiles of 64, 128 and 256, 10403 x 1024 x 2736 81 with 256 and 69 with 192, 1024^3 10.6, 11.3 and 26, 128 x 1024 x 4096 28, 29 and 74 whole, 12.6 with 64 in eight parts.
+// 2736 13 us whole, 9 in four; 1 x 16384 x 4096 in 8 bits 13.1, 14.3 and 16.6 with 8, 4 and 16 waves a block).  From 9 rows on
+// a block reads as much of x as of 16 weight rows, so it takes 32 where enough blocks are left (16384 x 4096 bfloat16 with 16, 12, 8
+// and 4 rows 30.0, 28.9, 28.6 and 28.2 us, with 16 weight rows 33.6, 30.9, 28.1 and 25.8).  Else the tiles, and the parts of the inner
+// dimension, that take least: 4096^3 bfloat16 183, 137 and 104 us with tiles of 64, 128 and 256, 10403 x 1024 x 2736 81 with
+// 256 and 69 with 192, 1024^3 10.6, 11.3 and 26, 128 x 1024 x 4096 28, 29 and 74 whole, 12.6 with 64 in eight parts.
+constexpr int kWideRows = 9;
 LinearPlan choose(int64_t n_rows, int n_out, int row_bytes, int dtype, int gated) {
   const int steps = (row_bytes + kStepBytes - 1) / kStepBytes;
   const auto in_parts = [&](int kind, int parts, int waves) {
     const int each = (steps + parts - 1) / parts;
-    return LinearPlan{kind, (steps + each - 1) / each, each * kStepBytes, waves};
+    return LinearPlan{kind, (steps + each - 1) / each, each * kStepBytes, waves, false};
   };
   const double w_rows = gated ? 2.0 * n_out : n_out;
   if (n_rows <= kLinearFewRows) {
     const int blocks = (n_out + 15) / 16;
     const int parts = std::min({8, kCus / blocks, row_bytes / 1280});
-    return in_parts(kLinearFew, std::max(1, parts), blocks <= kCus ? 16 : 8);
+    LinearPlan plan = in_parts(kLinearFew, std::max(1, parts), blocks <= kCus ? 16 : 8);
+    plan.wide = !gated && n_rows >= kWideRows && blocks >= 2 * kCus;
+    return plan;
   }
   LinearPlan best = {};
   double least = 0;

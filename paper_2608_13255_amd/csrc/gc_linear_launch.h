@@ -31,8 +31,10 @@ void launch_tiles(LinearArgs p, hipStream_t stream) {
 template <class Few, bool kGated>
 void launch_few(const LinearArgs& p, const LinearPlan& plan, hipStream_t stream) {
   const dim3 grid((unsigned)((p.n_out + 15) / 16), (unsigned)p.parts);
-  if (plan.waves == 8) k_linear_few<Few, 8, kGated><<<grid, 512, 0, stream>>>(p);
-  else k_linear_few<Few, 16, kGated><<<grid, 1024, 0, stream>>>(p);
+  if constexpr (!kGated)
+    if (plan.wide) return k_linear_few<Few, 8, false, true><<<dim3((unsigned)((p.n_out + 31) / 32)), 512, 0, stream>>>(p);
+  if (plan.waves == 8) k_linear_few<Few, 8, kGated, false><<<grid, 512, 0, stream>>>(p);
+  else k_linear_few<Few, 16, kGated, false><<<grid, 1024, 0, stream>>>(p);
 }
 
 // Few: the operand type of few rows; Op: of tiles; kLargeX: rows of x of a wave of the largest tiles.  Tiles of 128 hold two

@@ -19,6 +19,7 @@ enum LinearKind : int {
 struct LinearPlan {
   int kind, parts, part_bytes;
   int waves;      // of a block of kLinearFew
+  bool wide;      // 32 weight rows a block of kLinearFew (not gated, one part)
 };
 
 constexpr int kLinearFewRows = 16;

@@ -119,6 +119,13 @@ def test_epilogues(gc, kind, out, M, N, K, act, gated, bias, residual):
     run(gc, kind, out, M, N, K, act, gated, bias, residual)
 
 
+# more than eight rows and many weight rows: 32 of them a block, the last block's second 16 whole, one, or none
+@pytest.mark.parametrize("kind,out", PAIRS)
+@pytest.mark.parametrize("M,N,K", [(9, 8177, 272), (16, 8193, 1040), (12, 8208, 16), (16, 8224, 4096)])
+def test_rows_with_many_weight_rows(gc, kind, out, M, N, K):
+    run(gc, kind, out, M, N, K, "gelu", False, True, True)
+
+
 # every variant, by what the rule on sizes takes there: tiles of 64 (and 32 x 64) and 128, one and two on a compute unit, 192, 256;
 # one part, a few and sixteen
 @pytest.mark.parametrize("kind,out", PAIRS)
