@@ -119,33 +119,39 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
   if (kRows > 1 && row >= p.n_rows) return;   // (a block of one row is never past the end)
   const T* x = (const T*)p.x + row * p.x_row;
+  // A row's last group, if it is not whole, begins V before the row's end: its first values, the group before has as well.
+  const auto first = [&](int u) { return (u * kLanes + i) * V; };
+  const auto in_row = [&](int u) { return first(u) < p.width; };
+  const int last = p.width > V ? p.width - V : 0, have = p.width < V ? p.width : V;
+  const auto place = [&](int u) { return kWhole || first(u) < last ? first(u) : last; };
   float h[kGroups][V];
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
-    const int at = (u * kLanes + i) * V;
+    const int at = place(u);
 #pragma unroll
     for (int j = 0; j < V; ++j) h[u][j] = 0.f;
-    if (at < p.width) load_group<T, V, kWhole, kOnce>(x + at, p.width - at, h[u]);
+    if (in_row(u)) load_group<T, V, kWhole, kOnce>(x + at, have, h[u]);
   }
   if (p.residual) {
     const T* r = (const T*)p.residual + row * p.residual_row;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      const int at = (u * kLanes + i) * V;
-      if (at < p.width) {
+      const int at = place(u);
+      if (in_row(u)) {
         float a[V];
-        load_group<T, V, kWhole, kOnce>(r + at, p.width - at, a);
+        load_group<T, V, kWhole, kOnce>(r + at, have, a);
 #pragma unroll
         for (int j = 0; j < V; ++j) h[u][j] += a[j];
       }
     }
   }
   if (p.total) {
+    if constexpr (!kWhole && kWaves > 1) __syncthreads();   // (it may be an input: what another wave stores has been read by this one)
     T* t = (T*)p.total + row * p.total_row;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      const int at = (u * kLanes + i) * V;
-      if (at < p.width) store_group<T, V, kWhole, kOnce>(t + at, p.width - at, h[u]);
+      const int at = place(u);
+      if (in_row(u)) store_group<T, V, kWhole, kOnce>(t + at, have, h[u]);
     }
   }
   if (p.norm) {
@@ -153,7 +159,10 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
 #pragma unroll
     for (int u = 0; u < kGroups; ++u)
 #pragma unroll
-      for (int j = 0; j < V; ++j) q = __builtin_fmaf(h[u][j], h[u][j], q);
+      for (int j = 0; j < V; ++j) {
+        const float a = kWhole || j >= first(u) - place(u) ? h[u][j] : 0.f;
+        q = __builtin_fmaf(a, a, q);
+      }
     q = sum_lanes<kLanes>(q);
     if constexpr (kWaves > 1) {
       if (i % 64 == 0) shared[wave] = __float_as_uint(q);
@@ -165,14 +174,19 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
     const float r = reciprocal_root_of(__builtin_fmaf(q, p.inv_width, p.eps));
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      const int at = (u * kLanes + i) * V;
-      if (at < p.width) {
+      const int at = place(u);
+      if (in_row(u)) {
         float g[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) g[j] = 1.f;
         if (p.gain) {
+          if (kWhole || have == V) {
 #pragma unroll
-          for (int j = 0; j < V; ++j) g[j] = kWhole || at + j < p.width ? p.gain[at + j] : 0.f;
+            for (int j = 0; j < V; ++j) g[j] = p.gain[at + j];
+          } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) g[j] = j < have ? p.gain[j] : 0.f;
+          }
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) h[u][j] = h[u][j] * r * g[j];
@@ -183,8 +197,8 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
     T* o = (T*)p.out + row * p.out_row;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
-      const int at = (u * kLanes + i) * V;
-      if (at < p.width) store_group<T, V, kWhole, kOnce>(o + at, p.width - at, h[u]);
+      const int at = place(u);
+      if (in_row(u)) store_group<T, V, kWhole, kOnce>(o + at, have, h[u]);
     }
     return;
   }
@@ -207,14 +221,14 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
   uint8_t* o = (uint8_t*)p.out + row * p.out_row;
 #pragma unroll
   for (int u = 0; u < kGroups; ++u) {
-    const int at = (u * kLanes + i) * V;
-    if (at < p.width) {
+    const int at = place(u);
+    if (in_row(u)) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {   // the quotient, correctly rounded: the product and one step with its remainder
         const float q = h[u][j] * inv;
         h[u][j] = __builtin_fmaf(__builtin_fmaf(-q, scale, h[u][j]), inv, q);
       }
-      store_eight<V, kWhole, kOnce>(o + at, p.width - at, h[u]);
+      store_eight<V, kWhole, kOnce>(o + at, have, h[u]);
     }
   }
 }
@@ -244,7 +258,7 @@ constexpr int64_t kOnceBytes = 192 << 20;
 
 // Narrow rows in parts of a wave (70920 x 16 bfloat16 9 us, 18 in waves), a
 // row in one wave up to two groups a lane, rows that are not of whole groups
-// up to eight (5741 x 1283 float32 24 us, 27 in blocks); else in a block
+// up to eight (5741 x 1283 float32 21 us); else in a block
 // (196608 x 2048 bfloat16 with its sum 468 us, 497 in waves; 16384 x 4096
 // float32 to 8 bits 53 us in blocks of 512, 56 of 256 and 66 of 1024).
 template <class T, bool kWhole, bool kOnce>
