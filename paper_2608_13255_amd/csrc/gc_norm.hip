@@ -10,7 +10,7 @@
 //   196608 x 2048 bfloat16 with its sum, to 8 bits     470  434
 //   16384 x 4096 float32 to 8 bits                      53   52
 //   10403 x 4096 bfloat16 to 8 bits                     22   20
-//   5741 x 1283 float32 with its sum                    24   18   (rows that begin anywhere)
+//   5741 x 1283 float32 with its sum                    21   18   (rows that begin anywhere)
 //   1 x 4096 bfloat16                                  2.7        (a call from Python 8.1)
 #include <cmath>
 
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
     }
   }
   if (p.total) {
-    if constexpr (!kWhole && kWaves > 1) __syncthreads();   // (it may be an input: what another wave stores has been read by this one)
+    if constexpr (!kWhole && kWaves > 1) __syncthreads();   // (it may be an input; waves share a row's last bytes)
     T* t = (T*)p.total + row * p.total_row;
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {

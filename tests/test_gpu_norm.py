@@ -250,3 +250,25 @@ def test_sizes_past_32_bits_are_refused(gc):
             call(x.expand(2 ** 32 + 3, 16))
     with pytest.raises(ValueError, match="2\\^31"):
         gc.gc_linear(x, x.expand(2 ** 32 + 3, 16))
+
+
+# odd widths, whose last 16 bytes overlap the ones before: in parts of a wave, one wave, and several that store while others read
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("width", [9, 67, 131, 517, 1283, 4099, 9001, 20001, 32767])
+def test_odd_rows_in_place(gc, dtype, width):
+    n = 300
+    x, r = rows(n, width, dtype, 30), rows(n, width, dtype, 31)
+    gain = rows(1, width, torch.float32, 32)[0]
+    want, _, total = gc.gc_add_rms_norm(x, residual=r, gain=gain)
+    assert torch.equal(total, (x.float() + r.float()).to(dtype))
+    for times in range(3):
+        a, b = x.clone(), r.clone()
+        gc.gc_add_rms_norm(a, residual=b, gain=gain, total=a, out=b)
+        assert torch.equal(a, total) and torch.equal(b, want)
+        a, b = x.clone(), r.clone()
+        gc.gc_add_rms_norm(a, residual=b, gain=gain, total=b, out=a)
+        assert torch.equal(b, total) and torch.equal(a, want)
+    eight, scale, _ = gc.gc_add_rms_norm(x, residual=r, gain=gain, out_dtype=torch.float8_e4m3fn)
+    a = x.clone()
+    got, got_scale, _ = gc.gc_add_rms_norm(a, residual=r, gain=gain, total=a, out_dtype=torch.float8_e4m3fn)
+    assert torch.equal(a, total) and torch.equal(got.view(torch.uint8), eight.view(torch.uint8)) and torch.equal(got_scale, scale)
