@@ -119,7 +119,8 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm(const Norm
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
   if (kRows > 1 && row >= p.n_rows) return;   // (a block of one row is never past the end)
   const T* x = (const T*)p.x + row * p.x_row;
-  // A row's last group, if it is not whole, begins V before the row's end: its first values, the group before has as well.
+  // A row's last group, if it is not whole, begins V before the row's end, so that it is one access too (50000 x 1283 bfloat16
+  // with its sum 101 us, 162 by elements).  Its first values are the group before's as well: both store the same, one counts them.
   const auto first = [&](int u) { return (u * kLanes + i) * V; };
   const auto in_row = [&](int u) { return first(u) < p.width; };
   const int last = p.width > V ? p.width - V : 0, have = p.width < V ? p.width : V;
