@@ -192,8 +192,9 @@ class MultiViewBlock(_SlicedAttention):
         for n in (self.width, self.heads * self.dim, self.hidden):
             if n % 16:
                 raise ValueError(f"8-bit products need a width, heads * dim and hidden of whole 16 (got {n})")
-        self.eight_bits = {name: gc_quantize_rows(getattr(self, name)) for name in ("w_qkv", "w_out", "w_in", "w_down")}
+        rows = {name: gc_quantize_rows(getattr(self, name)) for name in ("w_qkv", "w_out", "w_in", "w_down")}
         torch.cuda.current_stream(self.foreground.device).synchronize()   # any stream may read them from here on
+        self.eight_bits = rows
 
     def _product(self, name: str, x: torch.Tensor, scale: Optional[torch.Tensor] = None, **more) -> torch.Tensor:
         """x (of the layer's type, or 8-bit rows with their scales) times a weight."""

@@ -1,0 +1,48 @@
+"""When a block's weights are laid out in 8 bits again: what other threads and
+streams see of it (the operators replaced by ones on the CPU, no GPU)."""
+import pytest
+import torch
+
+from paper_2608_13255_amd import multiview
+
+NAMES = ("w_qkv", "w_out", "w_in", "w_down")
+
+
+def block_with(numbers):
+    """A block without its construction; weight `name` holds numbers[name]."""
+    block = object.__new__(multiview.MultiViewBlock)
+    block.width, block.heads, block.kv_heads, block.dim, block.hidden = 16, 2, 1, 16, 32
+    block.dtype, block.eps, block.act, block.gated = torch.float32, 1e-6, 1, False
+    block.foreground = torch.ones((1, 1, 1, 1), dtype=torch.bool)
+    block.eight_bits = None
+    for name in NAMES:
+        setattr(block, name, torch.full((1, 1), float(numbers[name])))
+        setattr(block, "b" + name[1:], None)
+    block.q_gain = block.k_gain = block.attention_gain = block.feed_gain = torch.ones(1)
+    return block
+
+
+class Stream:
+    cuda_stream = 77
+
+    def __init__(self, at_synchronize=lambda: None):
+        self.at_synchronize = at_synchronize
+
+    def synchronize(self):
+        self.at_synchronize()
+
+
+@pytest.fixture
+def quantized(monkeypatch):
+    monkeypatch.setattr(multiview, "gc_quantize_rows", lambda w: (w.clone(), torch.ones(1)))
+
+
+def test_weights_are_published_when_they_are_complete(monkeypatch, quantized):
+    block = block_with(dict.fromkeys(NAMES, 1))
+    seen = []
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream(lambda: seen.append(block.eight_bits)))
+    block.lay_out_in_8_bits()
+    first = block.eight_bits
+    assert seen == [None] and set(first) == set(NAMES)
+    block.lay_out_in_8_bits()
+    assert seen[1] is first and block.eight_bits is not first
