@@ -188,7 +188,8 @@ class MultiViewBlock(_SlicedAttention):
     def lay_out_in_8_bits(self) -> None:
         """The products' weights as they are now in 8 bits with a scale a row:
         calls from here on use those, whatever is loaded into w_... later
-        (call again after that).  width, heads * dim and hidden are multiples of 16."""
+        (call again after that; calls that have begun go on with the rows that they began
+        with).  width, heads * dim and hidden are multiples of 16."""
         for n in (self.width, self.heads * self.dim, self.hidden):
             if n % 16:
                 raise ValueError(f"8-bit products need a width, heads * dim and hidden of whole 16 (got {n})")
@@ -196,14 +197,15 @@ class MultiViewBlock(_SlicedAttention):
         torch.cuda.current_stream(self.foreground.device).synchronize()   # any stream may read them from here on
         self.eight_bits = rows
 
-    def _product(self, name: str, x: torch.Tensor, scale: Optional[torch.Tensor] = None, **more) -> torch.Tensor:
-        """x (of the layer's type, or 8-bit rows with their scales) times a weight."""
+    def _product(self, name: str, rows: Optional[Dict[str, Tuple[torch.Tensor, torch.Tensor]]], x: torch.Tensor,
+                 scale: Optional[torch.Tensor] = None, **more) -> torch.Tensor:
+        """x (of the layer's type, or 8-bit rows with their scales) times a weight, that of `rows` where there are some."""
         bias = getattr(self, "b" + name[1:])
-        if self.eight_bits is None:
+        if rows is None:
             return gc_linear(x, getattr(self, name), bias, out_dtype=self.dtype, **more)
         if scale is None:
             x, scale = gc_quantize_rows(x)
-        w, w_scale = self.eight_bits[name]
+        w, w_scale = rows[name]
         return gc_linear(x, w, bias, x_scale=scale, w_scale=w_scale, out_dtype=self.dtype, **more)
 
     def __call__(self, x: torch.Tensor, views: Sequence[int]) -> torch.Tensor:
@@ -211,10 +213,11 @@ class MultiViewBlock(_SlicedAttention):
         output on foreground tokens, zeros on the background."""
         s, tokens = self._tokens(x, views, (self.w_qkv, self.w_out, self.w_in, self.w_down, self.b_qkv, self.b_out, self.b_in,
                                             self.b_down, self.q_gain, self.k_gain, self.attention_gain, self.feed_gain))
-        normed = torch.float8_e4m3fn if self.eight_bits is not None else self.dtype
+        rows = self.eight_bits                                            # (another thread may lay them out again)
+        normed = torch.float8_e4m3fn if rows is not None else self.dtype
         n, scale, _ = gc_add_rms_norm(tokens, gain=self.attention_gain, eps=self.eps, out_dtype=normed)
-        out = self._attend(self._product("w_qkv", n, scale), s)
-        out = self._product("w_out", out.view(-1, self.heads * self.dim))
+        out = self._attend(self._product("w_qkv", rows, n, scale), s)
+        out = self._product("w_out", rows, out.view(-1, self.heads * self.dim))
         n, scale, h = gc_add_rms_norm(out, residual=tokens, gain=self.feed_gain, eps=self.eps, out_dtype=normed, total=out)
-        m = self._product("w_in", n, scale, act=self.act, gated=self.gated)
-        return self._spread(self._product("w_down", m, residual=h, out=h), x, s)
+        m = self._product("w_in", rows, n, scale, act=self.act, gated=self.gated)
+        return self._spread(self._product("w_down", rows, m, residual=h, out=h), x, s)

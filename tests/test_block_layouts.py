@@ -1,5 +1,7 @@
 """When a block's weights are laid out in 8 bits again: what other threads and
 streams see of it (the operators replaced by ones on the CPU, no GPU)."""
+from types import SimpleNamespace
+
 import pytest
 import torch
 
@@ -46,3 +48,27 @@ def test_weights_are_published_when_they_are_complete(monkeypatch, quantized):
     assert seen == [None] and set(first) == set(NAMES)
     block.lay_out_in_8_bits()
     assert seen[1] is first and block.eight_bits is not first
+
+
+def test_a_call_keeps_the_weights_it_began_with(monkeypatch, quantized):
+    block = block_with(dict.fromkeys(NAMES, 1))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
+    block.lay_out_in_8_bits()
+    monkeypatch.setattr(block, "_tokens", lambda x, views, weights: (SimpleNamespace(), torch.zeros(3, 32)), raising=False)
+    monkeypatch.setattr(block, "_attend", lambda qkv, s: torch.zeros(3, 32), raising=False)
+    monkeypatch.setattr(block, "_spread", lambda y, x, s: y, raising=False)
+    monkeypatch.setattr(multiview, "gc_add_rms_norm", lambda x, **more: (x, torch.ones(3), x))
+    used = []
+
+    def product(x, w, bias, **more):
+        used.append(float(w))
+        for name in NAMES:                       # another thread, between two products
+            getattr(block, name).add_(1)
+        block.lay_out_in_8_bits()
+        return torch.zeros(3, 32)
+
+    monkeypatch.setattr(multiview, "gc_linear", product)
+    block(torch.zeros(3, 32), [0])
+    assert used == [1, 1, 1, 1]
+    block(torch.zeros(3, 32), [0])
+    assert used[4:] == [5, 5, 5, 5]
