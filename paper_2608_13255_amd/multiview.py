@@ -26,8 +26,29 @@ from . import (GC_ACT_SILU, GC_MAX_VIEWS, GC_ROPE_HALF, AttentionPlan, gc_add_rm
                gc_linear, gc_qk_norm_rope, gc_quantize_rows, gc_rope_table)
 
 
+class _Shared:
+    """Tensors that calls on several streams read.  known_streams: handles of
+    the streams after whose work torch's allocator reuses their memory."""
+
+    def _tensors(self) -> Sequence[torch.Tensor]:
+        raise NotImplementedError
+
+    def used_here(self) -> None:
+        """Work on the current stream reads the tensors: their memory stays
+        theirs until that is done, also where they are dropped before."""
+        tensors = self._tensors()
+        stream = torch.cuda.current_stream(tensors[0].device)
+        if stream.cuda_stream not in self.known_streams:
+            for t in tensors:
+                t.record_stream(stream)
+            self.known_streams.add(stream.cuda_stream)
+
+    def __getstate__(self):   # a copy's memory is another, known on no stream
+        return {**self.__dict__, "known_streams": set()}
+
+
 @dataclass
-class TokenSlice:
+class TokenSlice(_Shared):
     """Foreground tokens of a list of views: rows of the flattened
     [B, len(views), H, W] grid (int64), asset by asset; each asset's number of
     them; their (view, row, column) (int32 [T, 3]); the plan of attention
@@ -36,20 +57,21 @@ class TokenSlice:
     lens: List[int]
     positions: torch.Tensor
     plan: AttentionPlan
-    # handles of the streams after whose work torch's allocator reuses the tensors' memory
     known_streams: Set[int] = field(default_factory=set)
 
-    def used_here(self) -> None:
-        """Work on the current stream reads the slice: its memory stays its
-        own until that is done, also where the slice is dropped before."""
-        stream = torch.cuda.current_stream(self.index.device)
-        if stream.cuda_stream not in self.known_streams:
-            self.index.record_stream(stream)
-            self.positions.record_stream(stream)
-            self.known_streams.add(stream.cuda_stream)
+    def _tensors(self) -> Sequence[torch.Tensor]:
+        return self.index, self.positions
 
-    def __getstate__(self):   # a copy's memory is another, known on no stream
-        return {**self.__dict__, "known_streams": set()}
+
+class EightBitWeights(_Shared, Dict[str, Tuple[torch.Tensor, torch.Tensor]]):
+    """(8-bit rows, their scales) of a block's weights by name."""
+
+    def __init__(self, *args, **kwargs):
+        super().__init__(*args, **kwargs)
+        self.known_streams: Set[int] = set()
+
+    def _tensors(self) -> Sequence[torch.Tensor]:
+        return [t for pair in self.values() for t in pair]
 
 
 class _SlicedAttention:
@@ -183,7 +205,7 @@ class MultiViewBlock(_SlicedAttention):
         self.b_qkv = self.b_out = self.b_in = self.b_down = None
         self.attention_gain = torch.ones(width, dtype=torch.float32, device=dev)
         self.feed_gain = torch.ones(width, dtype=torch.float32, device=dev)
-        self.eight_bits: Optional[Dict[str, Tuple[torch.Tensor, torch.Tensor]]] = None
+        self.eight_bits: Optional[EightBitWeights] = None
 
     def lay_out_in_8_bits(self) -> None:
         """The products' weights as they are now in 8 bits with a scale a row:
@@ -193,12 +215,14 @@ class MultiViewBlock(_SlicedAttention):
         for n in (self.width, self.heads * self.dim, self.hidden):
             if n % 16:
                 raise ValueError(f"8-bit products need a width, heads * dim and hidden of whole 16 (got {n})")
-        rows = {name: gc_quantize_rows(getattr(self, name)) for name in ("w_qkv", "w_out", "w_in", "w_down")}
-        torch.cuda.current_stream(self.foreground.device).synchronize()   # any stream may read them from here on
+        stream = torch.cuda.current_stream(self.foreground.device)
+        rows = EightBitWeights({name: gc_quantize_rows(getattr(self, name)) for name in ("w_qkv", "w_out", "w_in", "w_down")})
+        rows.known_streams.add(stream.cuda_stream)
+        stream.synchronize()                                              # any stream may read them from here on
         self.eight_bits = rows
 
-    def _product(self, name: str, rows: Optional[Dict[str, Tuple[torch.Tensor, torch.Tensor]]], x: torch.Tensor,
-                 scale: Optional[torch.Tensor] = None, **more) -> torch.Tensor:
+    def _product(self, name: str, rows: Optional[EightBitWeights], x: torch.Tensor, scale: Optional[torch.Tensor] = None,
+                 **more) -> torch.Tensor:
         """x (of the layer's type, or 8-bit rows with their scales) times a weight, that of `rows` where there are some."""
         bias = getattr(self, "b" + name[1:])
         if rows is None:
@@ -214,6 +238,8 @@ class MultiViewBlock(_SlicedAttention):
         s, tokens = self._tokens(x, views, (self.w_qkv, self.w_out, self.w_in, self.w_down, self.b_qkv, self.b_out, self.b_in,
                                             self.b_down, self.q_gain, self.k_gain, self.attention_gain, self.feed_gain))
         rows = self.eight_bits                                            # (another thread may lay them out again)
+        if rows is not None:
+            rows.used_here()
         normed = torch.float8_e4m3fn if rows is not None else self.dtype
         n, scale, _ = gc_add_rms_norm(tokens, gain=self.attention_gain, eps=self.eps, out_dtype=normed)
         out = self._attend(self._product("w_qkv", rows, n, scale), s)

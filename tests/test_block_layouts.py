@@ -1,5 +1,6 @@
 """When a block's weights are laid out in 8 bits again: what other threads and
 streams see of it (the operators replaced by ones on the CPU, no GPU)."""
+import copy
 from types import SimpleNamespace
 
 import pytest
@@ -72,3 +73,32 @@ def test_a_call_keeps_the_weights_it_began_with(monkeypatch, quantized):
     assert used == [1, 1, 1, 1]
     block(torch.zeros(3, 32), [0])
     assert used[4:] == [5, 5, 5, 5]
+
+
+def test_weights_are_known_on_each_stream_that_reads_them(monkeypatch):
+    """Each stream that reads them is told to the allocator once; the one that they were made on needs no telling."""
+    told = []
+
+    class Tensor:
+        device = torch.device("cuda:0")
+
+        def record_stream(self, stream):
+            told.append((id(self), stream.cuda_stream))
+
+    pairs = {name: (Tensor(), Tensor()) for name in NAMES}
+    rows = multiview.EightBitWeights(pairs)
+    rows.known_streams.add(77)
+    home, other = Stream(), Stream()
+    other.cuda_stream = 78
+    for stream in (home, other, home, other):
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: stream)
+        rows.used_here()
+    assert sorted(told) == sorted((id(t), 78) for pair in pairs.values() for t in pair)
+
+
+def test_a_copy_is_known_on_no_stream():
+    rows = multiview.EightBitWeights({"w_in": (torch.zeros(2), torch.ones(1))})
+    rows.known_streams.add(77)
+    other = copy.deepcopy(rows)
+    assert not other.known_streams and rows.known_streams == {77}
+    assert torch.equal(other["w_in"][0], rows["w_in"][0]) and other["w_in"][0] is not rows["w_in"][0]

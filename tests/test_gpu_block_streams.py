@@ -1,0 +1,60 @@
+"""A block used on several streams while its weights are laid out again: what a
+call that is behind has yet to read stays its own."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def small_block(seed, dtype=torch.bfloat16):
+    from paper_2608_13255_amd.multiview import MultiViewBlock
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    pos = torch.randn((1, 6, 16, 16, 3), generator=g, device=DEV)
+    return MultiViewBlock(pos, 64, 4, 2, 64, 176, dtype=dtype, generator=g), g
+
+
+def stream_beside(home):
+    """A stream whose work does not hold up home's (streams may share a hardware queue)."""
+    probe = torch.zeros(1, device=DEV)
+    for _ in range(8):
+        other = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            torch.cuda._sleep(40_000_000)
+        with torch.cuda.stream(home):
+            probe.add_(1)
+        home.synchronize()
+        if not other.query():
+            torch.cuda.synchronize()
+            return other
+    pytest.skip("every stream shares home's queue")
+
+
+def test_weights_laid_out_again_while_another_stream_reads_them():
+    block, g = small_block(20)
+    x = torch.randn((1, 2, 16, 16, 64), generator=g, device=DEV).bfloat16()
+    home = torch.cuda.Stream()
+    home.wait_stream(torch.cuda.current_stream())
+    other = stream_beside(home)
+    with torch.cuda.stream(home):
+        block.lay_out_in_8_bits()
+        want = block(x, [0, 3])
+        block.w_in.mul_(2), block.w_down.neg_()
+    torch.cuda.synchronize()
+    old = [t for pair in block.eight_bits.values() for t in pair]
+    at, sizes = {t.data_ptr() for t in old}, [t.numel() * t.element_size() for t in old]
+    del old
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(40_000_000)
+        got = block(x, [0, 3])
+    with torch.cuda.stream(home):
+        block.lay_out_in_8_bits()
+        later = [torch.full((n,), 0x7f, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(3)]
+    assert not other.query()
+    assert not at & {t.data_ptr() for t in later}
+    assert not at & {t.data_ptr() for pair in block.eight_bits.values() for t in pair}
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    assert not torch.equal(block(x, [0, 3]), want)
