@@ -243,6 +243,28 @@ def _keep(stream, tensors) -> None:
             t.record_stream(s)
 
 
+def _empty(stream, shape, dtype: torch.dtype, device) -> torch.Tensor:
+    """Memory for work on `stream`.  Of a side stream's own, since current-stream
+    work that has yet to end may still use what torch's allocator hands out
+    here: nothing orders the side stream after it.  What the current stream
+    reads of it later keeps it from being handed out again, too."""
+    side = None if stream is None else _side_stream(stream)
+    if side is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(side):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _empty_like(stream, x: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """_empty of x's shape (and type), contiguous."""
+    if stream is None:
+        return torch.empty_like(x, dtype=dtype, memory_format=_CONTIGUOUS)
+    return _empty(stream, x.shape, x.dtype if dtype is None else dtype, x.device)
+
+
 def _after_side(stream) -> None:
     """Order torch's current stream (and so a following host read-back)
     after the work just enqueued on a side stream."""
@@ -310,7 +332,7 @@ def gc_posmap_downsample(pos_hi: torch.Tensor, f: int, pos_lat: torch.Tensor = N
     n = int(np.prod(lead)) if lead else 1
     fresh = []
     if pos_lat is None:
-        pos_lat = torch.empty(lead + (Hr // f, Wr // f, 3), dtype=torch.float32, device=pos_hi.device)
+        pos_lat = _empty(stream, lead + (Hr // f, Wr // f, 3), torch.float32, pos_hi.device)
         fresh.append(pos_lat)
     _check(lib().gc_posmap_downsample(_dev(pos_hi, "pos_hi"), n, Hr, Wr, f, _dev(pos_lat, "pos_lat"),
                                       _stream(stream)), "gc_posmap_downsample")
@@ -325,7 +347,7 @@ def gc_posmap_bbox(pos: torch.Tensor, tol_frac: float = 0.01, bbox: torch.Tensor
     B, N, H, W, _ = pos.shape
     fresh = []
     if bbox is None:
-        bbox = torch.empty((B, 8), dtype=torch.float32, device=pos.device)
+        bbox = _empty(stream, (B, 8), torch.float32, pos.device)
         fresh.append(bbox)
     _check(lib().gc_posmap_bbox(_dev(pos, "pos"), B, N, H, W, float(tol_frac), _dev(bbox, "bbox"),
                                 _stream(stream)), "gc_posmap_bbox")
@@ -349,10 +371,10 @@ def gc_build_correspondence(pos: torch.Tensor, cams: torch.Tensor, anchors: Sequ
     dev = pos.device
     fresh = []
     if corr is None:
-        corr = torch.empty((B, NT, H, W, a), dtype=torch.int32, device=dev)
+        corr = _empty(stream, (B, NT, H, W, a), torch.int32, dev)
         fresh.append(corr)
     if weights is None:
-        weights = torch.empty((B, NT, H, W, a, K), dtype=torch.float32, device=dev)
+        weights = _empty(stream, (B, NT, H, W, a, K), torch.float32, dev)
         fresh.append(weights)
     if tuple(corr.shape) != (B, NT, H, W, a) or corr.dtype != torch.int32:
         raise ValueError("corr must be int32 [B, N-a, H, W, a]")
@@ -390,12 +412,12 @@ def gc_index_correspondence(corr: torch.Tensor, workspace: torch.Tensor = None, 
     dev = corr.device
     need = int(lib().gc_index_workspace_bytes(n_tok))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, need, torch.uint8, dev)
     if workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace must hold at least {need} bytes")
-    bits = torch.empty(max(1, (n_tok + 31) // 32), dtype=torch.int32, device=dev)
-    lst = torch.empty(max(1, n_tok), dtype=torch.int32, device=dev)
-    nv = torch.empty(1, dtype=torch.int32, device=dev)
+    bits = _empty(stream, max(1, (n_tok + 31) // 32), torch.int32, dev)
+    lst = _empty(stream, max(1, n_tok), torch.int32, dev)
+    nv = _empty(stream, 1, torch.int32, dev)
     _check(lib().gc_index_correspondence(_dev(corr, "corr") if n_tok else None, n_views, H, W, a,
                                          _dev(bits, "vis_bits"), _dev(lst, "vis_list"), _dev(nv, "n_vis"),
                                          _dev(workspace, "workspace"),
@@ -417,9 +439,9 @@ def gc_index_correspondence_noalloc(corr: torch.Tensor, stream=None) -> VisibleI
     n_views = corr.shape[0] * corr.shape[1] if n_tok else 0
     H, W = max(corr.shape[2], 1), max(corr.shape[3], 1)
     dev = corr.device
-    bits = torch.empty(max(1, (n_tok + 31) // 32), dtype=torch.int32, device=dev)
-    lst = torch.empty(max(1, n_tok), dtype=torch.int32, device=dev)
-    nv = torch.empty(1, dtype=torch.int32, device=dev)
+    bits = _empty(stream, max(1, (n_tok + 31) // 32), torch.int32, dev)
+    lst = _empty(stream, max(1, n_tok), torch.int32, dev)
+    nv = _empty(stream, 1, torch.int32, dev)
     _check(lib().gc_index_correspondence_noalloc(_dev(corr, "corr") if n_tok else None, n_views, H, W, a,
                                                  _dev(bits, "vis_bits"), _dev(lst, "vis_list"), _dev(nv, "n_vis"),
                                                  _stream(stream)), "gc_index_correspondence_noalloc")
@@ -450,12 +472,12 @@ def gc_index_foreground(pos: torch.Tensor, workspace: torch.Tensor = None, strea
     dev = pos.device
     need = int(lib().gc_index_workspace_bytes(n_tok))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _empty(stream, need, torch.uint8, dev)
     if workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"workspace must hold at least {need} bytes")
-    bits = torch.empty(max(1, (n_tok + 31) // 32), dtype=torch.int32, device=dev)
-    recs = torch.empty((max(1, n_tok), 4), dtype=torch.int32, device=dev)
-    nf = torch.empty(1, dtype=torch.int32, device=dev)
+    bits = _empty(stream, max(1, (n_tok + 31) // 32), torch.int32, dev)
+    recs = _empty(stream, (max(1, n_tok), 4), torch.int32, dev)
+    nf = _empty(stream, 1, torch.int32, dev)
     _check(lib().gc_index_foreground(_dev(pos, "pos") if n_tok else None, n_views, max(H, 1), max(W, 1),
                                      _dev(bits, "fg_bits"),
                                      _dev(recs, "fg_recs"), _dev(nf, "n_fg"), _dev(workspace, "workspace"),
@@ -495,7 +517,7 @@ def gc_transport_step(x0_prev: torch.Tensor, x0_anchor_new: torch.Tensor, corr: 
         raise ValueError(f"x0_anchor_new must be [B, a={a}, H, W, C] of the same dtype as x0_prev")
     K = weights.shape[-1]
     if x0_out is None:
-        x0_out = torch.empty_like(x0_prev)
+        x0_out = _empty_like(stream, x0_prev)
     _check(lib().gc_transport_step(_dev(x0_prev, "x0_prev"), _dev(x0_anchor_new, "x0_anchor_new"),
                                    _dev(corr, "corr") if corr.numel() else None,
                                    _dev(weights, "weights") if weights.numel() else None, *_index_args(index),
@@ -511,9 +533,9 @@ def gc_sampler_reconstruct(x_t: torch.Tensor, x0: torch.Tensor, sampler: Sampler
     if x0.shape != x_t.shape or x0.dtype != x_t.dtype:
         raise ValueError("x_t and x0 must have the same shape and dtype")
     if x_next is None:
-        x_next = torch.empty_like(x_t)
+        x_next = _empty_like(stream, x_t)
     if sampler.pred_out != GC_PRED_NONE and model_out is None:
-        model_out = torch.empty_like(x_t)
+        model_out = _empty_like(stream, x_t)
     smp = sampler.c()
     _check(lib().gc_sampler_reconstruct(_dev(x_t, "x_t"), _dev(x0, "x0"), _dev(x_next, "x_next"),
                                         _opt(model_out, "model_out"), x_t.numel(), dtype_code(x_t),
@@ -537,11 +559,11 @@ def gc_transport_reconstruct(x0_prev: torch.Tensor, x0_anchor_new: torch.Tensor,
         raise ValueError("x_t must match x0_prev in shape and dtype")
     K = weights.shape[-1]
     if x0_out is None:
-        x0_out = torch.empty_like(x0_prev)
+        x0_out = _empty_like(stream, x0_prev)
     if x_next is None:
-        x_next = torch.empty_like(x_t)
+        x_next = _empty_like(stream, x_t)
     if sampler.pred_out != GC_PRED_NONE and model_out is None:
-        model_out = torch.empty_like(x_t)
+        model_out = _empty_like(stream, x_t)
     smp = sampler.c()
     _check(lib().gc_transport_reconstruct(_dev(x0_prev, "x0_prev"), _dev(x0_anchor_new, "x0_anchor_new"),
                                           _dev(corr, "corr") if corr.numel() else None,
@@ -578,7 +600,7 @@ def gc_transport_step_geom(x0_prev: torch.Tensor, x0_anchor_new: torch.Tensor, p
     `fg_index` (gc_index_foreground of pos) selects the foreground launch."""
     (B, N, H, W, C), arr, a = _geom_inputs(x0_prev, x0_anchor_new, pos, cams, bbox, anchors)
     if x0_out is None:
-        x0_out = torch.empty_like(x0_prev)
+        x0_out = _empty_like(stream, x0_prev)
     fb, fr, nf = _fg_args(fg_index)
     _check(lib().gc_transport_step_geom(_dev(x0_prev, "x0_prev"), _dev(x0_anchor_new, "x0_anchor_new"),
                                         _dev(pos, "pos"), _dev(cams, "cams"), _dev(bbox, "bbox"), fb, fr, nf, B, N, H,
@@ -601,11 +623,11 @@ def gc_transport_reconstruct_geom(x0_prev: torch.Tensor, x0_anchor_new: torch.Te
     if x_t.shape != x0_prev.shape or x_t.dtype != x0_prev.dtype:
         raise ValueError("x_t must match x0_prev in shape and dtype")
     if x0_out is None:
-        x0_out = torch.empty_like(x0_prev)
+        x0_out = _empty_like(stream, x0_prev)
     if x_next is None:
-        x_next = torch.empty_like(x_t)
+        x_next = _empty_like(stream, x_t)
     if sampler.pred_out != GC_PRED_NONE and model_out is None:
-        model_out = torch.empty_like(x_t)
+        model_out = _empty_like(stream, x_t)
     smp = sampler.c()
     fb, fr, nf = _fg_args(fg_index)
     _check(lib().gc_transport_reconstruct_geom(_dev(x0_prev, "x0_prev"), _dev(x0_anchor_new, "x0_anchor_new"),
@@ -672,9 +694,9 @@ def gc_unipc_update(st: UniPCStep, m_k: torch.Tensor, x_cur: torch.Tensor = None
                     x_next: torch.Tensor = None, stream=None):
     """UniPC update over all elements (a full step); returns (x_c, x_next)."""
     if x_c is None:
-        x_c = torch.empty_like(m_k)
+        x_c = _empty_like(stream, m_k)
     if x_next is None:
-        x_next = torch.empty_like(m_k)
+        x_next = _empty_like(stream, m_k)
     for name, t in (("x_cur", x_cur), ("x_prev", x_prev), ("m_km2", m_km2), ("m_km1", m_km1)):
         if t is not None and (t.shape != m_k.shape or t.dtype != m_k.dtype):
             raise ValueError(f"{name} must match m_k in shape and dtype")
@@ -700,9 +722,9 @@ def gc_transport_unipc(x0_prev: torch.Tensor, x0_anchor_new: torch.Tensor, corr:
         if t is not None and (t.shape != x0_prev.shape or t.dtype != x0_prev.dtype):
             raise ValueError(f"{name} must match x0_prev in shape and dtype")
     K = weights.shape[-1]
-    x0_out = torch.empty_like(x0_prev) if x0_out is None else x0_out
-    x_c = torch.empty_like(x0_prev) if x_c is None else x_c
-    x_next = torch.empty_like(x0_prev) if x_next is None else x_next
+    x0_out = _empty_like(stream, x0_prev) if x0_out is None else x0_out
+    x_c = _empty_like(stream, x0_prev) if x_c is None else x_c
+    x_next = _empty_like(stream, x0_prev) if x_next is None else x_next
     _check(lib().gc_transport_unipc(_dev(x0_prev, "x0_prev"), _dev(x0_anchor_new, "x0_anchor_new"),
                                     _dev(corr, "corr") if corr.numel() else None,
                                     _dev(weights, "weights") if weights.numel() else None, *_index_args(index),
@@ -726,9 +748,9 @@ def gc_transport_unipc_geom(x0_prev: torch.Tensor, x0_anchor_new: torch.Tensor, 
     for name, t in (("x_cur", x_cur), ("x_prev", x_prev), ("m_km2", m_km2)):
         if t is not None and (t.shape != x0_prev.shape or t.dtype != x0_prev.dtype):
             raise ValueError(f"{name} must match x0_prev in shape and dtype")
-    x0_out = torch.empty_like(x0_prev) if x0_out is None else x0_out
-    x_c = torch.empty_like(x0_prev) if x_c is None else x_c
-    x_next = torch.empty_like(x0_prev) if x_next is None else x_next
+    x0_out = _empty_like(stream, x0_prev) if x0_out is None else x0_out
+    x_c = _empty_like(stream, x0_prev) if x_c is None else x_c
+    x_next = _empty_like(stream, x0_prev) if x_next is None else x_next
     fb, fr, nf = _fg_args(fg_index)
     _check(lib().gc_transport_unipc_geom(_dev(x0_prev, "x0_prev"), _dev(x0_anchor_new, "x0_anchor_new"),
                                          _dev(pos, "pos"), _dev(cams, "cams"), _dev(bbox, "bbox"), fb, fr, nf,
@@ -795,7 +817,7 @@ def gc_coverage_pairs(pos: torch.Tensor, cams: torch.Tensor, bbox: torch.Tensor,
         raise ValueError(f"cams must be uint8 [B={B}, N={N}, 68]")
     wpr = (H * W + 31) // 32
     if out is None:
-        out = torch.empty((N, B, N, wpr), dtype=torch.int32, device=pos.device)
+        out = _empty(stream, (N, B, N, wpr), torch.int32, pos.device)
     if tuple(out.shape) != (N, B, N, wpr) or out.element_size() != 4:
         raise ValueError(f"out must be a 32-bit [{N}, {B}, {N}, {wpr}] tensor")
     _check(lib().gc_coverage_pairs(_dev(pos, "pos"), _dev(cams, "cams"), _dev(bbox, "bbox"), B, N, H, W,
@@ -808,7 +830,7 @@ def gc_coverage_init(pos: torch.Tensor, out: torch.Tensor = None, stream=None) -
     """Staleness uint8 [B, N, H, W]: 0 for foreground tokens, 255 for background."""
     B, N, H, W, _ = pos.shape
     if out is None:
-        out = torch.empty((B, N, H, W), dtype=torch.uint8, device=pos.device)
+        out = _empty(stream, (B, N, H, W), torch.uint8, pos.device)
     _check(lib().gc_coverage_init(_dev(pos, "pos"), B, N, H, W, _dev(out, "stale"), _stream(stream)),
            "gc_coverage_init")
     _keep(stream, (out,))
@@ -825,7 +847,7 @@ def gc_coverage_update(pair_bits: torch.Tensor, stale: torch.Tensor, anchors: Se
     B, N, H, W = stale.shape
     arr = (ctypes.c_int32 * len(anchors))(*anchors)
     if stats is None:
-        stats = torch.empty((B, N, 4), dtype=torch.int32, device=stale.device)
+        stats = _empty(stream, (B, N, 4), torch.int32, stale.device)
     if tuple(stats.shape) != (B, N, 4) or stats.element_size() != 4:
         raise ValueError(f"stats must be a 32-bit [{B}, {N}, 4] tensor")
     _check(lib().gc_coverage_update(_dev(pair_bits, "pair_bits"), B, N, H, W, arr, len(anchors), R,
@@ -845,9 +867,9 @@ def gc_coverage_select(pair_bits: torch.Tensor, stale: torch.Tensor, a: int, for
     device int32 [a], ascending.  Enqueued only: read it after a sync."""
     B, N, H, W = stale.shape
     if out is None:
-        out = torch.empty(a, dtype=torch.int32, device=stale.device)
+        out = _empty(stream, a, torch.int32, stale.device)
     if workspace is None:
-        workspace = torch.empty(gc_coverage_workspace_bytes(), dtype=torch.uint8, device=stale.device)
+        workspace = _empty(stream, gc_coverage_workspace_bytes(), torch.uint8, stale.device)
     farr = (ctypes.c_int32 * max(len(forced), 1))(*forced)
     _check(lib().gc_coverage_select(_dev(pair_bits, "pair_bits"), _dev(stale, "stale"), B, N, H, W, a, farr,
                                     len(forced), _dev(out, "anchors_out"), _dev(workspace, "workspace"),
@@ -866,9 +888,9 @@ def gc_coverage_score(pair_bits: torch.Tensor, stale: torch.Tensor, sets: Sequen
         raise ValueError("candidate sets must have the same size")
     flat = (ctypes.c_int32 * (M * a))(*[int(u) for S in sets for u in S])
     if out is None:
-        out = torch.empty(M, dtype=torch.int64, device=stale.device)
+        out = _empty(stream, M, torch.int64, stale.device)
     if workspace is None:
-        workspace = torch.empty(gc_coverage_workspace_bytes(), dtype=torch.uint8, device=stale.device)
+        workspace = _empty(stream, gc_coverage_workspace_bytes(), torch.uint8, stale.device)
     _check(lib().gc_coverage_score(_dev(pair_bits, "pair_bits"), _dev(stale, "stale"), B, N, H, W, flat, M, a,
                                    _dev(out, "scores"), _dev(workspace, "workspace"),
                                    workspace.numel() * workspace.element_size(), _stream(stream)),
@@ -877,10 +899,10 @@ def gc_coverage_score(pair_bits: torch.Tensor, stale: torch.Tensor, sets: Sequen
     return out
 
 
-def _stats_out(stale: torch.Tensor, stats: Optional[torch.Tensor]) -> torch.Tensor:
+def _stats_out(stale: torch.Tensor, stats: Optional[torch.Tensor], stream) -> torch.Tensor:
     B, N = stale.shape[:2]
     if stats is None:
-        stats = torch.empty((B, N, 4), dtype=torch.int32, device=stale.device)
+        stats = _empty(stream, (B, N, 4), torch.int32, stale.device)
     if tuple(stats.shape) != (B, N, 4) or stats.element_size() != 4:
         raise ValueError(f"stats must be a 32-bit [{B}, {N}, 4] tensor")
     return stats
@@ -896,11 +918,11 @@ def gc_coverage_update_select(pair_bits: torch.Tensor, stale: torch.Tensor, anch
         raise ValueError("stale must be uint8 [B, N, H, W]")
     B, N, H, W = stale.shape
     arr = (ctypes.c_int32 * len(anchors))(*anchors)
-    stats = _stats_out(stale, stats)
+    stats = _stats_out(stale, stats, stream)
     if out is None:
-        out = torch.empty(a_next, dtype=torch.int32, device=stale.device)
+        out = _empty(stream, a_next, torch.int32, stale.device)
     if workspace is None:
-        workspace = torch.empty(gc_coverage_workspace_bytes(), dtype=torch.uint8, device=stale.device)
+        workspace = _empty(stream, gc_coverage_workspace_bytes(), torch.uint8, stale.device)
     farr = (ctypes.c_int32 * max(len(forced), 1))(*forced)
     _check(lib().gc_coverage_update_select(_dev(pair_bits, "pair_bits"), B, N, H, W, arr, len(anchors), R,
                                            _dev(stale, "stale"), _dev(stats, "stats"), a_next, farr, len(forced),
@@ -925,11 +947,11 @@ def gc_coverage_update_score(pair_bits: torch.Tensor, stale: torch.Tensor, ancho
     if any(len(S) != a_set for S in sets):
         raise ValueError("candidate sets must have the same size")
     flat = (ctypes.c_int32 * (M * a_set))(*[int(u) for S in sets for u in S])
-    stats = _stats_out(stale, stats)
+    stats = _stats_out(stale, stats, stream)
     if out is None:
-        out = torch.empty(M, dtype=torch.int64, device=stale.device)
+        out = _empty(stream, M, torch.int64, stale.device)
     if workspace is None:
-        workspace = torch.empty(gc_coverage_workspace_bytes(), dtype=torch.uint8, device=stale.device)
+        workspace = _empty(stream, gc_coverage_workspace_bytes(), torch.uint8, stale.device)
     _check(lib().gc_coverage_update_score(_dev(pair_bits, "pair_bits"), B, N, H, W, arr, len(anchors), R,
                                           _dev(stale, "stale"), _dev(stats, "stats"), flat, M, a_set,
                                           _dev(out, "scores"), _dev(workspace, "workspace"),
@@ -1079,7 +1101,7 @@ def gc_rope_table(n_pos: int, sections: Sequence[int], base: float = 10000.0, sc
         raise ValueError("n_pos must be at least 1")
     fresh = []
     if table is None:
-        table = torch.empty((n_pos, max(0, columns), 2), dtype=torch.float32, device=device)
+        table = _empty(stream, (n_pos, max(0, columns), 2), torch.float32, device)
         fresh.append(table)
     if table.dtype != torch.float32 or table.shape != (n_pos, columns, 2):
         raise ValueError(f"table must be float32 [{n_pos}, {columns}, 2]")
@@ -1101,7 +1123,7 @@ def gc_rope(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, secti
     args = _rope_args(positions, table, sections, x)
     T, H, D = x.shape
     if out is None:
-        out = torch.empty_like(x, memory_format=_CONTIGUOUS)
+        out = _empty_like(stream, x)
         ho = _Heads(out.data_ptr(), H * D, D)
         fresh = (out,)
     else:
@@ -1131,13 +1153,13 @@ def gc_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_gain: torch.Tensor, k_ga
     args = _rope_args(positions, table, sections, q)
     fresh = []
     if q_out is None:
-        q_out = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        q_out = _empty_like(stream, q)
         ho = _Heads(q_out.data_ptr(), H * D, D)
         fresh.append(q_out)
     else:
         ho = _heads(_like_heads(q_out, "q_out", q.shape, q), "q_out")
     if k_out is None:
-        k_out = torch.empty_like(k, memory_format=_CONTIGUOUS)
+        k_out = _empty_like(stream, k)
         hp = _Heads(k_out.data_ptr(), Hk * D, D)
         fresh.append(k_out)
     else:
@@ -1230,20 +1252,20 @@ def gc_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attent
     hq, hk, hv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     fresh = []
     if out is None:
-        out = torch.empty_like(q, memory_format=_CONTIGUOUS)
+        out = _empty_like(stream, q)
         ho = _Heads(out.data_ptr(), H * D, D)
         fresh.append(out)
     else:
         ho = _heads(_like_heads(out, "out", q.shape, q), "out")
     if lse is None:
-        lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+        lse = _empty(stream, (H, T), torch.float32, q.device)
         fresh.append(lse)
     elif lse.dtype != torch.float32 or lse.shape != (H, T) or lse.get_device() != device:
         raise ValueError(f"lse must be float32 [{H}, {T}] on {q.device}")
     at, size = None, 0
     if need:
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = _empty(stream, need, torch.uint8, q.device)
             fresh.append(workspace)
         elif workspace.get_device() != device:
             raise ValueError(f"workspace must be on {q.device} (got {workspace.device})")
@@ -1339,19 +1361,19 @@ def gc_add_rms_norm(x: torch.Tensor, residual: torch.Tensor = None, gain: torch.
     if residual is not None:
         hr = _like_rows(residual, "residual", shape, x.dtype, device)
         if total is None:
-            total = torch.empty_like(x, memory_format=_CONTIGUOUS)
+            total = _empty_like(stream, x)
             ht = _Rows(total.data_ptr(), width)
             fresh.append(total)
     if total is not None and ht is None:
         ht = _like_rows(total, "total", shape, x.dtype, device)
     if out is None:
-        out = torch.empty_like(x, dtype=out_dtype, memory_format=_CONTIGUOUS)
+        out = _empty_like(stream, x, out_dtype)
         ho = _Rows(out.data_ptr(), width)
         fresh.append(out)
     else:
         ho = _like_rows(out, "out", shape, out_dtype, device)
     if out_code == GC_E4M3 and out_scale is None:
-        out_scale = torch.empty((n,), dtype=torch.float32, device=x.device)
+        out_scale = _empty(stream, (n,), torch.float32, x.device)
         scale_at = out_scale.data_ptr()
         fresh.append(out_scale)
     else:
@@ -1375,13 +1397,13 @@ def gc_quantize_rows(x: torch.Tensor, out: torch.Tensor = None, out_scale: torch
     device, handle = _device_of(x, stream)
     fresh = []
     if out is None:
-        out = torch.empty_like(x, dtype=torch.float8_e4m3fn, memory_format=_CONTIGUOUS)
+        out = _empty_like(stream, x, torch.float8_e4m3fn)
         ho = _Rows(out.data_ptr(), width)
         fresh.append(out)
     else:
         ho = _like_rows(out, "out", shape, torch.float8_e4m3fn, device)
     if out_scale is None:
-        out_scale = torch.empty((n,), dtype=torch.float32, device=x.device)
+        out_scale = _empty(stream, (n,), torch.float32, x.device)
         scale_at = out_scale.data_ptr()
         fresh.append(out_scale)
     else:
@@ -1435,7 +1457,7 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
         raise ValueError(f"out_dtype must be float32 or bfloat16 (got {out_dtype})")
     fresh = []
     if out is None:
-        out = x.new_empty((n, n_out), dtype=out_dtype)
+        out = x.new_empty((n, n_out), dtype=out_dtype) if stream is None else _empty(stream, (n, n_out), out_dtype, x.device)
         ho = _Rows(out.data_ptr(), n_out)
         fresh.append(out)
     else:
@@ -1445,7 +1467,7 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
     need = lib().gc_linear_workspace_bytes(n, n_out, n_in, code, gated)
     if need > 0:
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+            workspace = _empty(stream, need, torch.uint8, x.device)
             fresh.append(workspace)
         elif workspace.get_device() != device:
             raise ValueError(f"workspace must be on {x.device} (got {workspace.device})")
