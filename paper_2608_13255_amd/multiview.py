@@ -94,6 +94,7 @@ class _SlicedAttention:
         self.q_gain = torch.ones(dim, dtype=torch.float32, device=dev)
         self.k_gain = torch.ones(dim, dtype=torch.float32, device=dev)
         self._slices: OrderedDict[Tuple[int, ...], TokenSlice] = OrderedDict()   # the one used last at the end
+        self._captured: Dict[int, _Shared] = {}                           # what graphs read at their replays
 
     def slice(self, views: Sequence[int]) -> TokenSlice:
         """The tokens of a list of views, built where it is not among the
@@ -118,6 +119,13 @@ class _SlicedAttention:
             self._slices.popitem(last=False)
         return got
 
+    def _uses(self, shared: _Shared) -> None:
+        """Work on the current stream reads `shared`; where that is captured
+        into a graph, each of its replays does, for as long as the layer lives."""
+        shared.used_here()
+        if torch.cuda.is_current_stream_capturing():
+            self._captured[id(shared)] = shared
+
     def _tokens(self, x: torch.Tensor, views: Sequence[int], weights: Sequence[Optional[torch.Tensor]]):
         """(slice, its tokens of x), after the checks of a call."""
         shape = (self.B, len(views), self.H, self.W, self.width)
@@ -127,7 +135,7 @@ class _SlicedAttention:
         if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, *weights)):
             raise ValueError("the layer has no gradient: call it under torch.no_grad(), or on tensors that require none")
         s = self.slice(views)
-        s.used_here()
+        self._uses(s)
         return s, x.reshape(-1, self.width)[s.index]
 
     def _attend(self, qkv: torch.Tensor, s: TokenSlice) -> torch.Tensor:
@@ -150,7 +158,9 @@ class MultiViewAttention(_SlicedAttention):
     norms of queries and keys and rotary positions, between a fused input
     projection and an output projection.  The forward pass only: a call that
     torch would record for a gradient is refused.  One layer may be called
-    under several streams and from several threads at the same time."""
+    under several streams and from several threads at the same time.  A call
+    on views whose slice is known may be captured into a graph, which may be
+    replayed while the layer lives."""
 
     def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int,
                  dtype: torch.dtype = torch.bfloat16, sections: Optional[Sequence[int]] = None, base: float = 10000.0,
@@ -182,7 +192,8 @@ class MultiViewBlock(_SlicedAttention):
     part, gated (act(gate) * value) or not.  With lay_out_in_8_bits() the
     products' operands are 8-bit rows with a scale each.  The forward pass only: a call that
     torch would record for a gradient is refused.  One block may be called under several streams and from several
-    threads at the same time."""
+    threads at the same time.  A call on views whose slice is known may be captured into a graph, which may be replayed
+    while the block lives; it goes on with the 8-bit rows that it was captured with."""
 
     def __init__(self, pos: torch.Tensor, width: int, heads: int, kv_heads: int, dim: int, hidden: int,
                  act: int = GC_ACT_SILU, gated: bool = True, dtype: torch.dtype = torch.bfloat16,
@@ -239,7 +250,7 @@ class MultiViewBlock(_SlicedAttention):
                                             self.b_down, self.q_gain, self.k_gain, self.attention_gain, self.feed_gain))
         rows = self.eight_bits                                            # (another thread may lay them out again)
         if rows is not None:
-            rows.used_here()
+            self._uses(rows)
         normed = torch.float8_e4m3fn if rows is not None else self.dtype
         n, scale, _ = gc_add_rms_norm(tokens, gain=self.attention_gain, eps=self.eps, out_dtype=normed)
         out = self._attend(self._product("w_qkv", rows, n, scale), s)

@@ -17,7 +17,7 @@ def block_with(numbers):
     block.width, block.heads, block.kv_heads, block.dim, block.hidden = 16, 2, 1, 16, 32
     block.dtype, block.eps, block.act, block.gated = torch.float32, 1e-6, 1, False
     block.foreground = torch.ones((1, 1, 1, 1), dtype=torch.bool)
-    block.eight_bits = None
+    block.eight_bits, block._captured = None, {}
     for name in NAMES:
         setattr(block, name, torch.full((1, 1), float(numbers[name])))
         setattr(block, "b" + name[1:], None)
@@ -55,6 +55,7 @@ def test_a_call_keeps_the_weights_it_began_with(monkeypatch, quantized):
     block = block_with(dict.fromkeys(NAMES, 1))
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
     block.lay_out_in_8_bits()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     monkeypatch.setattr(block, "_tokens", lambda x, views, weights: (SimpleNamespace(), torch.zeros(3, 32)), raising=False)
     monkeypatch.setattr(block, "_attend", lambda qkv, s: torch.zeros(3, 32), raising=False)
     monkeypatch.setattr(block, "_spread", lambda y, x, s: y, raising=False)
@@ -102,3 +103,16 @@ def test_a_copy_is_known_on_no_stream():
     other = copy.deepcopy(rows)
     assert not other.known_streams and rows.known_streams == {77}
     assert torch.equal(other["w_in"][0], rows["w_in"][0]) and other["w_in"][0] is not rows["w_in"][0]
+
+
+def test_what_a_graph_reads_stays(monkeypatch):
+    """A slice or weights that a captured call reads are kept with the layer, those of other calls are not."""
+    block = block_with(dict.fromkeys(NAMES, 1))
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: Stream())
+    shared = [multiview.EightBitWeights({"w_in": (torch.zeros(2), torch.ones(1))}) for _ in range(2)]
+    for s in shared:
+        s.known_streams.add(Stream.cuda_stream)
+    for capturing, s in ((False, shared[0]), (True, shared[1]), (True, shared[1])):
+        monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+        block._uses(s)
+    assert [c is shared[1] for c in block._captured.values()] == [True]

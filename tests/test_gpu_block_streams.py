@@ -1,5 +1,6 @@
-"""A block used on several streams while its weights are laid out again: what a
-call that is behind has yet to read stays its own."""
+"""A block used on several streams, or captured into a graph, while its weights
+are laid out again or its slices give way to others: what a call has yet to read
+stays its own."""
 import pytest
 import torch
 
@@ -58,3 +59,41 @@ def test_weights_laid_out_again_while_another_stream_reads_them():
     torch.cuda.synchronize()
     assert torch.equal(got, want)
     assert not torch.equal(block(x, [0, 3]), want)
+
+
+@pytest.mark.parametrize("in_eight", [False, True])
+def test_a_graph_replayed_after_its_slice_and_weights_gave_way(in_eight):
+    """The captured call's slice is no longer among those used last, and the weights were laid out again: their memory is not
+    handed out while the layer lives, and replays go on with them."""
+    block, g = small_block(21)
+    block.MOST_SLICES = 2
+    place = torch.randn((1, 2, 16, 16, 64), generator=g, device=DEV).bfloat16()
+    if in_eight:
+        block.lay_out_in_8_bits()
+    block(place, [0, 3])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = block(place, [0, 3])
+    inputs = [torch.randn((1, 2, 16, 16, 64), generator=g, device=DEV).bfloat16() for _ in range(3)]
+    want = [block(x, [0, 3]) for x in inputs]
+    s, rows = block.slice([0, 3]), block.eight_bits
+    held = [s.index, s.positions, s.plan.items] + ([t for pair in rows.values() for t in pair] if in_eight else [])
+    at, sizes = {t.data_ptr() for t in held}, {t.numel() * t.element_size() for t in held}
+    del s, rows, held
+    for views in ([1, 2], [2, 3], [4, 5]):
+        block.slice(views)
+    if in_eight:
+        block.w_in.mul_(2)
+        block.lay_out_in_8_bits()
+    torch.cuda.synchronize()
+    assert (0, 3) not in block._slices
+    later = [torch.zeros(n, dtype=torch.uint8, device=DEV) for n in sizes for _ in range(4)]
+    assert not at & {t.data_ptr() for t in later}
+    for x, y in zip(inputs, want):
+        place.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, y)
+        block(x, [1, 2]).sum().item()
+    for x, y in zip(inputs, want):
+        assert torch.equal(block(x, [0, 3]), y) != in_eight
