@@ -21,9 +21,17 @@ from dataclasses import dataclass, field
 from typing import Dict, List, Optional, Sequence, Set, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import (GC_ACT_SILU, GC_MAX_VIEWS, GC_ROPE_HALF, AttentionPlan, gc_add_rms_norm, gc_attention, gc_attention_plan,
                gc_linear, gc_qk_norm_rope, gc_quantize_rows, gc_rope_table)
+
+
+def _has_tangent(tensors: Sequence[Optional[torch.Tensor]]) -> bool:
+    """Whether torch carries a forward-mode derivative of one of them along."""
+    if getattr(forward_ad, "_current_level", 0) < 0 or torch.is_inference_mode_enabled():   # (no dual_level() is open)
+        return False
+    return any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 class _Shared:
@@ -134,6 +142,9 @@ class _SlicedAttention:
                              f"{list(x.shape)} on {x.device})")
         if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, *weights)):
             raise ValueError("the layer has no gradient: call it under torch.no_grad(), or on tensors that require none")
+        if _has_tangent((x, *weights)):
+            raise ValueError("the layer has no gradient, of forward mode either: call it under torch.inference_mode(), or on "
+                             "tensors without tangents")
         s = self.slice(views)
         self._uses(s)
         return s, x.reshape(-1, self.width)[s.index]
