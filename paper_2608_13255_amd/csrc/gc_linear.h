@@ -211,9 +211,10 @@ struct BF16 : Blocks16 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, c, 0, 0, 0);
   }
 };
-// The 8-bit products add their terms to fewer bits than float32 has: over rows of 64 to 4096 they are 1.3e-5 off in the
-// 2-norm, 7e-5 with channels of 100 times the others' size.  A bfloat16 result is rounded by 1.7e-3, so it takes
-// them; for a float32 result the operands become bfloat16 first, which holds them exactly.
+// The 8-bit products add their terms to fewer bits than float32 has: over rows of 64 to 4096 they are 1.2e-5 of the products' root
+// sum of squares off in the 2-norm, 7e-5 with channels of 100 times the others' size, whatever the sum itself is.  A bfloat16
+// result is rounded by 1.7e-3 of itself, so it takes them; for a float32 result the operands become bfloat16 first, which
+// holds them exactly.
 struct E4M3Exact : Blocks32 {
   static constexpr int kChunks = 1, kProducts = 2;
   static constexpr bool kTotals = false;
