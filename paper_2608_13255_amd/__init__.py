@@ -1432,8 +1432,9 @@ def gc_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor = None, act: 
     one type: float32, bfloat16, or torch.float8_e4m3fn with a float32 scale
     for each row of x and of w.  gated: w and bias have 2 n_out rows, and the
     result is act(p of the first n_out) * p of the others + residual.  The
-    result is of out_dtype (default: residual's or out's type, else x's, bfloat16 for 8-bit
-    operands); float32 only with float32 operands.  out may be residual.
+    result is of out_dtype (default: out's or residual's type, else x's,
+    bfloat16 for 8-bit operands): float32 with any operands, bfloat16 with
+    bfloat16 and 8-bit ones.  out may be residual.
     workspace: gc_linear_workspace_bytes for this call (allocated if None)."""
     hx, hw = _rows(x, "x"), _rows(w, "w")
     code = _ROW_CODES.get(x.dtype)
