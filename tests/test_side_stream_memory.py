@@ -1,6 +1,4 @@
 """Where the binding takes memory from for a call on an explicit stream (torch's streams replaced, no GPU)."""
-import contextlib
-
 import pytest
 import torch
 
@@ -32,17 +30,15 @@ def test_memory_comes_from_the_stream_that_works_on_it(gc, monkeypatch, name, si
     current, places = ["here"], []
     real = torch.empty
 
-    @contextlib.contextmanager
-    def under(stream):
-        current.append(stream)
-        yield
-        current.pop()
+    def set_stream(stream):
+        current[0] = stream
 
     def empty(*args, **kwargs):
-        places.append(current[-1])
+        places.append(current[0])
         return real(*args, **kwargs)
 
-    monkeypatch.setattr(torch.cuda, "stream", under)
+    monkeypatch.setattr(torch.cuda, "set_stream", set_stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: current[0])
     monkeypatch.setattr(torch, "empty", empty)
     monkeypatch.setattr(gc, "_side_stream", lambda stream: stream if side else None)
     with pytest.raises(ValueError, match="device tensor"):
