@@ -836,9 +836,9 @@ int gc_quantize_rows(const gc_rows* x, int64_t n_rows, int width, int dtype, con
  * out and workspace may otherwise share no byte with an input or each other (columns of one buffer are apart).
  * The result does not depend on the order in which blocks run, but which products are added first depends on the sizes.
  * The sum is multiplied by x_scale first.  With GC_E4M3 operands, a GC_BF16 result and more than 16 rows the sum is that of the
- * 8-bit matrix units, which hold fewer bits than float32: it is off by at most 2^-7 of the largest product of each 64
- * columns, added up (2^-11.8 of that at most where it was measured), and by 1.2e-5 of the products' root sum of squares in the
- * 2-norm, 7e-5 where one channel in 64 is 100 times the others' size.  Where the products cancel that may be more than the sum.
+ * 8-bit matrix units, which hold fewer bits than float32: measured, it is off by up to 2^-11.8 of the largest product of each
+ * 64 columns, added up (tests hold it to 2^-7), and by 1.2e-5 of the products' root sum of squares in the 2-norm, 7e-5 where one
+ * channel in 64 is 100 times the others' size.  Where the products cancel that may be more than the sum.
  * At most 16 rows, and a GC_F32 result, have float32's sum.
  * gc_linear_workspace_bytes: -1 for sizes that gc_linear refuses.
  */
